@@ -237,6 +237,37 @@ size_t kvq_chunk_workspace_bytes(const kvq_cache* cache, int32_t n_q);
 kvq_status kvq_chunk_attention(const kvq_cache* cache, const void* q, int32_t n_q, float* out, void* ws,
                                size_t ws_bytes, void* stream);
 
+/* Workspace bytes that kvq_window_attention needs for n_q queries per
+ * sequence at any lengths, under the current split setting; 0 if n_q is
+ * outside [1, KVQ_MAX_CHUNK], window < 1 or sinks < 0. */
+size_t kvq_window_workspace_bytes(const kvq_cache* cache, int32_t n_q, int32_t window, int32_t sinks);
+
+/* Attention of the last n_q tokens of every sequence over a sliding window of
+ * its cache and the sequence's first tokens, which stay visible (sinks):
+ * query i of sequence s, the token at position p = L_s - n_q + i, attends to
+ * the tokens t <= p with t > p - window or t < sinks,
+ *   out[s][i][h][:] = softmax over those t of
+ *                     (q[s][i][h] . K^[s][kv(h)][t] / sqrt(d)) V^[s][kv(h)]
+ * (the decoder's attention of kvq_decode_attention and kvq_chunk_attention
+ * over fewer tokens, for models whose layers have such a window and for
+ * contexts whose full attention costs too much).  A query always sees its own
+ * token, so no row is empty; window >= L_s is full attention.  n_q = 1 is the
+ * decode step's form: a sequence without tokens yields zeros.  With n_q > 1
+ * every sequence must hold at least n_q tokens.  All classes, contiguous and
+ * paged.  Nothing outside the key groups that the windows and the sinks touch
+ * is read; the cache keeps every token (kvq_seq_release frees them).
+ * q: device fp16 [batch][n_q][Hq][d], finite; out: device fp32
+ * [batch][n_q][Hq][d]; ws: device scratch of ws_bytes >=
+ * kvq_window_workspace_bytes(cache, n_q, window, sinks), 16-byte aligned,
+ * contents undefined on entry and exit; calls that may overlap take one each.
+ * Results are within 1e-5 (2-norm) of the exact ones, and bitwise
+ * reproducible for a fixed split setting.
+ * Errors: KVQ_ERR_ARG (n_q, window or sinks out of range, a sequence shorter
+ * than n_q > 1, null pointers, misaligned workspace), KVQ_ERR_CAPACITY
+ * (workspace too small), KVQ_ERR_HIP. */
+kvq_status kvq_window_attention(const kvq_cache* cache, const void* q, int32_t n_q, int32_t window, int32_t sinks,
+                                float* out, void* ws, size_t ws_bytes, void* stream);
+
 /* Dequantize tokens [tok0, tok0 + ntok) of one sequence into device fp32
  * K_out, V_out [ntok][Hkv][d]: fmaf(code, s, z) for packed tokens (the
  * exact z + code*s rounded once to fp32) and the fp16 value for tail

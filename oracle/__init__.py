@@ -208,6 +208,26 @@ def chunk_seq(q, K, V, bits_k: int, bits_v: int, key_group: int, value_group: in
     return out
 
 
+def window_attention(q, Khat: np.ndarray, Vhat: np.ndarray, window: int, sinks: int):
+    """fp64 attention of the last n_q positions over a sliding window and the first tokens.
+
+    q fp16 [n_q][Hq][d]; Khat, Vhat fp64 [Hkv][L][d].  Query i, position
+    p = L - n_q + i, attends to the tokens t <= p with t > p - window or
+    t < sinks: the decode attention above on those tokens alone.
+    """
+    qu = _as_u16(q)
+    n_q = qu.shape[0]
+    L = Khat.shape[1]
+    if not 1 <= n_q <= L or window < 1 or sinks < 0:
+        raise OracleError(ERR_ARG, "window_attention: need 1 <= n_q <= L, window >= 1, sinks >= 0")
+    out = np.zeros((n_q,) + qu.shape[1:], dtype=np.float64)
+    for i in range(n_q):
+        p = L - n_q + i
+        t = np.array([t for t in range(p + 1) if t > p - window or t < sinks])
+        out[i] = attention(qu[i], Khat[:, t], Vhat[:, t])
+    return out
+
+
 def decode_seq(q, K, V, bits_k: int, bits_v: int, key_group: int, value_group: int,
                window: int, heads: Optional[List[int]] = None):
     """Quantize one sequence's cache, dequantize it and attend.

@@ -42,7 +42,8 @@ SOURCES = [
     ("kvq_api.cpp", [], None),
 ] + [("decode_mfma.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}", f"-DKVQ_BV={bv}"], f"decode_mfma_k{bk}v{bv}.o")
      for bk, bv in MATRIX_CLASSES] + [
-    ("decode_exact.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}"], f"decode_exact_k{bk}.o") for bk in (1, 2, 4, 8)]
+    ("decode_exact.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}"], f"decode_exact_k{bk}.o") for bk in (1, 2, 4, 8)] + [
+    ("decode_exact.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}", "-DKVQ_WINDOW"], f"window_k{bk}.o") for bk in (1, 2, 4, 8)]
 
 
 def _compile(src, extra, verbose, obj_name=None):

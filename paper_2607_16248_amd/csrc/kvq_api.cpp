@@ -711,30 +711,64 @@ struct FusedAppend {
   const std::vector<int32_t>* L_old;
 };
 
-kvq_status run_partials(const kvq_cache* c, const SplitPlan& p, const void* q, void* ws, size_t ws_bytes,
-                        void* stream, const FusedAppend* app = nullptr, float* out = nullptr) {
+// The parts of a launch's arguments that follow from the cache and its rows.
+void fill_args(kvq::DecodeArgs& a, const kvq_cache* c, int seq0, const Rows& r, const void* q, void* ws) {
   const kvq_cache_desc& d = c->d;
-  const size_t need = (size_t)p.required * d.num_q_heads * p.nqry * kvq::kRecFloats * sizeof(float);
-  if (!q) return fail(KVQ_ERR_ARG, "q must be a device pointer");
+  const HeadLayout& lay = c->lay[seq0];
+  a.arena = c->arena;
+  a.q = static_cast<const uint16_t*>(q);
+  a.ws = static_cast<float*>(ws);
+  a.head_stride = lay.stride;
+  a.kc = kvq::region_units(lay.kc); a.km = kvq::region_units(lay.km); a.vc = kvq::region_units(lay.vc);
+  a.vm = kvq::region_units(lay.vm); a.tk = kvq::region_units(lay.tk); a.tv = kvq::region_units(lay.tv); a.vb = kvq::region_units(lay.vb);
+  a.hq = d.num_q_heads; a.hkv = d.num_kv_heads; a.gk = d.key_group; a.gv = d.value_group; a.W = c->W;
+  a.qscale = (float)(1.4426950408889634 / std::sqrt((double)d.head_dim));
+  a.nqry = r.nqry; a.qpr = r.qpr; a.nrg = r.nrg; a.gqh = d.num_q_heads / d.num_kv_heads;
+  // rows past qpr whole queries (a chunk kernel group of five heads) are
+  // spare: row_x = kvq::kSpareRow marks them (a repeat of the last query)
+  for (int g = 0; g < 32; ++g) {
+    a.row_x[g] = g < r.qpr * a.gqh ? g / a.gqh : kvq::kSpareRow;
+    a.row_off[g] = a.row_x[g] * d.num_q_heads + g % a.gqh;
+  }
+  a.pm = c->pm;
+}
+
+// The launch's sequences (one bit class) and their workgroups.
+void fill_seqs(kvq::DecodeArgs& a, const kvq_cache* c, const std::vector<int>& seqs, const SplitPlan& p, const Rows& r) {
+  const int row_wgs = r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg;
+  int wg = 0, n = 0;
+  for (int i : seqs) {
+    kvq::DecodeSeq& s = a.seq[n++];
+    s.head0 = c->head0[i];
+    s.seq = i; s.L = s.L_old = c->L[i]; s.Lq = c->Lq[i];
+    s.nq = p.nq[i]; s.nsplit = p.ns[i]; s.ws_base = p.base[i];
+    s.wg_begin = wg;
+    wg += p.ns[i] * c->d.num_kv_heads * row_wgs;
+  }
+  a.nseq = n;
+  a.total_wg = wg;
+}
+
+// Whether the workspace fits `records` records of a plan's rows.
+kvq_status check_workspace(const kvq_cache* c, int64_t records, int nqry, const void* ws, size_t ws_bytes) {
+  const size_t need = (size_t)records * c->d.num_q_heads * nqry * kvq::kRecFloats * sizeof(float);
   if (need > 0 && !ws) return fail(KVQ_ERR_ARG, "workspace is NULL");
   if (ws_bytes < need) return fail(KVQ_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, need);
   if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return fail(KVQ_ERR_ARG, "workspace must be 16-byte aligned");
+  return KVQ_OK;
+}
+
+kvq_status run_partials(const kvq_cache* c, const SplitPlan& p, const void* q, void* ws, size_t ws_bytes,
+                        void* stream, const FusedAppend* app = nullptr, float* out = nullptr) {
+  const kvq_cache_desc& d = c->d;
+  if (!q) return fail(KVQ_ERR_ARG, "q must be a device pointer");
+  const kvq_status st = check_workspace(c, p.required, p.nqry, ws, ws_bytes);
+  if (st != KVQ_OK) return st;
   std::vector<int> seqs;
   for (int i = 0; i < d.batch; ++i)
     if (c->L[i] > 0) seqs.push_back(i);
-  const float qscale = (float)(1.4426950408889634 / std::sqrt((double)d.head_dim));
   for (auto& cls : bit_classes(c, seqs)) {
     kvq::DecodeArgs a{};
-    const HeadLayout& lay = c->lay[cls.second[0]];
-    a.arena = c->arena;
-    a.q = static_cast<const uint16_t*>(q);
-    a.ws = static_cast<float*>(ws);
-    a.head_stride = lay.stride;
-    a.kc = kvq::region_units(lay.kc); a.km = kvq::region_units(lay.km); a.vc = kvq::region_units(lay.vc);
-    a.vm = kvq::region_units(lay.vm); a.tk = kvq::region_units(lay.tk); a.tv = kvq::region_units(lay.tv); a.vb = kvq::region_units(lay.vb);
-    a.hq = d.num_q_heads; a.hkv = d.num_kv_heads; a.gk = d.key_group; a.gv = d.value_group; a.W = c->W;
-    a.split_tokens = p.st[cls.second[0]];
-    a.qscale = qscale;
     Rows r = rows_for(c, c->matrix[cls.second[0]] != 0, p.nqry, cls.first.first, cls.first.second);
     if (many_rows(c, cls.second[0], p.nqry)) {
       r.many = true;
@@ -743,32 +777,15 @@ kvq_status run_partials(const kvq_cache* c, const SplitPlan& p, const void* q, v
       r.nrg = (p.nqry + r.qpr - 1) / r.qpr;
       a.out = out;
     }
-    a.nqry = r.nqry; a.qpr = r.qpr; a.nrg = r.nrg; a.gqh = d.num_q_heads / d.num_kv_heads;
-    // rows past qpr whole queries (a chunk kernel group of five heads) are
-    // spare: row_x = kvq::kSpareRow marks them (a repeat of the last query)
-    for (int g = 0; g < 32; ++g) {
-      a.row_x[g] = g < r.qpr * a.gqh ? g / a.gqh : kvq::kSpareRow;
-      a.row_off[g] = a.row_x[g] * d.num_q_heads + g % a.gqh;
-    }
-    a.pm = c->pm;
+    fill_args(a, c, cls.second[0], r, q, ws);
+    a.split_tokens = p.st[cls.second[0]];
     if (app) {
       a.K_new = static_cast<const uint16_t*>(app->K);
       a.V_new = static_cast<const uint16_t*>(app->V);
       a.n_max = app->n_max;
     }
-    int wg = 0, n = 0;
-    for (int i : cls.second) {
-      kvq::DecodeSeq& s = a.seq[n++];
-      s.head0 = c->head0[i];
-      s.seq = i; s.L = c->L[i]; s.Lq = c->Lq[i];
-      s.L_old = app ? (*app->L_old)[i] : c->L[i];
-      s.nq = p.nq[i]; s.nsplit = p.ns[i]; s.ws_base = p.base[i];
-      s.wg_begin = wg;
-      const int row_wgs = r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg;
-      wg += p.ns[i] * d.num_kv_heads * row_wgs;
-    }
-    a.nseq = n;
-    a.total_wg = wg;
+    fill_seqs(a, c, cls.second, p, r);
+    for (int k = 0; app && k < a.nseq; ++k) a.seq[k].L_old = (*app->L_old)[a.seq[k].seq];
     const int e = !c->matrix[cls.second[0]] ? kvq::launch_decode(a, cls.first.first, cls.first.second, r.rows, stream)
                   : r.rows >= 16 ? kvq::launch_chunk_matrix(a, cls.first.first, cls.first.second, r.rows, stream)
                                        : kvq::launch_decode_matrix(a, cls.first.first, cls.first.second, r.rows, stream);
@@ -795,6 +812,94 @@ kvq_status run_merge(const kvq_cache* c, const SplitPlan& p, const void* ws, flo
     m.nseq = n;
     const int e = kvq::launch_merge(m, stream);
     if (e) return hip_fail(e, "merge launch");
+  }
+  return KVQ_OK;
+}
+
+// ------------------------------------------------------------ windowed attention
+
+// Rows of a windowed launch: one query's heads, or 16 rows of whole queries
+// (the last group may repeat the last query in its spare rows).
+Rows window_rows(const kvq_cache* c, int nqry) {
+  const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
+  Rows r;
+  r.nqry = nqry;
+  r.qpr = nqry == 1 ? 1 : 16 / gqh;
+  r.nrg = (nqry + r.qpr - 1) / r.qpr;
+  r.rows = 16;
+  return r;
+}
+
+// Most packed key groups that any row group of sequence i reads.
+int32_t window_reach(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks) {
+  const int32_t seen0 = c->L[i] - r.nqry + 1, gsh = log2_exact(c->d.key_group);
+  int32_t most = 0;
+  for (int rg = 0; rg < r.nrg; ++rg) {
+    const int first = rg * r.qpr, last = std::min(first + r.qpr, r.nqry) - 1;
+    most = std::max(most, kvq::window_groups(seen0 + first, seen0 + last, c->Lq[i], gsh, window, sinks).count);
+  }
+  return most;
+}
+
+// The split plan of a windowed call: every class's splits take the same number
+// of key groups, as many as leave two workgroups per compute unit (what the
+// kernel's registers allow at once) and no fewer than one group per wave.
+SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
+  SplitPlan p;
+  p.nqry = nqry;
+  const int B = c->d.batch, gk = c->d.key_group;
+  p.st.assign(B, 0);
+  p.nq.assign(B, 0);
+  p.ns.assign(B, 0);
+  p.base.assign(B, 0);
+  const Rows r = window_rows(c, nqry);
+  std::map<std::pair<int, int>, std::vector<int>> classes;
+  for (int i = 0; i < B; ++i)
+    if (c->L[i] > 0) classes[{c->bk[i], c->bv[i]}].push_back(i);
+  for (auto& cl : classes) {
+    int64_t total = 0, tails = 0, longest = 0;
+    const int64_t units = (int64_t)c->d.num_kv_heads * r.nrg;
+    for (int i : cl.second) {
+      p.nq[i] = window_reach(c, i, r, window, sinks);
+      total += p.nq[i] * units;
+      longest = std::max<int64_t>(longest, p.nq[i]);
+      if (c->L[i] > c->Lq[i]) tails += units;
+    }
+    const int64_t round = target_workgroups(2), target = std::max(round - tails, round / 2);
+    int64_t groups = c->split_tokens / gk;
+    if (groups == 0) groups = std::max<int64_t>((total + target - 1) / target, kMinGroupsPerSplit);
+    groups = std::max(groups, (longest + kMaxSplits - 1) / kMaxSplits);
+    for (int i : cl.second) {
+      p.st[i] = (int32_t)(groups * gk);
+      p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
+    }
+  }
+  for (int i = 0; i < B; ++i) {
+    p.ns[i] = p.nq[i] + (c->L[i] > c->Lq[i] ? 1 : 0);
+    p.base[i] = (int32_t)p.records;
+    p.records += p.ns[i];
+  }
+  p.required = p.records;
+  return p;
+}
+
+kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int32_t window, int32_t sinks, void* ws,
+                      size_t ws_bytes, void* stream) {
+  const kvq_status st = check_workspace(c, p.required, p.nqry, ws, ws_bytes);
+  if (st != KVQ_OK) return st;
+  std::vector<int> seqs;
+  for (int i = 0; i < c->d.batch; ++i)
+    if (c->L[i] > 0) seqs.push_back(i);
+  for (auto& cls : bit_classes(c, seqs)) {
+    kvq::DecodeArgs a{};
+    const Rows r = window_rows(c, p.nqry);
+    fill_args(a, c, cls.second[0], r, q, ws);
+    a.split_tokens = p.st[cls.second[0]];
+    a.window = window;
+    a.sinks = sinks;
+    fill_seqs(a, c, cls.second, p, r);
+    const int e = kvq::launch_window(a, cls.first.first, cls.first.second, stream);
+    if (e) return hip_fail(e, "windowed attention launch");
   }
   return KVQ_OK;
 }
@@ -913,6 +1018,39 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
       return fail(KVQ_ERR_ARG, "sequence %d holds %d tokens, fewer than the %d chunk queries", i, c->L[i], n_q);
   const SplitPlan p = plan_splits(c, n_q, ws_bytes);
   kvq_status st = run_partials(c, p, q, ws, ws_bytes, stream, nullptr, out);
+  if (st != KVQ_OK) return st;
+  st = run_merge(c, p, ws, out, stream);
+  if (st != KVQ_OK) return st;
+  return ok();
+}
+
+size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
+  if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
+  const int64_t gk = c->d.key_group, qpr = window_rows(c, n_q).qpr;
+  // a range of n tokens touches at most (n + gk - 2) / gk + 1 key groups
+  const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + qpr - 1 + gk - 2) / gk + 1);
+  const int64_t per = c->split_tokens > 0 ? c->split_tokens / gk : kMinGroupsPerSplit;
+  const int64_t splits = std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
+  return (size_t)c->d.batch * c->d.num_q_heads * n_q * (size_t)splits * kvq::kRecFloats * sizeof(float);
+}
+
+kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, int32_t window, int32_t sinks,
+                                float* out, void* ws, size_t ws_bytes, void* stream) {
+  if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
+  if (n_q < 1 || n_q > KVQ_MAX_CHUNK) return fail(KVQ_ERR_ARG, "n_q = %d outside [1, %d]", n_q, KVQ_MAX_CHUNK);
+  if (window < 1) return fail(KVQ_ERR_ARG, "window = %d must be at least 1", window);
+  if (sinks < 0) return fail(KVQ_ERR_ARG, "sinks = %d must not be negative", sinks);
+  if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
+  int32_t longest = 1;
+  for (int i = 0; i < c->d.batch; ++i) {
+    if (n_q > 1 && c->L[i] < n_q)
+      return fail(KVQ_ERR_ARG, "sequence %d holds %d tokens, fewer than the %d queries", i, c->L[i], n_q);
+    longest = std::max(longest, c->L[i]);
+  }
+  window = std::min(window, longest);
+  sinks = std::min(sinks, longest);
+  const SplitPlan p = plan_window(c, n_q, window, sinks);
+  kvq_status st = run_window(c, p, q, window, sinks, ws, ws_bytes, stream);
   if (st != KVQ_OK) return st;
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;

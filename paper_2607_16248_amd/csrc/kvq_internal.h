@@ -184,7 +184,39 @@ struct DecodeArgs {
   // blocks per split and nsplit the splits over packed and tail tokens
   // together; a sequence of one split is written to out
   float* out;         // fp32 [batch][nqry][Hq][128]
+  // windowed attention (launch_window): query position p sees token t <= p when
+  // t > p - window or t < sinks; nq counts splits of split_tokens over the row
+  // group's visible key groups (WindowGroups).  window = 0 elsewhere.
+  int32_t window, sinks;
 };
+
+// The packed key groups that a row group of windowed attention reads: the sinks'
+// (0 .. sink - 1), then the windows' (first .. first + count - sink - 1); a
+// launch's splits count through both as one list.
+struct WindowGroups {
+  int32_t sink, first, count;
+};
+#ifdef __HIPCC__
+#define KVQ_WINDOW_HD __host__ __device__
+#else
+#define KVQ_WINDOW_HD
+#endif
+// seen_first, seen_last: tokens that the group's first and last query see at
+// most (their position + 1).  The first query's window reaches back furthest.
+KVQ_WINDOW_HD inline WindowGroups window_groups(int32_t seen_first, int32_t seen_last, int32_t Lq, int32_t gk_shift,
+                                                int32_t window, int32_t sinks) {
+  const int32_t begin = seen_first > window ? seen_first - window : 0;
+  const int32_t end = Lq < seen_last ? Lq : seen_last;  // packed tokens that any query sees
+  const int32_t held = sinks < Lq ? sinks : Lq;
+  const uint32_t up = (1u << gk_shift) - 1u;
+  WindowGroups g;
+  g.first = begin >> gk_shift;
+  g.sink = (int32_t)(((uint32_t)held + up) >> gk_shift);
+  g.sink = g.sink < g.first ? g.sink : g.first;
+  const int32_t last = (int32_t)(((uint32_t)end + up) >> gk_shift);
+  g.count = g.sink + (last > g.first ? last - g.first : 0);
+  return g;
+}
 
 struct MergeSeq {
   int32_t seq, nsplit, ws_base, pad;
@@ -290,6 +322,11 @@ int launch_matrix_class(const DecodeArgs& a, int gq, void* stream);
 // The classes those kernels don't take, by key bits (decode_exact.hip).
 template <int BK>
 int launch_exact_class(const DecodeArgs& a, int bv, void* stream);
+// Windowed attention (a.window > 0) of every class, 16 rows per workgroup, by
+// key bits (decode_exact.hip).
+int launch_window(const DecodeArgs& a, int bk, int bv, void* stream);
+template <int BK>
+int launch_window_class(const DecodeArgs& a, int bv, void* stream);
 int launch_export(const ExportArgs& a, void* stream);
 int launch_merge(const MergeArgs& a, void* stream);
 int launch_dgap(const struct DgapArgs& a, int batch, void* stream);

@@ -31,4 +31,15 @@ int launch_decode(const DecodeArgs& a, int bk, int bv, int, void* stream) {
   }
 }
 
+int launch_window(const DecodeArgs& a, int bk, int bv, void* stream) {
+  if (a.total_wg <= 0) return 0;
+  switch (bk) {
+    case 1: return launch_window_class<1>(a, bv, stream);
+    case 2: return launch_window_class<2>(a, bv, stream);
+    case 4: return launch_window_class<4>(a, bv, stream);
+    case 8: return launch_window_class<8>(a, bv, stream);
+    default: return (int)hipErrorInvalidValue;
+  }
+}
+
 }  // namespace kvq

@@ -43,7 +43,9 @@ struct TailState {
 
 // Rows g0 .. g0 + 16 * NT - 1 of the workgroup's group of ROWS rows (those past
 // it repeat its first row and are dropped by the caller).
-template <int NT, int ROWS, bool CHUNK, int AHEAD = 4>
+// WINDOW: windowed attention, whose blocks outside every row's window and the
+// sinks are passed over.
+template <int NT, int ROWS, bool CHUNK, int AHEAD = 4, bool WINDOW = false>
 __device__ __forceinline__ void tail_split(const DecodeArgs& a, const DecodeSeq& S, int h, int rg, const uint8_t* ring,
                                            TailState<NT>& st, int lane, int wv) {
   typedef u4_t u4_any __attribute__((aligned(4)));
@@ -103,8 +105,18 @@ __device__ __forceinline__ void tail_split(const DecodeArgs& a, const DecodeSeq&
     return r;
   };
 
+  // windowed attention: tail tokens from `begin` on may be in a window, those
+  // below `sinks` are sinks, and none past `end` is seen
+  int begin = 0, sinks = 0, end = ntail;
+  if constexpr (WINDOW) {
+    const int j0 = min(rg * a.qpr, a.nqry - 1), j1 = min(rg * a.qpr + a.qpr - 1, a.nqry - 1);
+    begin = max(max(seen0 + j0 - a.window, 0) - S.Lq, 0);
+    sinks = a.sinks - S.Lq;
+    end = min(ntail, seen0 + j1 - S.Lq);
+  }
   bool raw[8] = {};  // per tile of 16 channels: its values enter lifted while they are small
-  for (int b = wv; 32 * b < ntail; b += kWaves) {
+  for (int b = WINDOW && sinks <= 0 ? (begin >> 5) + wv : wv; 32 * b < end; b += kWaves) {
+    if (WINDOW && 32 * b + 32 <= begin && 32 * b >= sinks) continue;
     // scores: tokens 32b + 16mb + 4blk + r of row 16u + col
     f4_t d[NT][2];
 #pragma unroll
@@ -128,10 +140,15 @@ __device__ __forceinline__ void tail_split(const DecodeArgs& a, const DecodeSeq&
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       const int left = min(lim[u] - S.Lq, ntail) - 32 * b - 4 * blk;  // token 16mb + 4blk + r is visible below it
+      // windowed attention: and from `from` on, or below `sunk`
+      const int from = WINDOW ? max(lim[u] - a.window, 0) - S.Lq - 32 * b - 4 * blk : 0;
+      const int sunk = WINDOW ? sinks - 32 * b - 4 * blk : 0;
       float s[8], top = -__builtin_inff();
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s[e] = 16 * (e >> 2) + (e & 3) < left ? d[u][e >> 2][e & 3] * a.qscale : -__builtin_inff();
+        const int i = 16 * (e >> 2) + (e & 3);
+        const bool seen = i < left && (!WINDOW || i >= from || i < sunk);
+        s[e] = seen ? d[u][e >> 2][e & 3] * a.qscale : -__builtin_inff();
         top = fmaxf(top, s[e]);
       }
       top = fmaxf(top, __shfl_xor(top, 16));

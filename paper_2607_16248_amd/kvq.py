@@ -23,6 +23,7 @@ EXPORTED = ["kvq_cache_bytes", "kvq_cache_init", "kvq_cache_destroy", "kvq_cache
             "kvq_append", "kvq_workspace_bytes", "kvq_decode_attention", "kvq_decode_attention_noalloc",
             "kvq_append_decode",
             "kvq_decode_partials", "kvq_decode_merge", "kvq_chunk_workspace_bytes", "kvq_chunk_attention",
+            "kvq_window_workspace_bytes", "kvq_window_attention",
             "kvq_dequant", "kvq_export_bytes", "kvq_export", "kvq_check",
             "kvq_set_split_tokens", "kvq_last_error", "kvq_version",
             "kvq_read_probe", "kvq_read_probe_sink_bytes",
@@ -82,6 +83,8 @@ def lib():
         "kvq_decode_attention_noalloc": ([P, P, P, P], ctypes.c_int),
         "kvq_chunk_workspace_bytes": ([P, ctypes.c_int32], S),
         "kvq_chunk_attention": ([P, P, ctypes.c_int32, P, P, S, P], ctypes.c_int),
+        "kvq_window_workspace_bytes": ([P, I32, I32, I32], S),
+        "kvq_window_attention": ([P, P, I32, I32, I32, P, P, S, P], ctypes.c_int),
         "kvq_append_decode": ([P, P, P, I32, ctypes.POINTER(I32), P, P, P, S, P], ctypes.c_int),
         "kvq_decode_partials": ([P, P, P, S, P], ctypes.c_int),
         "kvq_decode_merge": ([P, P, P, P], ctypes.c_int),
@@ -214,6 +217,20 @@ def kvq_chunk_attention(cache: int, q, n_q: int, out, ws, ws_bytes: Optional[int
                                      _stream(stream)))
 
 
+def kvq_window_workspace_bytes(cache: int, n_q: int, window: int, sinks: int = 0) -> int:
+    return int(lib().kvq_window_workspace_bytes(cache, int(n_q), int(window), int(sinks)))
+
+
+def kvq_window_attention(cache: int, q, n_q: int, window: int, sinks: int, out, ws, ws_bytes: Optional[int] = None,
+                         stream=None) -> None:
+    """The last n_q tokens of every sequence attend over the last ``window`` tokens up to their own and the first
+    ``sinks`` ones: q fp16 [batch][n_q][Hq][d], out fp32 [batch][n_q][Hq][d]."""
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().kvq_window_attention(cache, _ptr(q), int(n_q), int(window), int(sinks), _ptr(out), _ptr(ws),
+                                      int(ws_bytes), _stream(stream)))
+
+
 def kvq_append_decode(cache: int, K, V, n_new: Sequence[int], q, out, ws, ws_bytes: Optional[int] = None,
                       n_max: Optional[int] = None, stream=None) -> None:
     """kvq_append then kvq_decode_attention in one call (two launches when no key group fills)."""
@@ -339,6 +356,18 @@ class KVCache:
         need = kvq_chunk_workspace_bytes(self.handle, n_q)
         ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
         kvq_chunk_attention(self.handle, q, n_q, out, ws, stream=stream)
+        return out
+
+    def window(self, q, window, sinks=0, out=None, stream=None):
+        """Attention of the last q.shape[1] tokens over a sliding window and the first ``sinks`` tokens."""
+        import torch
+        n_q = int(q.shape[1])
+        if out is None:
+            out = torch.empty((self.batch, n_q, self.num_q_heads, self.head_dim), dtype=torch.float32,
+                              device=q.device)
+        need = kvq_window_workspace_bytes(self.handle, n_q, window, sinks)
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
+        kvq_window_attention(self.handle, q, n_q, window, sinks, out, ws, stream=stream)
         return out
 
     def append_decode(self, K, V, q, n_new=None, out=None, stream=None):

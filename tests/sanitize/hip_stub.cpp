@@ -195,6 +195,39 @@ int launch_decode_matrix(const DecodeArgs& a, int bk, int bv, int rows, void*) {
 int launch_chunk_matrix(const DecodeArgs& a, int bk, int bv, int rows, void*) {
   return check_rows(a, rows), touch_decode(a, bk, bv), 0;
 }
+// A windowed launch: the key groups of every row group's splits, which have to
+// be all that the row group sees and lie below the packed end.
+int launch_window(const DecodeArgs& a, int bk, int bv, void*) {
+  check_rows(a, 16);
+  const int gsh = a.gk == 32 ? 5 : a.gk == 64 ? 6 : 7, gps = a.split_tokens >> gsh;
+  const size_t rows = (size_t)a.hq * a.nqry;
+  auto bad = [&](const char* what, int seq) {
+    std::fprintf(stderr, "window check failed (%s): sequence %d, window %d, sinks %d\n", what, seq, a.window, a.sinks);
+    std::abort();
+  };
+  for (int i = 0; i < a.nseq; ++i) {
+    const DecodeSeq& S = a.seq[i];
+    for (int rg = 0; rg < a.nrg; ++rg) {
+      const int first = S.L - a.nqry + 1 + rg * a.qpr, last = S.L - a.nqry + std::min(rg * a.qpr + a.qpr, a.nqry);
+      const WindowGroups g = window_groups(first, last, S.Lq, gsh, a.window, a.sinks);
+      if (g.count > S.nq * gps) bad("splits", S.seq);
+      std::vector<char> held(S.Lq / a.gk, 0);
+      for (int v = 0; v < g.count; ++v) {
+        const int j = v < g.sink ? v : v - g.sink + g.first;
+        if (j >= S.Lq / a.gk || held[j]) bad("group", S.seq);
+        held[j] = 1;
+        for (int h = 0; h < a.hkv; ++h) packed_ranges(a, S.head0, S.seq, h, j * a.gk, (j + 1) * a.gk, bk, bv, rd);
+      }
+      for (int p = first; p <= last; ++p)
+        for (int t = 0; t < std::min(p, S.Lq); ++t)
+          if ((t >= p - a.window || t < a.sinks) && !held[t / a.gk]) bad("unread token", S.seq);
+    }
+    for (int h = 0; h < a.hkv; ++h) ring_ranges(a, S.head0, h, S.Lq, S.L, rd);
+    rd(a.q + (size_t)S.seq * rows * kHeadDim, rows * kTokenBytes);
+    wr(a.ws + (size_t)S.ws_base * rows * kRecFloats, S.nsplit * rows * kRecFloats * 4);
+  }
+  return ++g_launches, 0;
+}
 int launch_export(const ExportArgs& a, void*) {
   check_regions(a, nullptr);
   packed_ranges(a, a.head0, a.seq, a.h, 0, a.Lq, a.bk, a.bv, rd);

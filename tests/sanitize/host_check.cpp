@@ -127,6 +127,19 @@ static void exercise(const kvq_cache_desc& d) {
         if (st != KVQ_OK) break;
       }
     }
+    for (int nq : {1, 3, 40}) {
+      if (nq > 1 && nq > Lmin) continue;
+      for (int window : {1, 31, 100, 1 << 30})
+        for (int sinks : {0, 5, 70}) {
+          const size_t ww = kvq_window_workspace_bytes(c, nq, window, sinks);
+          Buf wws(ww);
+          EXPECT(kvq_window_attention(c, q.p, nq, window, sinks, out.as<float>(), wws.p, ww, nullptr) == KVQ_OK);
+        }
+    }
+    EXPECT(kvq_window_attention(c, q.p, 1, 0, 0, out.as<float>(), ws.p, wsb, nullptr) == KVQ_ERR_ARG);
+    EXPECT(kvq_window_attention(c, q.p, 1, 5, -1, out.as<float>(), ws.p, wsb, nullptr) == KVQ_ERR_ARG);
+    EXPECT(kvq_window_attention(c, q.p, 1, 5, 0, out.as<float>(), ws.p, 16, nullptr) == KVQ_ERR_CAPACITY);
+    EXPECT(kvq_window_workspace_bytes(c, 0, 5, 0) == 0 && kvq_window_workspace_bytes(c, 1, 0, 0) == 0);
     ++step;
   }
   for (int s = 0; s < B; ++s)
@@ -178,6 +191,7 @@ static void large_head(int bits_k, int bits_v, int gv, int max_tokens, int windo
   EXPECT(kvq_decode_attention(c, q.p, out.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
   EXPECT(kvq_chunk_attention(c, q.p, 3, out.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
   EXPECT(kvq_chunk_attention(c, q.p, 40, out.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
+  EXPECT(kvq_window_attention(c, q.p, 40, 50, 3, out.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
   EXPECT(kvq_dequant(c, 0, 0, n, ko.as<float>(), ko.as<float>(), nullptr) == KVQ_OK);
   Buf img(kvq_export_bytes(c, 0, 0));
   EXPECT(kvq_export(c, 0, 0, img.p, img.n, nullptr) == KVQ_OK);
