@@ -94,6 +94,110 @@ size_t dgap_info_floats(int32_t k);
 kvq_status dgap_restore(const dgap_params* p, float* logits, int32_t batch, void* ws, size_t ws_bytes,
                         float* info, void* stream);
 
+/* Element types of the rows of logits below. */
+typedef enum { DGAP_F32 = 0, DGAP_F16 = 1, DGAP_BF16 = 2 } dgap_type;
+
+/* Rows of logits and how a token is drawn from each (device pointers; the
+ * settings are arrays of `batch` values, one per row). */
+typedef struct {
+  const void* logits;       /* [batch] rows of `vocab` logits of `type`, row_stride elements apart */
+  int64_t row_stride;       /* >= vocab */
+  int32_t type;             /* dgap_type */
+  int32_t batch;            /* >= 1 */
+  int32_t vocab;            /* 1 .. 2^24 */
+  int32_t pad;
+  const float* temperature; /* T >= 0, finite; NULL: 1 */
+  const int32_t* top_k;     /* NULL, or k < 1 or k >= vocab in a row: off */
+  const float* top_p;       /* NULL, or p >= 1 in a row: off */
+  const float* min_p;       /* NULL, or m <= 0 in a row: off */
+  const float* uniform;     /* a number u in [0, 1) per row */
+} dgap_sampling;
+
+/* Workspace bytes dgap_sample needs; 0 if the shape is not supported. */
+size_t dgap_sample_workspace_bytes(int32_t batch, int32_t vocab);
+
+/* The next token of every row: token selection from the (restored) logits,
+ * what a decode step does after dgap_restore ("DGAP Overview", online
+ * restoration framework: decoding proceeds from z~).  In the row's descending
+ * order, equal logits by lower index, with weights e^((z - z_max) / T):
+ *   top-k keeps the first k; of their mass, top-p keeps the shortest beginning
+ *   that holds at least p of it (one element at least); min-p keeps those of
+ *   weight >= m (the largest alone where m > 1).  The token is the first of
+ *   the kept ones up to and with which their mass is more than u times all of
+ *   it (u is clipped to [0, 1 - 2^-24]).
+ * T = 0 gives the largest logit.  tokens: device int32 [batch]; logprobs: NULL
+ * or device fp32 [batch], the log of the token's share of the kept mass (0
+ * where T = 0).  A logit of -inf is never drawn (a masked token).  A row
+ * without a finite logit, with a NaN or +inf among them, or with a setting
+ * that is NaN (T: negative or infinite, too) gives token -1 and log-probability
+ * NaN.  Weights are taken to 24 bits and added up exactly in units of 2^-45 of
+ * the largest (2^-38 for the largest vocabularies): a sampled step differs
+ * from the exact one where u is within about 1e-7 of a border.
+ * ws: device scratch of ws_bytes >= dgap_sample_workspace_bytes, 16-byte
+ * aligned, contents undefined on entry and exit; calls that may overlap take
+ * one each.  Errors: KVQ_ERR_ARG (null pointers, shapes or type out of range,
+ * misaligned logits or workspace), KVQ_ERR_CAPACITY (workspace too small),
+ * KVQ_ERR_UNSUPPORTED (vocab above 2^24, more than 2^31 chunks of 8192 logits),
+ * KVQ_ERR_HIP.  Results are bitwise reproducible. */
+kvq_status dgap_sample(const dgap_sampling* p, int32_t* tokens, float* logprobs, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* Most teacher entries per row. */
+#define DGAP_MAX_TEACHER 256
+
+/* A student's logits and a teacher's top logits (device pointers). */
+typedef struct {
+  const void* logits;     /* [rows] rows of `vocab` logits of `type`, row_stride elements apart */
+  int64_t row_stride;     /* >= vocab */
+  int32_t type;           /* dgap_type */
+  int32_t rows;           /* >= 1 */
+  int32_t vocab;          /* 1 .. 2^24 */
+  int32_t k;              /* teacher entries per row, 1 .. DGAP_MAX_TEACHER */
+  const float* teacher;   /* [rows][k] the teacher's logits */
+  const int32_t* index;   /* [rows][k] their vocabulary indices */
+  float temperature;      /* T > 0, finite, and so 1 / T */
+  int32_t pad;
+} dgap_distillation;
+
+/* Workspace bytes dgap_distill needs; 0 if the shape is not supported. */
+size_t dgap_distill_workspace_bytes(int32_t rows, int32_t vocab);
+
+/* The loss of every row against the teacher's top logits, and its gradient:
+ * the Kullback-Leibler term at temperature T that DGAP's corrector is trained
+ * with against the FP16 decoder ("Selective Top-K Distribution Corrector",
+ * corrector loss: KL(q^fp || q~)), taken over the whole vocabulary on the
+ * student's side, so that it also tunes a model that will decode from a
+ * low-bit cache:
+ *   q = softmax(t / T) over the row's entries, p = softmax(z / T),
+ *   loss[r] = T^2 sum_k q_k (log q_k - log p_{i_k}),
+ *   grad[r][j] = grad_loss[r] T (p_j - sum_k q_k [i_k = j]).
+ * An index outside [0, vocab) or a teacher logit of -inf stands for no entry
+ * (rows of fewer entries); entries of one index add up; a row without entries
+ * has loss and gradient 0.  Logits are finite or -inf (p = 0: a loss of +inf
+ * where the teacher has an entry there), one of a row finite at least.
+ * loss: device fp32 [rows].  lse: NULL or device fp32 [rows], log sum e^(z/T)
+ * for dgap_distill_backward.  grad: NULL (the loss alone) or device rows of
+ * the logits' type, grad_row_stride >= vocab elements apart; it may be the
+ * logits' own memory (row strides equal), but overlap them in no other way.
+ * grad_loss: NULL (1) or device fp32 [rows].  ws: device scratch of ws_bytes
+ * >= dgap_distill_workspace_bytes, 16-byte aligned, contents undefined on entry
+ * and exit; calls that may overlap take one each.  Sums and logarithms are
+ * fp32 or wider, the gradient is rounded once; results are bitwise
+ * reproducible.  Errors: KVQ_ERR_ARG (null pointers, shapes, type or
+ * temperature out of range, misaligned logits, grad or workspace),
+ * KVQ_ERR_CAPACITY (workspace too small), KVQ_ERR_UNSUPPORTED (vocab above 2^24,
+ * more than 2^31 chunks of 8192 logits), KVQ_ERR_HIP. */
+kvq_status dgap_distill(const dgap_distillation* p, float* loss, float* lse, void* grad, int64_t grad_row_stride,
+                        const float* grad_loss, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradient alone, from the lse of an earlier dgap_distill on the same
+ * logits (a backward pass whose grad_loss was not known then).  Arguments,
+ * results and errors as there; p is as exact as the fp32 lse is (2^-24 |lse|
+ * relative), so a row's largest logit has to be a score, not a mask's lowest
+ * value. */
+kvq_status dgap_distill_backward(const dgap_distillation* p, const float* lse, const float* grad_loss, void* grad,
+                                 int64_t grad_row_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,6 +37,8 @@ SOURCES = [
     ("prefill_mfma.hip", ["-fno-honor-nans"], None),
     ("dequant.hip", [], None),
     ("dgap.hip", [], None),
+    ("sample.hip", [], None),
+    ("distill.hip", [], None),
     ("noalloc.hip", [], None),
     ("matrix_dispatch.cpp", [], None),
     ("kvq_api.cpp", [], None),

@@ -24,6 +24,7 @@
 using kvq::HeadLayout;
 
 static_assert(kvq::kScratchBytes == KVQ_NOALLOC_SCRATCH_BYTES, "scratch array size as the header states");
+static_assert(kvq::kDistillMaxK == DGAP_MAX_TEACHER, "teacher entries as the header states");
 static_assert(kvq::kSpareRow >= KVQ_MAX_CHUNK, "a spare row lies past every chunk query");
 
 struct kvq_cache {
@@ -259,6 +260,66 @@ std::vector<std::pair<std::pair<int, int>, std::vector<int>>> bit_classes(const 
     }
   }
   return out;
+}
+
+// Rows of logits that a call reads whole.
+kvq_status check_rows(const void* logits, int type, int64_t row_stride, int rows, int vocab, const char* what) {
+  if (!logits) return fail(KVQ_ERR_ARG, "logits is NULL");
+  if (type != DGAP_F32 && type != DGAP_F16 && type != DGAP_BF16) return fail(KVQ_ERR_ARG, "type %d is none of dgap_type", type);
+  if (rows < 1) return fail(KVQ_ERR_ARG, "%s must be >= 1 (got %d)", what, rows);
+  if (vocab < 1) return fail(KVQ_ERR_ARG, "vocab must be >= 1 (got %d)", vocab);
+  if (vocab > 1 << 24) return fail(KVQ_ERR_UNSUPPORTED, "vocab %d above 2^24", vocab);
+  if (row_stride < vocab) return fail(KVQ_ERR_ARG, "row_stride %lld smaller than vocab %d", (long long)row_stride, vocab);
+  if ((int64_t)rows * ((vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk) > INT32_MAX)
+    return fail(KVQ_ERR_UNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
+  const int size = type == DGAP_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % size != 0) return fail(KVQ_ERR_ARG, "logits must be aligned to their type");
+  return KVQ_OK;
+}
+
+kvq_status check_scratch(const void* ws, size_t ws_bytes, size_t need) {
+  if (!ws) return fail(KVQ_ERR_ARG, "workspace is NULL");
+  if (ws_bytes < need) return fail(KVQ_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, need);
+  if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return fail(KVQ_ERR_ARG, "workspace must be 16-byte aligned");
+  return KVQ_OK;
+}
+
+// Workspace of one row of dgap_sample (see SampleArgs::ws).
+uint64_t sample_row_bytes(int vocab) {
+  const uint64_t nchunk = (vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk;
+  return kvq::align_up(8 * (kvq::kSampleBins + kvq::kSampleList + nchunk) + 4 * (kvq::kSampleBins + 1), kvq::kAlign);
+}
+
+kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* grad, int64_t grad_row_stride,
+                        const float* grad_loss, bool need_grad) {
+  if (!p) return fail(KVQ_ERR_ARG, "parameters are NULL");
+  const kvq_status st = check_rows(p->logits, p->type, p->row_stride, p->rows, p->vocab, "rows");
+  if (st != KVQ_OK) return st;
+  if (!p->teacher || !p->index) return fail(KVQ_ERR_ARG, "teacher and index must be device pointers");
+  if (p->k < 1 || p->k > DGAP_MAX_TEACHER) return fail(KVQ_ERR_ARG, "k = %d outside [1, %d]", p->k, DGAP_MAX_TEACHER);
+  if (!(p->temperature > 0.f) || !std::isfinite(p->temperature) || !std::isfinite(1.4426950408889634f / p->temperature))
+    return fail(KVQ_ERR_ARG, "temperature %g must be positive and finite, its reciprocal too", (double)p->temperature);
+  if (!grad && need_grad) return fail(KVQ_ERR_ARG, "grad must be a device pointer");
+  if (grad && grad_row_stride < p->vocab)
+    return fail(KVQ_ERR_ARG, "grad_row_stride %lld smaller than vocab %d", (long long)grad_row_stride, p->vocab);
+  if (reinterpret_cast<uintptr_t>(grad) % (p->type == DGAP_F32 ? 4 : 2) != 0)
+    return fail(KVQ_ERR_ARG, "grad must be aligned to its type");
+  if (grad == p->logits && grad && grad_row_stride != p->row_stride)
+    return fail(KVQ_ERR_ARG, "a gradient in the logits' place needs their row stride");
+  const double c = 1.4426950408889634 / (double)p->temperature;
+  a.logits = p->logits;
+  a.teacher = p->teacher;
+  a.index = p->index;
+  a.grad_loss = grad_loss;
+  a.grad = grad;
+  a.row_stride = p->row_stride;
+  a.grad_stride = grad_row_stride;
+  a.rows = p->rows; a.vocab = p->vocab; a.k = p->k;
+  a.nchunk = (p->vocab + kvq::kDistillChunk - 1) / kvq::kDistillChunk;
+  a.temperature = p->temperature;
+  a.c = (float)c;
+  a.c_low = (float)(c - (double)a.c);
+  return KVQ_OK;
 }
 
 }  // namespace
@@ -1192,6 +1253,75 @@ kvq_status dgap_restore(const dgap_params* p, float* logits, int32_t batch, void
   a.ws_cand = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(ws) + stats);
   const int e = kvq::launch_dgap(a, batch, stream);
   if (e) return hip_fail(e, "dgap launch");
+  return ok();
+}
+
+// ------------------------------------------------------------------ sampling
+
+size_t dgap_sample_workspace_bytes(int32_t batch, int32_t vocab) {
+  if (batch < 1 || vocab < 1 || vocab > (1 << 24)) return 0;
+  return (size_t)batch * sample_row_bytes(vocab);
+}
+
+kvq_status dgap_sample(const dgap_sampling* p, int32_t* tokens, float* logprobs, void* ws, size_t ws_bytes,
+                       void* stream) {
+  if (!p) return fail(KVQ_ERR_ARG, "parameters are NULL");
+  kvq_status st = check_rows(p->logits, p->type, p->row_stride, p->batch, p->vocab, "batch");
+  if (st != KVQ_OK) return st;
+  if (!p->uniform || !tokens) return fail(KVQ_ERR_ARG, "uniform and tokens must be device pointers");
+  st = check_scratch(ws, ws_bytes, dgap_sample_workspace_bytes(p->batch, p->vocab));
+  if (st != KVQ_OK) return st;
+  kvq::SampleArgs a{};
+  a.logits = p->logits;
+  a.temperature = p->temperature; a.top_k = p->top_k; a.top_p = p->top_p; a.min_p = p->min_p; a.uniform = p->uniform;
+  a.tokens = tokens;
+  a.logprobs = logprobs;
+  a.ws = static_cast<uint8_t*>(ws);
+  a.row_stride = p->row_stride;
+  a.row_bytes = sample_row_bytes(p->vocab);
+  a.batch = p->batch; a.vocab = p->vocab;
+  a.nchunk = (p->vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk;
+  // the sum of all weights stays below 2^63; 45: a bin 51 octaves below the
+  // largest weight holds none
+  a.unit = std::min(45, 62 - log2_exact(p->vocab));
+  const int e = kvq::launch_sample(a, p->type, stream);
+  if (e) return hip_fail(e, "sampling launch");
+  return ok();
+}
+
+// ------------------------------------------------------------------ teacher loss
+
+size_t dgap_distill_workspace_bytes(int32_t rows, int32_t vocab) {
+  if (rows < 1 || vocab < 1 || vocab > (1 << 24)) return 0;
+  return (size_t)rows * (8 + 8 * (size_t)((vocab + kvq::kDistillChunk - 1) / kvq::kDistillChunk));
+}
+
+kvq_status dgap_distill(const dgap_distillation* p, float* loss, float* lse, void* grad, int64_t grad_row_stride,
+                        const float* grad_loss, void* ws, size_t ws_bytes, void* stream) {
+  kvq::DistillArgs a{};
+  kvq_status st = distill_args(a, p, grad, grad_row_stride, grad_loss, false);
+  if (st != KVQ_OK) return st;
+  if (!loss) return fail(KVQ_ERR_ARG, "loss must be a device pointer");
+  st = check_scratch(ws, ws_bytes, dgap_distill_workspace_bytes(p->rows, p->vocab));
+  if (st != KVQ_OK) return st;
+  a.loss = loss;
+  a.lse = lse;
+  a.row_sum = static_cast<float*>(ws);
+  a.ws = a.row_sum + 2 * (size_t)p->rows;
+  const int e = kvq::launch_distill(a, p->type, stream);
+  if (e) return hip_fail(e, "teacher loss launch");
+  return ok();
+}
+
+kvq_status dgap_distill_backward(const dgap_distillation* p, const float* lse, const float* grad_loss, void* grad,
+                                 int64_t grad_row_stride, void* stream) {
+  kvq::DistillArgs a{};
+  const kvq_status st = distill_args(a, p, grad, grad_row_stride, grad_loss, true);
+  if (st != KVQ_OK) return st;
+  if (!lse) return fail(KVQ_ERR_ARG, "lse must be a device pointer");
+  a.lse = const_cast<float*>(lse);
+  const int e = kvq::launch_distill(a, p->type, stream);
+  if (e) return hip_fail(e, "teacher loss gradient launch");
   return ok();
 }
 

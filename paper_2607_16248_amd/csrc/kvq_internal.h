@@ -254,6 +254,48 @@ struct DgapArgs {
   float tau, det_b2, corr_b2;
 };
 
+// ---------------------------------------------------------------- sampling
+
+constexpr int kSampleChunk = 8192;   // logits per workgroup
+constexpr int kSampleBins = 2048;    // bins of a row's weights
+constexpr int kSampleList = 2048;    // elements that a row's searches may end among
+
+struct SampleArgs {
+  const void* logits;
+  const float* temperature;  // per row; null: 1
+  const int32_t* top_k;      // null: off, like the next two
+  const float* top_p;
+  const float* min_p;
+  const float* uniform;
+  int32_t* tokens;
+  float* logprobs;           // or null
+  uint8_t* ws;               // per row: bin masses, list, chunk keys (64 bits each), bin counts, list length (32)
+  int64_t row_stride;        // elements
+  uint64_t row_bytes;        // of ws
+  int32_t batch, vocab, nchunk;
+  int32_t unit;              // masses are in units of 2^-unit of the largest weight
+};
+
+// ---------------------------------------------------------------- teacher loss
+
+constexpr int kDistillChunk = 8192;  // logits per workgroup
+constexpr int kDistillMaxK = 256;    // teacher entries per row
+
+struct DistillArgs {
+  const void* logits;
+  const float* teacher;     // [rows][k]
+  const int32_t* index;     // [rows][k]
+  const float* grad_loss;   // per row; null: 1
+  float* loss;              // per row; null: the gradient alone, from lse
+  float* lse;               // per row; with loss: null or written
+  void* grad;               // logits' type; null: the loss alone
+  float* ws;                // per (row, chunk): largest logit m, sum of 2^((z - m) c)
+  float* row_sum;           // per row: the same m, and the sum's log2
+  int64_t row_stride, grad_stride;
+  int32_t rows, vocab, nchunk, k;
+  float temperature, c, c_low;  // c + c_low = log2(e) / T
+};
+
 // ---------------------------------------------------------------- dequant
 
 struct DequantArgs {
@@ -330,6 +372,8 @@ int launch_window_class(const DecodeArgs& a, int bv, void* stream);
 int launch_export(const ExportArgs& a, void* stream);
 int launch_merge(const MergeArgs& a, void* stream);
 int launch_dgap(const struct DgapArgs& a, int batch, void* stream);
+int launch_sample(const SampleArgs& a, int type, void* stream);
+int launch_distill(const DistillArgs& a, int type, void* stream);
 int launch_dequant(const DequantArgs& a, void* stream);
 int launch_fill_zero(void* dst, size_t words, void* stream);
 // Streaming-read probe: kvq_read_probe's kernel and its grid size.

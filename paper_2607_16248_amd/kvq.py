@@ -27,7 +27,9 @@ EXPORTED = ["kvq_cache_bytes", "kvq_cache_init", "kvq_cache_destroy", "kvq_cache
             "kvq_dequant", "kvq_export_bytes", "kvq_export", "kvq_check",
             "kvq_set_split_tokens", "kvq_last_error", "kvq_version",
             "kvq_read_probe", "kvq_read_probe_sink_bytes",
-            "dgap_workspace_bytes", "dgap_info_floats", "dgap_restore"]
+            "dgap_workspace_bytes", "dgap_info_floats", "dgap_restore",
+            "dgap_sample_workspace_bytes", "dgap_sample",
+            "dgap_distill_workspace_bytes", "dgap_distill", "dgap_distill_backward"]
 
 
 class KvqError(RuntimeError):
@@ -53,6 +55,22 @@ class DgapParams(ctypes.Structure):
                 ("corr_b2", ctypes.c_float), ("pad", ctypes.c_int32),
                 ("det_w1", ctypes.c_void_p), ("det_b1", ctypes.c_void_p), ("det_w2", ctypes.c_void_p),
                 ("corr_w1", ctypes.c_void_p), ("corr_b1", ctypes.c_void_p), ("corr_w2", ctypes.c_void_p)]
+
+
+class DgapSampling(ctypes.Structure):
+    """dgap_sampling of include/dgap.h (device pointers)."""
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("vocab", ctypes.c_int32), ("pad", ctypes.c_int32),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p), ("uniform", ctypes.c_void_p)]
+
+
+class DgapDistillation(ctypes.Structure):
+    """dgap_distillation of include/dgap.h (device pointers)."""
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("teacher", ctypes.c_void_p), ("index", ctypes.c_void_p), ("temperature", ctypes.c_float),
+                ("pad", ctypes.c_int32)]
 
 
 _lib = None
@@ -100,6 +118,11 @@ def lib():
         "dgap_workspace_bytes": ([I32, I32, I32], S),
         "dgap_info_floats": ([I32], S),
         "dgap_restore": ([ctypes.POINTER(DgapParams), P, I32, P, S, P, P], ctypes.c_int),
+        "dgap_sample_workspace_bytes": ([I32, I32], S),
+        "dgap_distill_workspace_bytes": ([I32, I32], S),
+        "dgap_distill": ([ctypes.POINTER(DgapDistillation), P, P, P, I64, P, P, S, P], ctypes.c_int),
+        "dgap_distill_backward": ([ctypes.POINTER(DgapDistillation), P, P, P, I64, P], ctypes.c_int),
+        "dgap_sample": ([ctypes.POINTER(DgapSampling), P, P, P, S, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -438,3 +461,92 @@ def dgap_restore(params: DgapParams, logits, batch: int, ws, ws_bytes: Optional[
         ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(lib().dgap_restore(ctypes.byref(params), _ptr(logits), int(batch), _ptr(ws), int(ws_bytes),
                               _ptr(info), _stream(stream)))
+
+
+# ---------------------------------- rows of logits: tokens, teacher loss
+
+def _rows(logits):
+    """(dgap_type, row stride) of a [rows][vocab] tensor whose rows are contiguous."""
+    name = str(logits.dtype)
+    if name not in _DGAP_TYPES:
+        raise TypeError(f"logits of {name}: float32, float16 or bfloat16 are supported")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows][vocab] with contiguous rows")
+    return _DGAP_TYPES[name], int(logits.stride(0)) if logits.shape[0] > 1 else int(logits.shape[1])
+
+
+_DGAP_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+
+
+def _per_row(name, x, rows, dtype):
+    """A device array of one value per row, or None; its address."""
+    if x is None:
+        return None
+    if str(x.dtype) != dtype or x.numel() != rows or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {rows} values")
+    return x.data_ptr()
+
+
+def dgap_sample_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(lib().dgap_sample_workspace_bytes(int(batch), int(vocab)))
+
+
+def dgap_sample(logits, uniform, tokens, ws, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=None,
+                ws_bytes: Optional[int] = None, stream=None) -> None:
+    """The next token of every row of ``logits`` ([rows][vocab], fp32, fp16 or bf16) from one number in [0, 1) per row.
+
+    ``tokens`` int32 [rows] and ``logprobs`` fp32 [rows] receive the result; the settings are tensors of one value per
+    row (top_k int32, the others fp32) or None.
+    """
+    kind, stride = _rows(logits)
+    n, f32, i32 = int(logits.shape[0]), "torch.float32", "torch.int32"
+    p = DgapSampling(_ptr(logits), stride, kind, n, int(logits.shape[1]), 0,
+                     _per_row("temperature", temperature, n, f32), _per_row("top_k", top_k, n, i32),
+                     _per_row("top_p", top_p, n, f32), _per_row("min_p", min_p, n, f32),
+                     _per_row("uniform", uniform, n, f32))
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().dgap_sample(ctypes.byref(p), _per_row("tokens", tokens, n, i32), _per_row("logprobs", logprobs, n, f32),
+                             _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def dgap_distill_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(lib().dgap_distill_workspace_bytes(int(rows), int(vocab)))
+
+
+def _distillation(logits, teacher, index, temperature, grad):
+    kind, stride = _rows(logits)
+    n, v, k = int(logits.shape[0]), int(logits.shape[1]), int(teacher.shape[-1])
+    p = DgapDistillation(_ptr(logits), stride, kind, n, v, k, _per_row("teacher", teacher, n * k, "torch.float32"),
+                         _per_row("index", index, n * k, "torch.int32"), float(temperature), 0)
+    grad_stride = 0
+    if grad is not None:
+        if grad.dtype != logits.dtype or grad.shape != logits.shape:
+            raise ValueError("grad must have the logits' type and shape")
+        grad_stride = _rows(grad)[1]
+    return p, grad_stride
+
+
+def dgap_distill(logits, teacher, index, temperature: float, loss, ws, lse=None, grad=None, grad_loss=None,
+                 ws_bytes: Optional[int] = None, stream=None) -> None:
+    """The loss of every row of ``logits`` ([rows][vocab]) against a teacher's top logits, and its gradient.
+
+    ``teacher`` fp32 and ``index`` int32 [rows][k]; ``loss``, ``lse`` and ``grad_loss`` fp32 [rows]; ``grad`` like
+    ``logits`` (or ``logits`` itself), None for the loss alone.
+    """
+    p, grad_stride = _distillation(logits, teacher, index, temperature, grad)
+    n, f32 = p.rows, "torch.float32"
+    if ws_bytes is None:
+        ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().dgap_distill(ctypes.byref(p), _per_row("loss", loss, n, f32), _per_row("lse", lse, n, f32), _ptr(grad),
+                              grad_stride, _per_row("grad_loss", grad_loss, n, f32), _ptr(ws), int(ws_bytes),
+                              _stream(stream)))
+
+
+def dgap_distill_backward(logits, teacher, index, temperature: float, lse, grad, grad_loss=None, stream=None) -> None:
+    """The gradient alone, from the ``lse`` that dgap_distill wrote for these logits."""
+    p, grad_stride = _distillation(logits, teacher, index, temperature, grad)
+    n, f32 = p.rows, "torch.float32"
+    _check(lib().dgap_distill_backward(ctypes.byref(p), _per_row("lse", lse, n, f32),
+                                       _per_row("grad_loss", grad_loss, n, f32), _ptr(grad), grad_stride,
+                                       _stream(stream)))

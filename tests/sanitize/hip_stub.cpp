@@ -249,6 +249,37 @@ int launch_merge(const MergeArgs& a, void*) {
   return ++g_launches, 0;
 }
 int launch_dgap(const DgapArgs&, int, void*) { return ++g_launches, 0; }
+// What the row kernels read and write.
+int launch_sample(const SampleArgs& a, int type, void*) {
+  const size_t size = type == 0 ? 4 : 2;
+  if (a.unit < 24 || ((double)a.vocab * (double)(1ull << a.unit)) > 9.2e18 || (a.unit + 1) * 40 >= kSampleBins) std::abort();
+  for (int r = 0; r < a.batch; ++r) {
+    rd(static_cast<const uint8_t*>(a.logits) + (size_t)r * a.row_stride * size, a.vocab * size);
+    wr(a.ws + (size_t)r * a.row_bytes, 8 * (size_t)(kSampleBins + kSampleList + a.nchunk) + 4 * (kSampleBins + 1));
+  }
+  for (const void* p : {(const void*)a.temperature, (const void*)a.top_k, (const void*)a.top_p, (const void*)a.min_p, (const void*)a.uniform})
+    if (p) rd(p, 4 * (size_t)a.batch);
+  wr(a.tokens, 4 * (size_t)a.batch);
+  if (a.logprobs) wr(a.logprobs, 4 * (size_t)a.batch);
+  return ++g_launches, 0;
+}
+int launch_distill(const DistillArgs& a, int type, void*) {
+  const size_t size = type == 0 ? 4 : 2;
+  rd(a.teacher, 4 * (size_t)a.rows * a.k);
+  rd(a.index, 4 * (size_t)a.rows * a.k);
+  if (a.grad_loss) rd(a.grad_loss, 4 * (size_t)a.rows);
+  for (int r = 0; r < a.rows; ++r) rd(static_cast<const uint8_t*>(a.logits) + (size_t)r * a.row_stride * size, a.vocab * size);
+  if (a.loss) {
+    wr(a.row_sum, 8 * (size_t)a.rows);
+    wr(a.ws, 8 * (size_t)a.rows * a.nchunk);
+    wr(a.loss, 4 * (size_t)a.rows);
+    if (a.lse) wr(a.lse, 4 * (size_t)a.rows);
+  } else {
+    rd(a.lse, 4 * (size_t)a.rows);
+  }
+  for (int r = 0; a.grad && r < a.rows; ++r) wr(static_cast<uint8_t*>(a.grad) + (size_t)r * a.grad_stride * size, a.vocab * size);
+  return ++g_launches, 0;
+}
 int launch_dequant(const DequantArgs& a, void*) {
   check_regions(a, nullptr);
   for (int h = 0; h < a.hkv; ++h) {

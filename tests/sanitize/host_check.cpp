@@ -251,6 +251,62 @@ int main() {
     EXPECT(dgap_restore(&p, logits.data(), 2, ws.p, wsb - 1, nullptr, nullptr) != KVQ_OK);
     EXPECT(dgap_restore(nullptr, logits.data(), 2, ws.p, wsb, nullptr, nullptr) == KVQ_ERR_ARG);
   }
+  // token sampling and the teacher loss: shapes, types, refusals, exact sizes
+  for (int type : {DGAP_F32, DGAP_F16, DGAP_BF16})
+    for (int vocab : {1, 37, 8192, 8193, 100000}) {
+      const int rows = 3, k = 20;
+      const size_t size = type == DGAP_F32 ? 4 : 2;
+      const int64_t stride = vocab + 5;
+      Buf z(((rows - 1) * stride + vocab) * size), f(rows * 4), tok(rows * 4), lp(rows * 4);
+      dgap_sampling p{};
+      p.logits = z.p; p.row_stride = stride; p.type = type; p.batch = rows; p.vocab = vocab;
+      p.uniform = f.as<float>();
+      Buf ws(dgap_sample_workspace_bytes(rows, vocab));
+      EXPECT(dgap_sample(&p, tok.as<int32_t>(), nullptr, ws.p, ws.n, nullptr) == KVQ_OK);
+      p.temperature = p.top_p = p.min_p = f.as<float>();
+      p.top_k = tok.as<int32_t>();
+      EXPECT(dgap_sample(&p, tok.as<int32_t>(), lp.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
+      EXPECT(dgap_sample(&p, tok.as<int32_t>(), lp.as<float>(), ws.p, ws.n - 1, nullptr) == KVQ_ERR_CAPACITY);
+      EXPECT(dgap_sample(&p, nullptr, lp.as<float>(), ws.p, ws.n, nullptr) == KVQ_ERR_ARG);
+      EXPECT(dgap_sample(nullptr, tok.as<int32_t>(), nullptr, ws.p, ws.n, nullptr) == KVQ_ERR_ARG);
+      for (auto bad : {+[](dgap_sampling& x) { x.type = 3; }, +[](dgap_sampling& x) { x.batch = 0; },
+                       +[](dgap_sampling& x) { x.vocab = 0; }, +[](dgap_sampling& x) { x.row_stride = x.vocab - 1; },
+                       +[](dgap_sampling& x) { x.logits = nullptr; }, +[](dgap_sampling& x) { x.uniform = nullptr; },
+                       +[](dgap_sampling& x) { x.logits = static_cast<const char*>(x.logits) + 1; }}) {
+        dgap_sampling b = p;
+        bad(b);
+        EXPECT(dgap_sample(&b, tok.as<int32_t>(), lp.as<float>(), ws.p, ws.n, nullptr) == KVQ_ERR_ARG);
+      }
+      dgap_sampling wide = p;
+      wide.vocab = (1 << 24) + 1;
+      wide.row_stride = wide.vocab;
+      EXPECT(dgap_sample(&wide, tok.as<int32_t>(), nullptr, ws.p, ws.n, nullptr) == KVQ_ERR_UNSUPPORTED);
+      Buf t(rows * k * 4), idx(rows * k * 4), loss(rows * 4), lse(rows * 4), g(((rows - 1) * (stride + 2) + vocab) * size);
+      dgap_distillation d{};
+      d.logits = z.p; d.row_stride = stride; d.type = type; d.rows = rows; d.vocab = vocab; d.k = k;
+      d.teacher = t.as<float>(); d.index = idx.as<int32_t>(); d.temperature = 2.f;
+      Buf dws(dgap_distill_workspace_bytes(rows, vocab));
+      EXPECT(dgap_distill(&d, loss.as<float>(), nullptr, nullptr, 0, nullptr, dws.p, dws.n, nullptr) == KVQ_OK);
+      EXPECT(dgap_distill(&d, loss.as<float>(), lse.as<float>(), g.p, stride + 2, f.as<float>(), dws.p, dws.n, nullptr) == KVQ_OK);
+      EXPECT(dgap_distill(&d, loss.as<float>(), nullptr, z.p, stride, nullptr, dws.p, dws.n, nullptr) == KVQ_OK);
+      EXPECT(dgap_distill_backward(&d, lse.as<float>(), nullptr, g.p, stride + 2, nullptr) == KVQ_OK);
+      EXPECT(dgap_distill(&d, loss.as<float>(), nullptr, z.p, stride + 2, nullptr, dws.p, dws.n, nullptr) == KVQ_ERR_ARG);
+      EXPECT(dgap_distill(&d, loss.as<float>(), nullptr, g.p, vocab - 1, nullptr, dws.p, dws.n, nullptr) == KVQ_ERR_ARG);
+      EXPECT(dgap_distill(&d, loss.as<float>(), nullptr, nullptr, 0, nullptr, dws.p, dws.n - 1, nullptr) == KVQ_ERR_CAPACITY);
+      EXPECT(dgap_distill(&d, nullptr, nullptr, nullptr, 0, nullptr, dws.p, dws.n, nullptr) == KVQ_ERR_ARG);
+      EXPECT(dgap_distill_backward(&d, nullptr, nullptr, g.p, stride + 2, nullptr) == KVQ_ERR_ARG);
+      EXPECT(dgap_distill_backward(&d, lse.as<float>(), nullptr, nullptr, stride, nullptr) == KVQ_ERR_ARG);
+      for (auto bad : {+[](dgap_distillation& x) { x.temperature = 0.f; }, +[](dgap_distillation& x) { x.temperature = 1e-45f; },
+                       +[](dgap_distillation& x) { x.k = 0; }, +[](dgap_distillation& x) { x.k = DGAP_MAX_TEACHER + 1; },
+                       +[](dgap_distillation& x) { x.teacher = nullptr; }, +[](dgap_distillation& x) { x.index = nullptr; },
+                       +[](dgap_distillation& x) { x.rows = 0; }}) {
+        dgap_distillation b = d;
+        bad(b);
+        EXPECT(dgap_distill(&b, loss.as<float>(), nullptr, nullptr, 0, nullptr, dws.p, dws.n, nullptr) == KVQ_ERR_ARG);
+      }
+    }
+  EXPECT(dgap_sample_workspace_bytes(0, 5) == 0 && dgap_sample_workspace_bytes(1, (1 << 24) + 1) == 0);
+  EXPECT(dgap_distill_workspace_bytes(0, 5) == 0 && dgap_distill_workspace_bytes(1, 0) == 0);
   if (g_fail) {
     std::fprintf(stderr, "%d host checks failed\n", g_fail);
     return 1;
