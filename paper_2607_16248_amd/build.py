@@ -35,6 +35,7 @@ SOURCES = [
     ("merge.hip", ["-fno-honor-nans"], None),
     ("chunk_mfma.hip", ["-fno-honor-nans"], None),
     ("prefill_mfma.hip", ["-fno-honor-nans"], None),
+    ("prefill_mfma.hip", ["-fno-honor-nans", "-DKVQ_WINDOW"], "window_rows.o"),
     ("dequant.hip", [], None),
     ("dgap.hip", [], None),
     ("sample.hip", [], None),

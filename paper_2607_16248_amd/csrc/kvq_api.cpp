@@ -879,32 +879,65 @@ kvq_status run_merge(const kvq_cache* c, const SplitPlan& p, const void* ws, flo
 
 // ------------------------------------------------------------ windowed attention
 
-// Rows of a windowed launch: one query's heads, or 16 rows of whole queries
-// (the last group may repeat the last query in its spare rows).
-Rows window_rows(const kvq_cache* c, int nqry) {
+// (query, head) rows per kv head.  One sequence of four heads per kv head, 16-row
+// groups against many rows: windows of 512 tokens 128 rows 19 and 23 us, 256 rows
+// 19 and 20, 512 rows 27 and 22; windows of 4096 128 rows 29 and 32, 256 rows 40
+// and 28, 4096 rows 626 and 123 (K2V2; the other classes alike).
+constexpr int kWindowManyRows = 256;
+constexpr double kWindowBlockUs2 = 2.0;  // a block of 4- or 8-bit operands with the values' low halves
+
+// Whether a class's windowed queries go to the many-row kernel, which reads a
+// block once for 256 rows.
+bool window_many(const kvq_cache* c, int seq0, int nqry) {
+  return c->matrix[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyRows;
+}
+
+// Rows of a class's windowed launch: one query's heads, 16 rows of whole
+// queries, or row groups of 32 of the many-row kernel (the last group may
+// repeat the last query in its spare rows).
+Rows window_rows(const kvq_cache* c, int seq0, int nqry) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
   Rows r;
   r.nqry = nqry;
-  r.qpr = nqry == 1 ? 1 : 16 / gqh;
+  r.many = window_many(c, seq0, nqry);
+  r.rows = r.many ? 32 : 16;
+  r.qpr = nqry == 1 ? 1 : r.rows / gqh;
   r.nrg = (nqry + r.qpr - 1) / r.qpr;
-  r.rows = 16;
   return r;
 }
 
-// Most packed key groups that any row group of sequence i reads.
+// Most packed key groups (many rows: blocks, the tail's too) that any workgroup
+// of sequence i reads.
 int32_t window_reach(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks) {
   const int32_t seen0 = c->L[i] - r.nqry + 1, gsh = log2_exact(c->d.key_group);
+  const int32_t step = r.qpr * (r.many ? kvq::kPrefillWaves : 1);  // queries per workgroup
   int32_t most = 0;
-  for (int rg = 0; rg < r.nrg; ++rg) {
-    const int first = rg * r.qpr, last = std::min(first + r.qpr, r.nqry) - 1;
-    most = std::max(most, kvq::window_groups(seen0 + first, seen0 + last, c->Lq[i], gsh, window, sinks).count);
+  for (int first = 0; first < r.nqry; first += step) {
+    const int32_t seen_first = seen0 + first, seen_last = seen0 + std::min(first + step, r.nqry) - 1;
+    int32_t n = kvq::window_groups(seen_first, seen_last, c->Lq[i], gsh, window, sinks).count;
+    if (r.many) {
+      const int32_t tail0 = sinks <= c->Lq[i] ? std::max(c->Lq[i], std::max(seen_first - window, 0)) / 32 : c->Lq[i] / 32;
+      n = (n << (gsh - 5)) + std::max(0, (int32_t)(((int64_t)seen_last + 31) / 32) - tail0);
+    }
+    most = std::max(most, n);
   }
   return most;
 }
 
-// The split plan of a windowed call: every class's splits take the same number
-// of key groups, as many as leave two workgroups per compute unit (what the
-// kernel's registers allow at once) and no fewer than one group per wave.
+// Most splits of a sequence in a windowed call, at any lengths.
+int64_t window_splits(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
+  const int64_t gk = c->d.key_group, qpr = 16 / (c->d.num_q_heads / c->d.num_kv_heads);
+  // a range of n tokens touches at most (n + gk - 2) / gk + 1 key groups
+  const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + (nqry > 1 ? qpr : 1) - 1 + gk - 2) / gk + 1);
+  const int64_t per = c->split_tokens > 0 ? c->split_tokens / gk : kMinGroupsPerSplit;
+  return std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
+}
+
+// The split plan of a windowed call.  16-row groups: every class's splits take
+// the same number of key groups, as many as leave two workgroups per compute
+// unit (what the kernel's registers allow at once) and no fewer than one group
+// per wave.  Many rows: the splits with the smallest estimated time, as for
+// chunk queries.
 SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   SplitPlan p;
   p.nqry = nqry;
@@ -913,18 +946,45 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   p.nq.assign(B, 0);
   p.ns.assign(B, 0);
   p.base.assign(B, 0);
-  const Rows r = window_rows(c, nqry);
+  p.direct.assign(B, 0);
+  const int64_t bound = window_splits(c, nqry, window, sinks);
   std::map<std::pair<int, int>, std::vector<int>> classes;
   for (int i = 0; i < B; ++i)
     if (c->L[i] > 0) classes[{c->bk[i], c->bv[i]}].push_back(i);
   for (auto& cl : classes) {
+    const Rows r = window_rows(c, cl.second[0], nqry);
+    const int64_t units = (int64_t)c->d.num_kv_heads * (r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg);
     int64_t total = 0, tails = 0, longest = 0;
-    const int64_t units = (int64_t)c->d.num_kv_heads * r.nrg;
     for (int i : cl.second) {
       p.nq[i] = window_reach(c, i, r, window, sinks);
       total += p.nq[i] * units;
       longest = std::max<int64_t>(longest, p.nq[i]);
       if (c->L[i] > c->Lq[i]) tails += units;
+    }
+    if (r.many) {
+      const double block_us = cl.first.first + cl.first.second <= 4 ? kBlockUs : kWindowBlockUs2;
+      const int64_t cus = target_workgroups(1);
+      int64_t bps = longest;
+      double best = 0.0;
+      for (int64_t ns = 1; ns <= std::min<int64_t>(bound, 64); ++ns) {
+        const int64_t n = (longest + ns - 1) / ns;
+        int64_t wgs = 0, records = 0;
+        for (int i : cl.second) {
+          const int64_t k = (p.nq[i] + n - 1) / n;
+          wgs += units * k;
+          records += k > 1 ? k : 0;
+        }
+        const double t = (double)((wgs + cus - 1) / cus) * (n * block_us + kSplitUs) +
+                         records * (double)nqry * c->d.num_q_heads * kRecordUs;
+        if (ns == 1 || t < best) best = t, bps = n;
+      }
+      if (c->split_tokens > 0) bps = std::max<int64_t>(c->split_tokens / 32, (longest + bound - 1) / bound);
+      for (int i : cl.second) {
+        p.ns[i] = (int32_t)((p.nq[i] + bps - 1) / bps);
+        p.nq[i] = (int32_t)bps;
+        p.direct[i] = p.ns[i] <= 1;
+      }
+      continue;
     }
     const int64_t round = target_workgroups(2), target = std::max(round - tails, round / 2);
     int64_t groups = c->split_tokens / gk;
@@ -933,19 +993,19 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
     for (int i : cl.second) {
       p.st[i] = (int32_t)(groups * gk);
       p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
+      p.ns[i] = p.nq[i] + (c->L[i] > c->Lq[i] ? 1 : 0);
     }
   }
   for (int i = 0; i < B; ++i) {
-    p.ns[i] = p.nq[i] + (c->L[i] > c->Lq[i] ? 1 : 0);
     p.base[i] = (int32_t)p.records;
-    p.records += p.ns[i];
+    p.records += p.direct[i] ? 0 : p.ns[i];
   }
   p.required = p.records;
   return p;
 }
 
-kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int32_t window, int32_t sinks, void* ws,
-                      size_t ws_bytes, void* stream) {
+kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int32_t window, int32_t sinks, float* out,
+                      void* ws, size_t ws_bytes, void* stream) {
   const kvq_status st = check_workspace(c, p.required, p.nqry, ws, ws_bytes);
   if (st != KVQ_OK) return st;
   std::vector<int> seqs;
@@ -953,13 +1013,15 @@ kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int
     if (c->L[i] > 0) seqs.push_back(i);
   for (auto& cls : bit_classes(c, seqs)) {
     kvq::DecodeArgs a{};
-    const Rows r = window_rows(c, p.nqry);
+    const Rows r = window_rows(c, cls.second[0], p.nqry);
     fill_args(a, c, cls.second[0], r, q, ws);
     a.split_tokens = p.st[cls.second[0]];
     a.window = window;
     a.sinks = sinks;
+    if (r.many) a.out = out;
     fill_seqs(a, c, cls.second, p, r);
-    const int e = kvq::launch_window(a, cls.first.first, cls.first.second, stream);
+    const int e = r.many ? kvq::launch_window_rows(a, cls.first.first, cls.first.second, stream)
+                         : kvq::launch_window(a, cls.first.first, cls.first.second, stream);
     if (e) return hip_fail(e, "windowed attention launch");
   }
   return KVQ_OK;
@@ -1087,11 +1149,7 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
 
 size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
-  const int64_t gk = c->d.key_group, qpr = window_rows(c, n_q).qpr;
-  // a range of n tokens touches at most (n + gk - 2) / gk + 1 key groups
-  const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + qpr - 1 + gk - 2) / gk + 1);
-  const int64_t per = c->split_tokens > 0 ? c->split_tokens / gk : kMinGroupsPerSplit;
-  const int64_t splits = std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
+  const int64_t splits = window_splits(c, n_q, window, sinks);
   return (size_t)c->d.batch * c->d.num_q_heads * n_q * (size_t)splits * kvq::kRecFloats * sizeof(float);
 }
 
@@ -1111,7 +1169,7 @@ kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, 
   window = std::min(window, longest);
   sinks = std::min(sinks, longest);
   const SplitPlan p = plan_window(c, n_q, window, sinks);
-  kvq_status st = run_window(c, p, q, window, sinks, ws, ws_bytes, stream);
+  kvq_status st = run_window(c, p, q, window, sinks, out, ws, ws_bytes, stream);
   if (st != KVQ_OK) return st;
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;

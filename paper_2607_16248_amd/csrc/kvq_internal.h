@@ -367,6 +367,9 @@ int launch_exact_class(const DecodeArgs& a, int bv, void* stream);
 // Windowed attention (a.window > 0) of every class, 16 rows per workgroup, by
 // key bits (decode_exact.hip).
 int launch_window(const DecodeArgs& a, int bk, int bv, void* stream);
+// The same of many rows: kPrefillWaves row groups of 32 rows per workgroup; per
+// sequence, nq is the blocks per split of its workgroups' lists (prefill_mfma.hip).
+int launch_window_rows(const DecodeArgs& a, int bk, int bv, void* stream);
 template <int BK>
 int launch_window_class(const DecodeArgs& a, int bv, void* stream);
 int launch_export(const ExportArgs& a, void* stream);

@@ -64,6 +64,7 @@ constexpr int kTile = 16;           // rows of one tile (the N dimension); a wav
 constexpr int kSlots = 4;            // operand buffers (blocks in flight between two barriers)
 constexpr int kZGroups = 16;        // key groups per zero-point table
 constexpr int kSubRow = 12;         // first row z' of the operand [z; s; 1; z']
+constexpr float kMidLift = 2048.f;  // of the low halves of z + c0 s (a half's last step of 65504, 16, stays finite)
 constexpr int kZRow = 132;          // dwords per staged key group: s[128], z[128] (+ 4: rows start in distinct banks)
 constexpr float kTop = 14.f;        // weights stay below 2^14 ...
 constexpr float kHeadroom = 6.f;    // ... a new reference puts the largest at 2^8
@@ -87,10 +88,14 @@ struct PrefillSmem {
 // a dword of the rows [z; s] of the values.
 struct Staged {
   uint32_t x[2], zz;
+  [[maybe_unused]] uint32_t zs;  // windowed attention: zz a dword of zeros, zs the same one of scales
   u4_t s;
 };
 
-template <int BK, int BV, bool PAGED>
+// WINDOW: windowed attention.  The blocks of a split are those of the key groups
+// that the workgroup's windows and the sinks touch, as one list, and then the
+// tail's; b counts through the list, block_at gives a block's place.
+template <int BK, int BV, bool PAGED, bool WINDOW>
 __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefill_mfma_kernel(DecodeArgs a) {
   constexpr int PK = Code<BK>::parts, PV = Code<BV>::parts, kZOp = 8 * PK + 8 * PV;
   __shared__ __attribute__((aligned(16))) PrefillSmem<BK, BV> sm;
@@ -111,8 +116,22 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   const bool active = rg < a.nrg;
   const int seen0 = S.L - a.nqry + 1;  // tokens query 0 sees
   const int wg_limit = seen0 + min(rg_last * a.qpr + a.qpr - 1, a.nqry - 1);
-  const int nb_packed = S.Lq / 32;
-  const int b0 = sp * S.nq, b1 = min(min(b0 + S.nq, (S.L + 31) / 32), (wg_limit + 31) / 32);
+  const int bsh = gsh - 5;  // 2^bsh blocks per key group
+  int nb_packed = S.Lq / 32, tail0 = nb_packed;  // packed blocks, the first tail block's place
+  [[maybe_unused]] WindowGroups wgroups{};
+  if constexpr (WINDOW) {
+    const int wg_first = seen0 + min(rw * kNW * a.qpr, a.nqry - 1);
+    wgroups = window_groups(wg_first, wg_limit, S.Lq, gsh, a.window, a.sinks);
+    nb_packed = wgroups.count << bsh;
+    if (a.sinks <= S.Lq) tail0 = max(tail0, max(wg_first - a.window, 0) / 32);
+  }
+  const int b0 = sp * S.nq, b1 = WINDOW ? min(b0 + S.nq, nb_packed + max(0, (wg_limit + 31) / 32 - tail0))
+                                       : min(min(b0 + S.nq, (S.L + 31) / 32), (wg_limit + 31) / 32);
+  auto block_at = [&](int b) {
+    if constexpr (!WINDOW) return b;
+    if (b >= nb_packed) return b - nb_packed + tail0;
+    return b + ((b >> bsh) < wgroups.sink ? 0 : (wgroups.first - wgroups.sink) << bsh);
+  };
   const int wave_first = active ? seen0 + min(rg * a.qpr, a.nqry - 1) : 0;
   const int wave_limit = active ? seen0 + min(rg * a.qpr + a.qpr - 1, a.nqry - 1) : 0;
 
@@ -165,7 +184,7 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   const uint32_t lo_zz = (zrow < 4 ? fresh_vm : 0) + (zrow & 3) * 64 + zpos * 4;
   const __amdgpu_buffer_rsrc_t ring_rs = head_rsrc(ring, PAGED ? 0 : a.head_stride);
   auto seg_of = [&](int b, int& tin) -> __amdgpu_buffer_rsrc_t {
-    tin = 32 * b;
+    tin = 32 * block_at(b);
     if constexpr (!PAGED) return ring_rs;
     const int pg = tin >> a.pm.page_shift;
     tin &= a.pm.page_tokens - 1;
@@ -199,6 +218,7 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     o.s = ld128(r, lo_vs, vm);
     if (wv < 2) o.zz = ld32(r, has_zz ? lo_zz : lo_vs, vm);
+    if (WINDOW && wv < 1) o.zs = ld32(r, has_zz ? lo_zz - fresh_vm : lo_vs, vm);
   };
   auto put_key = [&](int b, u4_t hi, u4_t lo) {
     u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
@@ -209,6 +229,25 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
     op[8 * PK + wv * PV][lane] = hi;
     if constexpr (PV == 2) op[8 * PK + wv * PV + 1][lane] = lo;
+  };
+  // Windowed attention: z + c0 s as hi and lifted lo halves (22 bits; below 2^-14
+  // a multiple of 2^-25, all of it in the low one) in place of z and s, whose
+  // sums over the tokens are opposite and leave their rounding where the values
+  // average out (4096 tokens K2V2: 4.3e-6 apart, 1.8e-6 so).
+  auto put_mid = [&](int b, uint32_t zz, uint32_t zs) {
+    if (wv < 1 && has_zz) {
+      u4_t* op = &sm.op[b & (kSlots - 1)][kZOp][16 * (zpos >> 2)];
+      const h2_t z = u2h(zz), sc = u2h(zs);
+      h2_t hi, lo;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float x = fmaf((float)sc[e], Code<BV>::c0, (float)z[e]);
+        hi[e] = fabsf(x) < 0x1p-14f ? (_Float16)0.f : (_Float16)x;
+        lo[e] = (_Float16)((x - (float)hi[e]) * kMidLift);
+      }
+      reinterpret_cast<uint32_t*>(&op[zrow])[zpos & 3] = h2u(hi);
+      reinterpret_cast<uint32_t*>(&op[4 + zrow])[zpos & 3] = h2u(lo);
+    }
   };
   auto put_zz = [&](int b, uint32_t zz) {
     if (wv < 2 && has_zz) {
@@ -232,7 +271,8 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     u4_t hi, lo;
     unpack_scaled<BV, true>(o.x, o.s, BV == 1 ? 4 * (wv & 3) : 16 * (wv & 1), vfac, hi, lo);
     put_value(b, hi, lo);
-    put_zz(b, o.zz);
+    if constexpr (WINDOW) put_mid(b, o.zz, o.zs);
+    else put_zz(b, o.zz);
   };
   // fp16 tail: the raw halves are the operands (keys negated with q)
   auto load_tail = [&](int b, u4_t& k, u4_t& v) {
@@ -251,13 +291,14 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   // key zero-point tables: block b starts one when it is the first block of
   // the first of 16 key groups, counted from the split's first
-  const int bsh = gsh - 5, j0 = b0 >> bsh;  // 2^bsh blocks per key group
+  const int j0 = b0 >> bsh;
   auto table_start = [&](int b) {
     return (b == b0 || ((b & ((1 << bsh) - 1)) == 0 && ((b >> bsh) - j0) % kZGroups == 0));
   };
   u4_t zreg = {0u, 0u, 0u, 0u};
   auto load_zs = [&](int b) {  // 512 threads: 16 groups of 512 bytes, 16 each
-    const int j = min((b >> bsh) + (int)(threadIdx.x >> 5), (S.Lq >> gsh) - 1);
+    int j = min((b >> bsh) + (int)(threadIdx.x >> 5), (WINDOW ? wgroups.count : S.Lq >> gsh) - 1);
+    if constexpr (WINDOW) j += j < wgroups.sink ? 0 : wgroups.first - wgroups.sink;
     const int t = j << gsh, pg = PAGED ? t >> a.pm.page_shift : 0, tin = PAGED ? t & (a.pm.page_tokens - 1) : t;
     const uint8_t* seg = PAGED ? a.arena + a.pm.pool0 +
                                      (uint64_t)a.pm.table[(size_t)S.seq * a.pm.max_pages + pg] * a.pm.page_bytes +
@@ -326,14 +367,26 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr bool MASKED = decltype(masked_c)::value, PACKED = decltype(packed_c)::value;
     const float ksc = PACKED ? (BK == 1 ? 0.5f : 2.f) * a.qscale : a.qscale;
     float z[2], top[2];
+    // token 16 mb + 4 blk + r is visible below left; windowed attention: and
+    // from `from` on, or below `sunk`
     int left[2];
+    [[maybe_unused]] int from[2], sunk;
+    const int place = block_at(b);
+    auto seen = [&](int u, int e) {
+      const int i = 16 * (e >> 2) + (e & 3);
+      return i < left[u] && (!WINDOW || i >= from[u] || i < sunk);
+    };
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       z[u] = PACKED ? sm.dz[wv][((b >> bsh) - j0) % kZGroups][16 * u + col] * ksc : 0.f;
-      left[u] = lim[u] - 32 * b - 4 * blk;  // token 16 mb + 4 blk + r is visible below it
+      left[u] = lim[u] - 32 * place - 4 * blk;
+      if constexpr (WINDOW) {
+        from[u] = max(lim[u] - a.window, 0) - 32 * place - 4 * blk;
+        sunk = a.sinks - 32 * place - 4 * blk;
+      }
       if constexpr (MASKED) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[u][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < left[u] ? d[u][e >> 2][e & 3] : kNoScore;
+        for (int e = 0; e < 8; ++e) d[u][e >> 2][e & 3] = seen(u, e) ? d[u][e >> 2][e & 3] : kNoScore;
       }
       const f4_t x = d[u][0], y = d[u][1];
       top[u] = fmaf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))), ksc, z[u]);
@@ -364,7 +417,7 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[u][e] = __builtin_amdgcn_exp2f(fmaf(d[u][e >> 2][e & 3], ksc, bias));
-        if constexpr (MASKED) p[u][e] = 16 * (e >> 2) + (e & 3) < left[u] ? p[u][e] : 0.f;
+        if constexpr (MASKED) p[u][e] = seen(u, e) ? p[u][e] : 0.f;
       }
     }
     next();
@@ -459,6 +512,10 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   const std::true_type yes{};
   const std::false_type no{};
   const int bp = min(b1, nb_packed);  // packed blocks [b0, bp), then the tail's
+  // whether any row of the wave sees a token of the block at tok
+  auto wave_sees = [&](int tok) {
+    return tok < wave_limit && (!WINDOW || tok + 32 > wave_first - a.window || tok < a.sinks);
+  };
   // Pipeline: step b reads the keys of block b + 1 and the values of block b,
   // and writes the keys of b + 3 and the values of b + 2, whose loads went out
   // a step earlier; a barrier before every second step then keeps each
@@ -503,6 +560,34 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     };
     // three phases with the same barriers: all tokens visible to the wave's
     // rows, some, none (the wave only unpacks for the others)
+    if constexpr (WINDOW) {
+      // runs of blocks of one kind: every row sees all of it, some, none
+      auto kind = [&](int b) {
+        const int tok = 32 * block_at(b);
+        if (!wave_sees(tok)) return 2;
+        return tok + 32 <= wave_first && (tok >= wave_limit - a.window || tok + 32 <= a.sinks) ? 0 : 1;
+      };
+      for (int b = b0; b < bp;) {
+        for (; b < bp && kind(b) == 1; ++b) {
+          begin(b);
+          softmax(yes, yes, b, d, [&] { scores(b + 1, d); fetch(b); });
+          values(lows_c, b);
+          refill(b);
+        }
+        for (; b < bp && kind(b) == 0; ++b) {
+          begin(b);
+          softmax(no, yes, b, d, [&] { scores(b + 1, d); fetch(b); });
+          values(lows_c, b);
+          refill(b);
+        }
+        for (; b < bp && kind(b) == 2; ++b) {
+          begin(b);
+          scores(b + 1, d);
+          refill(b);
+        }
+      }
+      return;
+    }
     const int bv = max(b0, min(bp, wave_first / 32)), bm = max(b0, min(bp, (wave_limit + 31) / 32));
     int b = b0;
     for (; b < bv; ++b) {
@@ -528,9 +613,10 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   // low halves join (5e-7 to 1e-6; 8192 tokens 120 us, 105 without them).  At
   // four and eight bits the smaller groups are at 1.6e-4 to 2.9e-4 themselves,
   // and the low halves matter only where the scales are subnormal: their
-  // rounding leaves codes unused, and the products are lopsided.
+  // rounding leaves codes unused, and the products are lopsided.  Windowed
+  // attention takes the low halves in every class.
   if (b0 < bp) {
-    if (PV == 1 || vbits < 0x0400u) packed_blocks(yes);
+    if (WINDOW || PV == 1 || vbits < 0x0400u) packed_blocks(yes);
     else packed_blocks(no);
   }
   float unit_acc = unit_packed;  // factor of the value accumulators
@@ -545,17 +631,18 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     bool own_raw = false;  // this wave's value tile met a number of 8 or more
     const u4_t none = {0u, 0u, 0u, 0u};
     u4_t k, v;
-    load_tail(max(b0, nb_packed), k, v);
+    load_tail(block_at(max(b0, nb_packed)), k, v);
     for (int b = max(b0, nb_packed); b < b1; ++b) {
       __syncthreads();  // every wave is done with the buffer
       put_key(b, k, none);
       own_raw = own_raw || needs_raw(v);
       if (lane == 0) sm.raw[wv] = own_raw ? 1u : 0u;
       put_value(b, __builtin_bit_cast(u4_t, lifted(v, own_raw)), none);
-      put_zz(b, 0u);
-      if (b + 1 < b1) load_tail(b + 1, k, v);
+      if constexpr (WINDOW) put_mid(b, 0u, 0u);
+      else put_zz(b, 0u);
+      if (b + 1 < b1) load_tail(block_at(b + 1), k, v);
       __syncthreads();
-      if (32 * b < wave_limit) {
+      if (wave_sees(32 * block_at(b))) {
         f4_t d[2][2];
         scores(b, d);
         softmax(yes, no, b, d, [] {});
@@ -575,7 +662,8 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
     float zt[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      zt[r] = fmaf(Code<BV>::c0 / (float)sf, __shfl(zac[u][r], 16 + col),
+      zt[r] = WINDOW ? fmaf(1.f / kMidLift, __shfl(zac[u][r], 16 + col), __shfl(zac[u][r], col))
+                     : fmaf(Code<BV>::c0 / (float)sf, __shfl(zac[u][r], 16 + col),
                    fmaf(1.f / kLift, __shfl(zac[u][r], 48 + col), __shfl(zac[u][r], col)));
     const float l = __shfl(zac[u][0], 32 + col);
     int x, head;
@@ -608,18 +696,29 @@ __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 }
 
+#ifdef KVQ_WINDOW
+constexpr bool kWindow = true;
+#else
+constexpr bool kWindow = false;
+#endif
+
 template <int BK, int BV>
 int launch_pages(const DecodeArgs& a, void* stream) {
   if (a.pm.table != nullptr)
-    hipLaunchKernelGGL((prefill_mfma_kernel<BK, BV, true>), dim3(a.total_wg), dim3(64 * kNW), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((prefill_mfma_kernel<BK, BV, true, kWindow>), dim3(a.total_wg), dim3(64 * kNW), 0, (hipStream_t)stream, a);
   else
-    hipLaunchKernelGGL((prefill_mfma_kernel<BK, BV, false>), dim3(a.total_wg), dim3(64 * kNW), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((prefill_mfma_kernel<BK, BV, false, kWindow>), dim3(a.total_wg), dim3(64 * kNW), 0, (hipStream_t)stream, a);
   return (int)hipGetLastError();
 }
 
 }  // namespace
 
+// This source is compiled once more for windowed attention (KVQ_WINDOW).
+#ifdef KVQ_WINDOW
+int launch_window_rows(const DecodeArgs& a, int bk, int bv, void* stream) {
+#else
 int launch_prefill(const DecodeArgs& a, int bk, int bv, void* stream) {
+#endif
   if (a.total_wg <= 0) return 0;
   if (bk == 1 && bv == 1) return launch_pages<1, 1>(a, stream);
   if (bk == 1 && bv == 2) return launch_pages<1, 2>(a, stream);

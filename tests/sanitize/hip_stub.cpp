@@ -195,10 +195,9 @@ int launch_decode_matrix(const DecodeArgs& a, int bk, int bv, int rows, void*) {
 int launch_chunk_matrix(const DecodeArgs& a, int bk, int bv, int rows, void*) {
   return check_rows(a, rows), touch_decode(a, bk, bv), 0;
 }
-// A windowed launch: the key groups of every row group's splits, which have to
-// be all that the row group sees and lie below the packed end.
-int launch_window(const DecodeArgs& a, int bk, int bv, void*) {
-  check_rows(a, 16);
+// A windowed launch: what its workgroups read of the cache has to be all that
+// their rows see, and lie below the packed end.  step: queries per workgroup.
+static void touch_window(const DecodeArgs& a, int bk, int bv, int step, bool many) {
   const int gsh = a.gk == 32 ? 5 : a.gk == 64 ? 6 : 7, gps = a.split_tokens >> gsh;
   const size_t rows = (size_t)a.hq * a.nqry;
   auto bad = [&](const char* what, int seq) {
@@ -207,26 +206,44 @@ int launch_window(const DecodeArgs& a, int bk, int bv, void*) {
   };
   for (int i = 0; i < a.nseq; ++i) {
     const DecodeSeq& S = a.seq[i];
-    for (int rg = 0; rg < a.nrg; ++rg) {
-      const int first = S.L - a.nqry + 1 + rg * a.qpr, last = S.L - a.nqry + std::min(rg * a.qpr + a.qpr, a.nqry);
+    for (int q0 = 0; q0 < a.nqry; q0 += step) {
+      const int first = S.L - a.nqry + 1 + q0, last = S.L - a.nqry + std::min(q0 + step, a.nqry);
       const WindowGroups g = window_groups(first, last, S.Lq, gsh, a.window, a.sinks);
-      if (g.count > S.nq * gps) bad("splits", S.seq);
-      std::vector<char> held(S.Lq / a.gk, 0);
+      std::vector<char> held((S.L + 31) / 32 + 4, 0);  // by block
       for (int v = 0; v < g.count; ++v) {
         const int j = v < g.sink ? v : v - g.sink + g.first;
-        if (j >= S.Lq / a.gk || held[j]) bad("group", S.seq);
-        held[j] = 1;
+        if (j >= S.Lq / a.gk || held[j << (gsh - 5)]) bad("group", S.seq);
+        for (int b = 0; b < 1 << (gsh - 5); ++b) held[(j << (gsh - 5)) + b] = 1;
         for (int h = 0; h < a.hkv; ++h) packed_ranges(a, S.head0, S.seq, h, j * a.gk, (j + 1) * a.gk, bk, bv, rd);
       }
+      const int nb = g.count << (gsh - 5);
+      if (many) {
+        const int tail0 = a.sinks <= S.Lq ? std::max(S.Lq, std::max(first - a.window, 0)) / 32 : S.Lq / 32;
+        const int total = nb + std::max(0, (last + 31) / 32 - tail0);
+        if (total > S.nq * S.nsplit) bad("blocks", S.seq);
+        for (int b = nb; b < total; ++b) held[b - nb + tail0] = 1;
+      } else {
+        if (g.count > S.nq * gps) bad("splits", S.seq);
+        for (int b = S.Lq / 32; 32 * b < S.L; ++b) held[b] = 1;
+      }
       for (int p = first; p <= last; ++p)
-        for (int t = 0; t < std::min(p, S.Lq); ++t)
-          if ((t >= p - a.window || t < a.sinks) && !held[t / a.gk]) bad("unread token", S.seq);
+        for (int t = 0; t < p; ++t)
+          if ((t >= p - a.window || t < a.sinks) && !held[t / 32]) bad("unread token", S.seq);
     }
     for (int h = 0; h < a.hkv; ++h) ring_ranges(a, S.head0, h, S.Lq, S.L, rd);
     rd(a.q + (size_t)S.seq * rows * kHeadDim, rows * kTokenBytes);
-    wr(a.ws + (size_t)S.ws_base * rows * kRecFloats, S.nsplit * rows * kRecFloats * 4);
+    if (many && S.nsplit == 1)
+      wr(a.out + (size_t)S.seq * rows * kHeadDim, rows * kHeadDim * 4);
+    else
+      wr(a.ws + (size_t)S.ws_base * rows * kRecFloats, S.nsplit * rows * kRecFloats * 4);
   }
-  return ++g_launches, 0;
+  ++g_launches;
+}
+int launch_window(const DecodeArgs& a, int bk, int bv, void*) {
+  return check_rows(a, 16), touch_window(a, bk, bv, a.qpr, false), 0;
+}
+int launch_window_rows(const DecodeArgs& a, int bk, int bv, void*) {
+  return check_rows(a, 32), touch_window(a, bk, bv, a.qpr * kPrefillWaves, true), 0;
 }
 int launch_export(const ExportArgs& a, void*) {
   check_regions(a, nullptr);

@@ -2,8 +2,12 @@
 against the fp64 oracle on the same quantized cache, through the public calls.
 
 Every output has to lie within
-    tol * softmax-weighted |V^| of its channel,  tol = 2 ln 2 * 16 * 2^-24 * A + 2^-20,
-A the largest sum_c |q_c K^_c| log2(e) / sqrt(d) of the row's tokens: a score
+    tol * softmax-weighted M of its channel,  tol = 2 ln 2 * 16 * 2^-24 * A + 2^-20,
+M a token's largest |V^| in the channel's value group: V^ = z + code s is the
+sum of (z + c0 s) and (code - c0) s, neither of them larger than 2 M, each held
+to 22 bits or more, so that a value that comes out near zero is as exact as its
+group's largest and no more (2^-24 M for each of the two, and for their sums).
+A is the largest sum_c |q_c K^_c| log2(e) / sqrt(d) of the row's tokens: a score
 is a sum of 128 fp32-accumulated products (16 roundings at its magnitude
 allowed), an error d of base-2 scores moves a weight and the sum of weights by
 ln 2 * d each, and weights, keys and values enter with 22 bits or more
@@ -27,7 +31,7 @@ HQ_HKV = {1: (2, 2), 2: (4, 2), 4: (8, 2), 5: (10, 2), 8: (8, 1)}
 class Setup:
     """A cache of ragged sequences, its inputs, and the oracle's dequantized heads."""
 
-    def __init__(self, lens, bk, bv, gq=4, gk=32, gv=32, R=0, page=0, cap=0, seed=11):
+    def __init__(self, lens, bk, bv, gq=4, gk=32, gv=32, R=0, page=0, cap=0, seed=11, kmul=1.0, vmul=1.0, vadd=0.0):
         self.hq, self.hkv = HQ_HKV[gq]
         b = len(lens)
         bk, bv = ([x] * b if isinstance(x, int) else list(x) for x in (bk, bv))
@@ -37,6 +41,9 @@ class Setup:
                                  page_tokens=page)
         w = Workload("window", b, self.hq, self.hkv, 128, tuple(lens), tuple(bk), tuple(bv), gk, gv, R, cfg_id=seed)
         self.kv = [gen_kv(w, 0, s) for s in range(b)]
+        if (kmul, vmul, vadd) != (1.0, 1.0, 0.0):
+            self.kv = [((k * np.float32(kmul)).astype(np.float16), (v * np.float32(vmul) + np.float32(vadd)).astype(np.float16))
+                       for k, v in self.kv]
         n = max(max(lens), 1)
         K, V = (np.zeros((b, n, self.hkv, 128), dtype=np.float16) for _ in range(2))
         for s, (k, v) in enumerate(self.kv):
@@ -66,7 +73,8 @@ class Setup:
                 continue
             Kh, Vh = self.dequant(s)
             ref = oracle.window_attention(q[s], Kh, Vh, window, sinks)
-            size = oracle.window_attention(q[s], Kh, np.abs(Vh), window, sinks)
+            M = np.abs(Vh).reshape(self.hkv, n, 128 // self.gv, self.gv).max(-1).repeat(self.gv, -1)
+            size = oracle.window_attention(q[s], Kh, M, window, sinks)
             k = np.abs(Kh).repeat(self.hq // self.hkv, 0)
             A = (np.abs(q[s].astype(np.float64)).transpose(1, 0, 2) @ k.transpose(0, 2, 1)).max() * math.log2(math.e) / math.sqrt(128)
             tol = 2 * math.log(2) * 16 * 2.0 ** -24 * A + 2.0 ** -20
@@ -134,8 +142,20 @@ def test_every_class(bk, bv):
     c = Setup((420, 77), bk, bv, R=3)
     q = c.queries(1)
     c.check(q, run(c, q, 100, 4), 100, 4)
-    q = c.queries(30)
-    c.check(q, run(c, q, 50, 4), 50, 4)
+    for n_q in (30, 70):  # 16-row groups, many rows
+        q = c.queries(n_q)
+        c.check(q, run(c, q, 50, 4), 50, 4)
+
+
+@pytest.mark.parametrize("kw", [dict(vmul=1e-5), dict(vmul=2e-7), dict(vadd=3000.0), dict(vmul=5000.0), dict(kmul=1e-5),
+                                dict(kmul=20.0), dict(vmul=1e-3, vadd=1e-4)], ids=str)
+@pytest.mark.parametrize("bits", [1, 2, 4, 8])
+def test_small_and_large_numbers(kw, bits):
+    # scales and zero-points that are subnormal halves, values far from zero, keys that peak the softmax
+    c = Setup((330, 200), bits, bits, R=20, **kw)
+    for n_q in (1, 6, 70):
+        q = c.queries(n_q)
+        c.check(q, run(c, q, 120, 4), 120, 4)
 
 
 def test_forced_splits_and_growing_cache():
