@@ -29,6 +29,21 @@ constexpr int kThreads = 256;
 constexpr int kPer = kDistillChunk / kThreads;  // logits per thread, in runs of 8
 constexpr int kMaxK = kDistillMaxK;
 
+// 8 consecutive logits; those from `n` on read as -inf
+template <class T>
+__device__ __forceinline__ void load_part(const typename T::raw* p, int n, float (&v)[8]) {
+  raw8_t<T> x = all8<T>(-__builtin_inff());
+  if (n >= 8) {
+    x = load8<T>(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) x[j] = p[j];
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = T::value(x[j]);
+}
+
 // T's gradient or loss entry of a row: its place, its share q (0: no entry)
 struct Entry {
   int index;
@@ -51,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void distill_sums_kernel(DistillArgs a) {
 #pragma unroll
   for (int i = 0; i < kPer / 8; ++i) {
     const int at = from + 8 * (i * kThreads + tid);
-    load8<T>(z + at, a.vocab - at, v[i]);
+    load_part<T>(z + at, a.vocab - at, v[i]);
   }
 #pragma unroll
   for (int i = 0; i < kPer / 8; ++i)
@@ -79,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void distill_sums_kernel(DistillArgs a) {
 
 __device__ __forceinline__ double wave_sum_d(double v) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __builtin_bit_cast(double, shfl_xor64(__builtin_bit_cast(uint64_t, v), d));
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   return v;
 }
 
@@ -178,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a) {
 #pragma unroll
   for (int i = 0; i < kPer / 8; ++i) {
     const int at = from + 8 * (i * kThreads + tid);
-    load8<T>(z + at, a.vocab - at, v[i]);
+    load_part<T>(z + at, a.vocab - at, v[i]);
   }
   // p = 2^((z - m) c - less)
   float m, less;

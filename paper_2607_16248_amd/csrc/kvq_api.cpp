@@ -270,7 +270,7 @@ kvq_status check_rows(const void* logits, int type, int64_t row_stride, int rows
   if (vocab < 1) return fail(KVQ_ERR_ARG, "vocab must be >= 1 (got %d)", vocab);
   if (vocab > 1 << 24) return fail(KVQ_ERR_UNSUPPORTED, "vocab %d above 2^24", vocab);
   if (row_stride < vocab) return fail(KVQ_ERR_ARG, "row_stride %lld smaller than vocab %d", (long long)row_stride, vocab);
-  if ((int64_t)rows * ((vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk) > INT32_MAX)
+  if ((int64_t)rows * ((vocab + 8191) / 8192) > INT32_MAX)
     return fail(KVQ_ERR_UNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
   const int size = type == DGAP_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(logits) % size != 0) return fail(KVQ_ERR_ARG, "logits must be aligned to their type");
@@ -284,10 +284,16 @@ kvq_status check_scratch(const void* ws, size_t ws_bytes, size_t need) {
   return KVQ_OK;
 }
 
+// A workgroup per row takes all steps of a draw from so many rows on, and for
+// vocabularies up to kSampleSmall: 128 rows of 128256 fp32 58 us, with chunks of
+// rows 66 (64 rows 45 and 39); one row of 32768 16 us and 17.
+constexpr int kSampleRows = 128, kSampleSmall = 32768;
+
 // Workspace of one row of dgap_sample (see SampleArgs::ws).
 uint64_t sample_row_bytes(int vocab) {
   const uint64_t nchunk = (vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk;
-  return kvq::align_up(8 * (kvq::kSampleBins + kvq::kSampleList + nchunk) + 4 * (kvq::kSampleBins + 1), kvq::kAlign);
+  const uint64_t ngroup = (vocab + kvq::kSampleGroup - 1) / kvq::kSampleGroup;
+  return kvq::align_up(12 * kvq::kSampleBins + 4 * (ngroup + nchunk), kvq::kAlign);
 }
 
 kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* grad, int64_t grad_row_stride,
@@ -1338,7 +1344,14 @@ kvq_status dgap_sample(const dgap_sampling* p, int32_t* tokens, float* logprobs,
   a.row_stride = p->row_stride;
   a.row_bytes = sample_row_bytes(p->vocab);
   a.batch = p->batch; a.vocab = p->vocab;
-  a.nchunk = (p->vocab + kvq::kSampleChunk - 1) / kvq::kSampleChunk;
+  a.ngroup = (p->vocab + kvq::kSampleGroup - 1) / kvq::kSampleGroup;
+  if ((p->batch < kSampleRows && p->vocab > kSampleSmall) || p->vocab > kvq::kSampleNarrow) {
+    // workgroups for every compute unit, of 2048 logits at least
+    int64_t chunk = 8192;
+    while (chunk > kvq::kSampleChunk && p->batch * ((p->vocab + chunk - 1) / chunk) < target_workgroups(1)) chunk /= 2;
+    a.chunk = (int32_t)chunk;
+    a.nchunk = (int32_t)((p->vocab + chunk - 1) / chunk);
+  }
   // the sum of all weights stays below 2^63; 45: a bin 51 octaves below the
   // largest weight holds none
   a.unit = std::min(45, 62 - log2_exact(p->vocab));

@@ -256,9 +256,11 @@ struct DgapArgs {
 
 // ---------------------------------------------------------------- sampling
 
-constexpr int kSampleChunk = 8192;   // logits per workgroup
+constexpr int kSampleChunk = 2048;   // logits per workgroup at least
+constexpr int kSampleNarrow = 1 << 19;  // logits of a row whose bins count in one word
 constexpr int kSampleBins = 2048;    // bins of a row's weights
 constexpr int kSampleList = 2048;    // elements that a row's searches may end among
+constexpr int kSampleGroup = 512;    // logits whose largest one is kept
 
 struct SampleArgs {
   const void* logits;
@@ -269,10 +271,11 @@ struct SampleArgs {
   const float* uniform;
   int32_t* tokens;
   float* logprobs;           // or null
-  uint8_t* ws;               // per row: bin masses, list, chunk keys (64 bits each), bin counts, list length (32)
+  uint8_t* ws;               // per row: bins (64 bits each), their counts, the groups' and the chunks' largest logits (32)
   int64_t row_stride;        // elements
   uint64_t row_bytes;        // of ws
-  int32_t batch, vocab, nchunk;
+  int32_t batch, vocab, ngroup;
+  int32_t nchunk, chunk;     // chunks of a row, their logits; nchunk = 0: a workgroup per row takes all steps
   int32_t unit;              // masses are in units of 2^-unit of the largest weight
 };
 

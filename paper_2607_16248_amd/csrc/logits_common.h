@@ -9,37 +9,41 @@
 namespace kvq {
 namespace logits {
 
-// One type's storage and its value in fp32 (exact for all three).
+// One type's storage and its value in fp32 (exact for all three), whose lowest
+// kZeroBits bits are zero.
 struct F32 {
   typedef float raw;
+  static constexpr int kZeroBits = 0;
   static __device__ __forceinline__ float value(raw x) { return x; }
   static __device__ __forceinline__ raw make(float x) { return x; }
 };
 struct F16 {
   typedef _Float16 raw;
+  static constexpr int kZeroBits = 13;
   static __device__ __forceinline__ float value(raw x) { return (float)x; }
   static __device__ __forceinline__ raw make(float x) { return (_Float16)x; }
 };
 struct BF16 {
   typedef __bf16 raw;
+  static constexpr int kZeroBits = 16;
   static __device__ __forceinline__ float value(raw x) { return (float)x; }
   static __device__ __forceinline__ raw make(float x) { return (__bf16)x; }
 };
 
-// 8 consecutive logits from p, which has its element's alignment only; those
-// from `n` on read as -inf.
+// 8 consecutive logits from p, which has its element's alignment only.
 template <class T>
-__device__ __forceinline__ void load8(const typename T::raw* p, int n, float (&v)[8]) {
-  typedef typename T::raw vec __attribute__((ext_vector_type(8)));
-  typedef vec vec_any __attribute__((aligned(sizeof(typename T::raw))));
-  if (n >= 8) {
-    const vec x = *reinterpret_cast<const vec_any*>(p);
+using raw8_t = typename T::raw __attribute__((ext_vector_type(8)));
+template <class T>
+__device__ __forceinline__ raw8_t<T> load8(const typename T::raw* p) {
+  typedef raw8_t<T> any __attribute__((aligned(sizeof(typename T::raw))));
+  return *reinterpret_cast<const any*>(p);
+}
+template <class T>
+__device__ __forceinline__ raw8_t<T> all8(float x) {
+  raw8_t<T> v;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = T::value(x[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? T::value(p[j]) : -__builtin_inff();
-  }
+  for (int j = 0; j < 8; ++j) v[j] = T::make(x);
+  return v;
 }
 
 // Keys whose order is that of (logit, lower index first): the sign-flipped bits
@@ -58,36 +62,29 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return ~(uint32_t)k; }
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int mask) {
-  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, mask), hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), mask);
+// 64-bit wave reductions over DPP moves (no LDS round trips): shifts by 1, 2, 4
+// and 8 within each row of 16 lanes, then the row totals through the row
+// broadcasts 15 and 31.  Lanes without a source read 0.
+template <int CTRL, int ROW_MASK = 0xF>
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROW_MASK, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROW_MASK, 0xF, false);
   return ((uint64_t)hi << 32) | lo;
 }
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) {
-  const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)v, d), hi = (uint32_t)__shfl_up((int)(uint32_t)(v >> 32), d);
-  return ((uint64_t)hi << 32) | lo;
-}
-__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t o = shfl_xor64(v, d);
-    v = o > v ? o : v;
-  }
-  return v;
-}
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += shfl_xor64(v, d);
-  return v;
+__device__ __forceinline__ uint64_t lane64(uint64_t v, int lane) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
 __device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t o = shfl_up64(v, d);
-    v += lane >= d ? o : 0;
-  }
+  v += dpp64<0x111>(v);
+  v += dpp64<0x112>(v);
+  v += dpp64<0x114>(v);
+  v += dpp64<0x118>(v);
+  v += dpp64<0x142, 0xA>(v);
+  v += dpp64<0x143, 0xC>(v);
   return v;
 }
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) { return lane64(wave_scan64(v), 63); }
 
 }  // namespace logits
 }  // namespace kvq

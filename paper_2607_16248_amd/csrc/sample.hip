@@ -6,23 +6,37 @@
 // that order, passes u times the kept total: every step is a search for the
 // element where a count or a mass reaches a target.  With d = log2(e) / T
 // (z_max - z) an element weighs 2^-d.
-//   max     one workgroup per (row, chunk): the chunk's largest key
-//   bins    one per (row, chunk): counts and masses of 2048 bins of d, 1/40 of an
-//           octave each, added up per row with integer atomics
-//   gather  one per (row, chunk): from the bins' prefix sums the bins where the
-//           searches end (a bracket of bins, where a target depends on an
-//           earlier search); their elements, a few hundred, go to the row's list
-//   finish  one per row: the list sorted, the searches ended
-// Masses are whole numbers of 2^-kUnit of the largest weight (64 bits): sums are
-// exact, so they depend neither on the order of the atomics nor on which
-// elements a bin or the list summed.  A weight is a 24-bit number (one hardware
-// exponential of the fraction of d, taken in 64 bits); those below
-// 2^-(kUnit + 1) count as 0, at most V 2^-(kUnit + 1) of the largest weight
-// together.  They, and all of the last bin, are never chosen.
-// A row whose bins hold more elements than a list (thousands of equal logits)
-// is searched by the finish over all its logits, a digit of the keys at a time.
+//   max     the row's largest logit
+//   bins    counts and masses of 2048 bins of d, 1/40 of an octave each
+//   ends    from the bins' prefix sums the bins where the searches end (a
+//           bracket of bins, where a target depends on an earlier search)
+//   select  the elements of those bins, a few hundred, listed; the
+//           searches ended among them, a digit of the keys at a time
+// Few rows: max and bins take one workgroup per (row, chunk), ends and select
+// one per row (three launches).  Many rows: one workgroup per row takes all
+// steps, reading the row three times (the second and third time from cache).
+//
+// A weight is a 24-bit number M 2^-n (n = floor(d), one hardware exponential of
+// the rest, d itself in 64 bits), and all elements of a bin share n, so a bin's
+// mass is a whole number, counted up with its elements in one 64-bit atomic;
+// masses across bins are whole numbers of 2^-unit of the largest weight.  Sums
+// are exact: they depend neither on the order of the atomics nor on whether a
+// bin or the list summed an element.  Weights below 2^-unit count as 0 (unit is
+// 45, 38 for the largest vocabularies); they, and all of the last bin, are never
+// chosen.  A row whose bins hold more elements than a list (thousands of equal
+// logits) is searched over all its logits, a digit of the keys at a time.
+//
+// What bounds it: latency, along one workgroup's dependent steps: of one row's 25
+// us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then ends 4, listing
+// 7 and the three searches 4, one step after the other at a few waves per SIMD.
+// Many rows: 256 flat ones of 128256 fp16 61 us, of which the bins are half (fp64
+// differences, an exponential and an LDS atomic per logit).  Each row is read once
+// from HBM (13 us of those 61).  Sorting the list took 5 to 22 us where the digit
+// searches take 4 to 8; straight-line code for every match of a load, run once
+// from a cold instruction cache, cost more than a loop.
 #include <hip/hip_runtime.h>
 
+#include "decode_common.h"
 #include "kvq_internal.h"
 #include "logits_common.h"
 
@@ -32,10 +46,16 @@ namespace {
 using namespace logits;
 
 constexpr int kThreads = 256;
+constexpr int kRowThreads = 1024;
+constexpr int kAhead = 4;  // loads under way of a thread of those as it lists elements
+constexpr int kGroup = kSampleGroup;
+static_assert(kGroup == 64 * 8, "a wave's loads");
 constexpr int kBins = kSampleBins;
-constexpr double kPerOctave = 40.0;  // 51 octaves: past them no weight is left (kUnit <= 45)
-constexpr int kFinishThreads = 1024;
-constexpr uint64_t kBadRow = ~0ull;  // key of a chunk that holds a NaN or +inf
+constexpr int kPerOctave = 40;  // 51 octaves: past them no weight is left (unit <= 45)
+// a bin while its elements are counted: their number above bit kCount, the sum
+// of their M below (of a chunk or a row of up to 2^19: 2^43)
+constexpr int kCount = 44;
+constexpr uint64_t kSum = (1ull << kCount) - 1;
 
 struct Row {
   double inv;      // log2(e) / T
@@ -62,125 +82,178 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
 }
 
 __device__ __forceinline__ double depth(double zmax, float z, double inv) { return (zmax - (double)z) * inv; }
-__device__ __forceinline__ int bin_of(double d) { return (int)fmin(d * kPerOctave, (double)(kBins - 1)); }
-// 2^-d in units of 2^-unit
-__device__ __forceinline__ uint64_t weight_of(double d, int unit) {
-  if (!(d < (double)(unit + 1))) return 0;
+
+// An element's bin and M.
+struct Place {
+  int bin;
+  uint32_t m;
+};
+__device__ __forceinline__ Place place_of(double d) {
+  d = fmin(d, 60.0);
   const int n = (int)d;
-  const uint32_t m = (uint32_t)(__builtin_amdgcn_exp2f(-(float)(d - (double)n)) * 16777216.f);
-  const int sh = unit - 24 - n;
-  return sh >= 0 ? (uint64_t)m << sh : (uint64_t)((m + (1u << (-sh - 1))) >> -sh);
+  const float f = fminf((float)__builtin_amdgcn_fract(d), 0x1.fffffep-1f);
+  return {min(n * kPerOctave + (int)(f * (float)kPerOctave), kBins - 1),
+          (uint32_t)(__builtin_amdgcn_exp2f(-f) * 16777216.f)};
+}
+// M or a sum of them in a bin, in units of 2^-unit
+__device__ __forceinline__ uint64_t mass_of(uint64_t m, int bin, int unit) {
+  const int sh = unit - 24 - bin / kPerOctave;
+  return sh >= 0 ? m << sh : m >> -sh;
 }
 
-__device__ __forceinline__ uint64_t* row_mass(const SampleArgs& a, int row) {
+__device__ __forceinline__ uint64_t* row_bins(const SampleArgs& a, int row) {
   return reinterpret_cast<uint64_t*>(a.ws + (size_t)row * a.row_bytes);
 }
-__device__ __forceinline__ uint64_t* row_list(const SampleArgs& a, int row) { return row_mass(a, row) + kBins; }
-__device__ __forceinline__ uint64_t* row_keys(const SampleArgs& a, int row) { return row_list(a, row) + kSampleList; }
+// (vocabularies past 2^19 count their bins' elements apart)
 __device__ __forceinline__ uint32_t* row_count(const SampleArgs& a, int row) {
-  return reinterpret_cast<uint32_t*>(row_keys(a, row) + a.nchunk);  // [kBins], then the list's length
+  return reinterpret_cast<uint32_t*>(row_bins(a, row) + kBins);
+}
+// the groups' largest logits, then the chunks'
+__device__ __forceinline__ float* row_groups(const SampleArgs& a, int row) {
+  return reinterpret_cast<float*>(row_count(a, row) + kBins);
+}
+__device__ __forceinline__ float* row_top(const SampleArgs& a, int row) { return row_groups(a, row) + a.ngroup; }
+template <class T>
+__device__ __forceinline__ const typename T::raw* row_logits(const SampleArgs& a, int row) {
+  return reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
 }
 
-// f(logits, first index, valid) for the chunk's logits, 8 a thread at a time
+// 8 logits from i on, or the last 8 of those below bulk (>= 8): loads without a
+// branch around them, which would end the overlap of several.
+template <class T>
+__device__ __forceinline__ raw8_t<T> load_below(const typename T::raw* z, int i, int bulk) {
+  return load8<T>(z + min(i, bulk - 8));
+}
+
+// f(logit, index) for the logits [from, to), 8 a thread at a time with the next
+// load on its way, then the last few one by one.
 template <class T, int NT, class F>
-__device__ __forceinline__ void each8(const typename T::raw* z, int from, int to, F f) {
-  for (int i = from + 8 * (int)threadIdx.x; i < to; i += 8 * NT) {
-    float v[8];
-    load8<T>(z + i, to - i, v);
-    f(v, i, min(8, to - i));
+__device__ __forceinline__ void each(const typename T::raw* z, int from, int to, F f) {
+  const int bulk = from + ((to - from) & ~7);
+  int i = from + 8 * (int)threadIdx.x;
+  if (bulk > from) {
+    raw8_t<T> v = load_below<T>(z, i, bulk);
+#pragma unroll 1
+    for (; i < bulk; i += 8 * NT) {
+      const raw8_t<T> x = v;
+      v = load_below<T>(z, i + 8 * NT, bulk);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f(T::value(x[j]), i + j);
+    }
   }
+  i = bulk + (int)threadIdx.x;
+  if (i < to) f(T::value(z[i]), i);
+}
+
+// The largest of the logits [from, to), in every thread; +inf where one is NaN
+// or +inf.  from is a multiple of kGroup; groups: the row's, one per kGroup
+// logits, of which this writes its own (a wave's loads at a time).
+template <class T, int NT>
+__device__ __forceinline__ float top_of(const typename T::raw* z, int from, int to, float* groups, float* part) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, bulk = from + ((to - from) & ~7);
+  float top = -__builtin_inff();
+  bool bad = false;
+  constexpr int U = NT == kRowThreads ? 4 : 1;  // (a row's one workgroup: four loads under way)
+  for (int g = from + kGroup * wv; g < to; g += 8 * NT * U) {
+    raw8_t<T> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (bulk > from) v[u] = load_below<T>(z, g + 8 * NT * u + 8 * lane, bulk);
+      else v[u] = all8<T>(-__builtin_inff());
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int g0 = g + 8 * NT * u;
+      float m = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        // (past the end the last 8 again, which the group's maximum may hold: they
+        // are below bulk, and a group's maximum is a bound)
+        const float x = T::value(v[u][j]);
+        m = fmaxf(m, x);
+        bad |= !(x < __builtin_inff());
+      }
+      if (g0 + kGroup > bulk && g0 < to && bulk + lane < to) {  // the last few, of the last group
+        const float x = T::value(z[bulk + lane]);
+        m = fmaxf(m, x);
+        bad |= !(x < __builtin_inff());
+      }
+      m = dec::wave_max(m);
+      if (lane == 0 && g0 < to) groups[g0 / kGroup] = m;
+      top = fmaxf(top, m);
+    }
+  }
+  if (__builtin_amdgcn_ballot_w64(bad)) top = __builtin_inff();
+  if (lane == 0) part[wv] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, part[w]);
+  return top;
+}
+
+// Counts the logits [from, to) into bins (LDS, cleared).
+template <class T, int NT>
+__device__ __forceinline__ void count_bins(const typename T::raw* z, int from, int to, double zmax, double inv, uint64_t* bins) {
+  uint32_t rest = 0;  // elements of the last bin: their mass is 0
+  each<T, NT>(z, from, to, [&](float x, int) {
+    const Place p = place_of(depth(zmax, x, inv));
+    if (p.bin == kBins - 1)
+      ++rest;
+    else
+      atomicAdd(reinterpret_cast<unsigned long long*>(&bins[p.bin]), (1ull << kCount) | p.m);
+  });
+  if (rest) atomicAdd(reinterpret_cast<unsigned long long*>(&bins[kBins - 1]), (unsigned long long)rest << kCount);
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void sample_max_kernel(SampleArgs a) {
-  __shared__ uint64_t part[kThreads / 64];
+  __shared__ float part[kThreads / 64];
   const int row = blockIdx.x / a.nchunk, chunk = blockIdx.x % a.nchunk, tid = threadIdx.x;
-  const auto* z = reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
-  // this workgroup's share of the row's bins and the list's length start at 0
+  // this workgroup's share of the row's bins starts at 0
   const int share = (kBins + a.nchunk - 1) / a.nchunk;
   for (int b = chunk * share + tid; b < min(kBins, (chunk + 1) * share); b += kThreads) {
-    row_mass(a, row)[b] = 0;
+    row_bins(a, row)[b] = 0;
     row_count(a, row)[b] = 0;
   }
-  if (chunk == 0 && tid == 0) row_count(a, row)[kBins] = 0;
-  uint64_t key = 0;
-  const int from = chunk * kSampleChunk, to = min(a.vocab, from + kSampleChunk);
-  each8<T, kThreads>(z, from, to, [&](const float(&v)[8], int i, int n) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint64_t k = j < n ? make_key(v[j], i + j) : 0;
-      if (!(v[j] < __builtin_inff())) k = kBadRow;
-      key = k > key ? k : key;
-    }
-  });
-  key = wave_max64(key);
-  if ((tid & 63) == 0) part[tid >> 6] = key;
-  __syncthreads();
-  if (tid == 0) {
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) key = part[w] > key ? part[w] : key;
-    row_keys(a, row)[chunk] = key;
-  }
+  const int from = chunk * a.chunk, to = min(a.vocab, from + a.chunk);
+  const float m = top_of<T, kThreads>(row_logits<T>(a, row), from, to, row_groups(a, row), part);
+  if (tid == 0) row_top(a, row)[chunk] = m;
 }
 
-// The row's largest key, in every thread.
+// The row's largest logit from its chunks', in every thread.
 template <int NT>
-__device__ __forceinline__ uint64_t row_top(const SampleArgs& a, int row, uint64_t* part) {
-  uint64_t key = 0;
-  for (int c = threadIdx.x; c < a.nchunk; c += NT) {
-    const uint64_t k = row_keys(a, row)[c];
-    key = k > key ? k : key;
-  }
-  key = wave_max64(key);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = key;
+__device__ __forceinline__ float join_top(const SampleArgs& a, int row, float* part) {
+  float m = -__builtin_inff();
+  for (int c = threadIdx.x; c < a.nchunk; c += NT) m = fmaxf(m, row_top(a, row)[c]);
+  m = dec::wave_max(m);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) key = part[w] > key ? part[w] : key;
-  __syncthreads();
-  return key;
+  for (int w = 0; w < NT / 64; ++w) m = fmaxf(m, part[w]);
+  return m;
 }
 // A row without a token to sample: settings out of range, NaN or +inf, nothing finite.
-__device__ __forceinline__ bool no_token(const Row& r, uint64_t top) {
-  return r.bad || top == kBadRow || !(key_value(top) > -__builtin_inff());
-}
+__device__ __forceinline__ bool no_token(const Row& r, float top) { return r.bad || not_finite(top); }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
-  __shared__ uint64_t mass[kBins], part[kThreads / 64];
-  __shared__ uint32_t count[kBins];
+  __shared__ uint64_t bins[kBins];
+  __shared__ float part[kThreads / 64];
   const int row = blockIdx.x / a.nchunk, chunk = blockIdx.x % a.nchunk, tid = threadIdx.x;
   const Row r = row_of(a, row);
   if (r.bad || r.greedy) return;
-  for (int b = tid; b < kBins; b += kThreads) {
-    mass[b] = 0;
-    count[b] = 0;
-  }
-  const uint64_t top = row_top<kThreads>(a, row, part);
+  for (int b = tid; b < kBins; b += kThreads) bins[b] = 0;
+  const float top = join_top<kThreads>(a, row, part);
   if (no_token(r, top)) return;
-  const double zmax = (double)key_value(top);
-  const auto* z = reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
-  const int from = chunk * kSampleChunk, to = min(a.vocab, from + kSampleChunk);
-  uint32_t rest = 0;  // elements of the last bin
-  each8<T, kThreads>(z, from, to, [&](const float(&v)[8], int, int n) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j >= n) continue;
-      const double d = depth(zmax, v[j], r.inv);
-      const int b = bin_of(d);
-      if (b == kBins - 1) {
-        ++rest;
-        continue;
-      }
-      atomicAdd(&count[b], 1u);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&mass[b]), (unsigned long long)weight_of(d, a.unit));
-    }
-  });
-  if (rest) atomicAdd(&count[kBins - 1], rest);
+  const int from = chunk * a.chunk, to = min(a.vocab, from + a.chunk);
+  count_bins<T, kThreads>(row_logits<T>(a, row), from, to, (double)top, r.inv, bins);
   __syncthreads();
+  const bool wide = a.vocab > kSampleNarrow;
   for (int b = tid; b < kBins; b += kThreads) {
-    if (count[b] == 0) continue;
-    atomicAdd(&row_count(a, row)[b], count[b]);
-    if (mass[b]) atomicAdd(reinterpret_cast<unsigned long long*>(&row_mass(a, row)[b]), (unsigned long long)mass[b]);
+    const uint64_t x = bins[b];
+    if (x == 0) continue;
+    if (wide) atomicAdd(&row_count(a, row)[b], (uint32_t)(x >> kCount));
+    atomicAdd(reinterpret_cast<unsigned long long*>(&row_bins(a, row)[b]), (unsigned long long)(wide ? x & kSum : x));
   }
 }
 
@@ -199,20 +272,22 @@ struct Ends {
 struct Prefix {
   uint64_t mass[kBins + 1];
   uint32_t count[kBins + 1];
-  uint64_t part[kFinishThreads / 64][2];
+  uint64_t part[kRowThreads / 64][2];
   int found[6];
 };
 
-template <int NT>
-__device__ __forceinline__ Ends find_ends(const SampleArgs& a, int row, const Row& r, Prefix& s, uint32_t& wanted) {
-  constexpr int kPer = kBins / NT;
+// read(bin): its count and sum of M
+template <class F>
+__device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Prefix& s, uint32_t& wanted, F read) {
+  constexpr int NT = kRowThreads, kPer = kBins / NT;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   uint64_t m[kPer], msum = 0;
   uint32_t c[kPer], csum = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    m[j] = row_mass(a, row)[tid * kPer + j];
-    c[j] = row_count(a, row)[tid * kPer + j];
+    uint64_t sum;
+    read(tid * kPer + j, c[j], sum);
+    m[j] = mass_of(sum, tid * kPer + j, a.unit);
     msum += m[j];
     csum += c[j];
   }
@@ -266,7 +341,7 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, int row, const Ro
   }
   e.mb = -1;
   if (r.min_p > 0.f && r.min_p <= 1.f) {
-    e.mb = bin_of(-log2((double)r.min_p));
+    e.mb = place_of(-log2((double)r.min_p)).bin;
     if (e.mb == kBins - 1) e.mb = -1;
   }
   int end0 = e.kb, end1 = e.kb;
@@ -278,6 +353,11 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, int row, const Ro
     end0 = min(end0, e.mb);
     end1 = min(end1, e.mb);
   }
+  // what lies past the end decides nothing
+  if (e.p0 > end1) e.p0 = e.p1 = -1;
+  e.p1 = min(e.p1, end1);
+  if (e.mb > end1) e.mb = -1;
+  if (e.kb > end1 && e.p0 < 0) e.cut = false;
   const double t0 = (double)r.u * (double)s.mass[end0], t1 = (double)r.u * (double)s.mass[end1 + 1];
   search(3, [&](int b) { return (double)s.mass[b] > t0; });
   search(4, [&](int b) { return (double)s.mass[b] > t1; });
@@ -298,31 +378,6 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, int row, const Ro
   return e;
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs a) {
-  __shared__ Prefix s;
-  __shared__ uint64_t part[kThreads / 64];
-  const int row = blockIdx.x / a.nchunk, chunk = blockIdx.x % a.nchunk;
-  const Row r = row_of(a, row);
-  if (r.bad || r.greedy) return;
-  const uint64_t top = row_top<kThreads>(a, row, part);
-  if (no_token(r, top)) return;
-  uint32_t wanted;
-  const Ends e = find_ends<kThreads>(a, row, r, s, wanted);
-  if (wanted > (uint32_t)kSampleList) return;
-  const double zmax = (double)key_value(top);
-  const auto* z = reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
-  const int from = chunk * kSampleChunk, to = min(a.vocab, from + kSampleChunk);
-  each8<T, kThreads>(z, from, to, [&](const float(&v)[8], int i, int n) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j >= n || !e.wanted(bin_of(depth(zmax, v[j], r.inv)))) continue;
-      const uint32_t at = atomicAdd(&row_count(a, row)[kBins], 1u);
-      if (at < (uint32_t)kSampleList) row_list(a, row)[at] = make_key(v[j], i + j);
-    }
-  });
-}
-
 // A search over all of a row's logits, a digit of the keys at a time: the first
 // element, in descending order, with which the count or the mass of the elements
 // so far is past a target.
@@ -336,7 +391,7 @@ struct Digits {
   uint32_t digit;
 };
 template <class T, class F>
-__device__ Found search_row(const SampleArgs& a, const typename T::raw* z, double zmax, const Row& r, Digits& s, F past) {
+__device__ __forceinline__ Found search_row(const SampleArgs& a, const typename T::raw* z, double zmax, const Row& r, Digits& s, F past) {
   uint64_t prefix = 0, mass = 0, count = 0;
   // (bits 24-31, of the index's complement, are ones: V <= 2^24)
   for (int shift = 56; shift >= 0; shift -= 8) {
@@ -349,48 +404,34 @@ __device__ Found search_row(const SampleArgs& a, const typename T::raw* z, doubl
       s.count[threadIdx.x] = 0;
     }
     __syncthreads();
-    for (int base = 0; base < a.vocab; base += 8 * kFinishThreads) {  // (every lane stays: waves add up together)
-      const int i = base + 8 * (int)threadIdx.x, n = min(8, a.vocab - i);
-      float v[8];
-      load8<T>(z + i, n, v);
-      uint32_t digit[8], first = 256, own = 0;
-      uint64_t w[8], sum = 0;
-      bool same = true;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint64_t key = make_key(v[j], i + j);
-        const bool in = j < n && (shift == 56 || (key >> (shift + 8)) == prefix);
-        digit[j] = in ? (uint32_t)(key >> shift) & 255u : 256u;
-        w[j] = in ? weight_of(depth(zmax, v[j], r.inv), a.unit) : 0;
-        if (!in) continue;
-        first = first == 256 ? digit[j] : first;
-        same &= digit[j] == first;
-        ++own;
-        sum += w[j];
-      }
-      const uint64_t some = __builtin_amdgcn_ballot_w64(own != 0);
+#pragma unroll 1
+    for (int base = 0; base < a.vocab; base += kRowThreads) {  // (every lane stays: waves add up together)
+      const int i = base + (int)threadIdx.x;
+      const float value = i < a.vocab ? T::value(z[i]) : -__builtin_inff();
+      const uint64_t key = make_key(value, i);
+      const bool in = i < a.vocab && (shift == 56 || (key >> (shift + 8)) == prefix);
+      const uint64_t some = __builtin_amdgcn_ballot_w64(in);
       if (!some) continue;
-      const uint32_t common = (uint32_t)__builtin_amdgcn_readlane((int)first, __builtin_ctzll(some));
-      if (__builtin_amdgcn_ballot_w64(own != 0 && !(same && first == common)) == 0) {
-        const uint64_t all = wave_sum64(sum), count_all = wave_sum64(own);
+      const Place p = place_of(depth(zmax, value, r.inv));
+      const uint64_t w = in ? mass_of(p.m, p.bin, a.unit) : 0;
+      const uint32_t digit = (uint32_t)(key >> shift) & 255u;
+      const uint32_t common = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(some));
+      if (__builtin_amdgcn_ballot_w64(in && digit != common) == 0) {
+        const uint64_t all = wave_sum64(w);
         if ((threadIdx.x & 63) == 0) {
-          atomicAdd(&s.count[common], (uint32_t)count_all);
+          atomicAdd(&s.count[common], (uint32_t)__builtin_popcountll(some));
           atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[common]), (unsigned long long)all);
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (digit[j] == 256) continue;
-          atomicAdd(&s.count[digit[j]], 1u);
-          atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[digit[j]]), (unsigned long long)w[j]);
-        }
+      } else if (in) {
+        atomicAdd(&s.count[digit], 1u);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[digit]), (unsigned long long)w);
       }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
       int d = 255;
       for (; d > 0; --d) {
-        if (past(count + s.count[d], mass + s.mass[d])) break;
+        if (past((uint32_t)count + s.count[d], mass + s.mass[d])) break;
         count += s.count[d];
         mass += s.mass[d];
       }
@@ -408,156 +449,373 @@ __device__ Found search_row(const SampleArgs& a, const typename T::raw* z, doubl
   return {prefix, mass};
 }
 
+// Logits that hold those of the bins b0 .. b1, a hundredth of a bin wider, and
+// a step of fp32 at either end.  step: logits per bin.
+struct Range {
+  float lo, hi;
+  __device__ __forceinline__ bool has(float v) const { return v >= lo && v <= hi; }
+};
+__device__ __forceinline__ float step_from(float f, int by) {  // to the next float down (-1) or up (1)
+  const int i = __builtin_bit_cast(int, f);
+  if (f == 0.f) return __builtin_bit_cast(float, by < 0 ? (int)0x80000001 : 1);
+  if (not_finite(f)) return f;
+  return __builtin_bit_cast(float, i + (i < 0 ? -by : by));
+}
+__device__ __forceinline__ Range range_of(double zmax, double step, int b0, int b1) {
+  if (b1 < b0) return {__builtin_inff(), -__builtin_inff()};
+  return {step_from((float)(zmax - ((double)b1 + 1.01) * step), -1), step_from((float)(zmax - ((double)b0 - 0.01) * step), 1)};
+}
+
+constexpr int kListPer = kSampleList / kRowThreads;
+struct Select {
+  Prefix s;
+  union {
+    uint64_t bins[kBins];  // until the prefix sums are taken
+    uint2 list[kSampleList];  // logit, index
+    Digits digits;
+  };
+  uint64_t part[kRowThreads / 64];
+  uint64_t digit[3][256];  // of a search in the list: counts above bit kCount, sums of M below
+  uint64_t found[2];
+  uint32_t held;
+  float top[kRowThreads / 64];
+};
+
+__device__ __forceinline__ void put_token(const SampleArgs& a, int row, int token, float logprob) {
+  if (threadIdx.x != 0) return;
+  a.tokens[row] = token;
+  if (a.logprobs) a.logprobs[row] = logprob;
+}
+
+// Rows that need no search: no token, or the largest logit.  False for the others.
 template <class T>
-__global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleArgs a) {
-  constexpr int kPer = kSampleList / kFinishThreads;
-  __shared__ Prefix s;
-  __shared__ uint64_t list[kSampleList], part[kFinishThreads / 64], start_mass[kBins];
-  __shared__ uint32_t start[kBins];
-  __shared__ uint64_t got[4];  // masses: top-k, top-p, min-p; the token's key
-  __shared__ Digits digits;
-  const int row = blockIdx.x, tid = threadIdx.x;
-  const Row r = row_of(a, row);
-  const uint64_t top = row_top<kFinishThreads>(a, row, part);
-  const bool none = no_token(r, top);
-  if (none || r.greedy) {
-    if (tid == 0) {
-      a.tokens[row] = none ? -1 : (int)key_index(top);
-      if (a.logprobs) a.logprobs[row] = none ? __builtin_nanf("") : 0.f;
-    }
-    return;
+__device__ __forceinline__ bool simple_row(const SampleArgs& a, int row, const Row& r, float top, const float* groups, Select& m) {
+  if (no_token(r, top)) {
+    put_token(a, row, -1, __builtin_nanf(""));
+    return true;
   }
-  const double zmax = (double)key_value(top);
+  if (!r.greedy) return false;
+  if (threadIdx.x == 0) m.held = ~0u;
+  __syncthreads();
+  uint32_t first = ~0u;
+  for (int g = threadIdx.x >> 6; g < a.ngroup; g += kRowThreads / 64) {
+    if (groups[g] != top) continue;
+    for (int i = kGroup * g + (threadIdx.x & 63); i < min(a.vocab, kGroup * (g + 1)); i += 64)
+      if (T::value(row_logits<T>(a, row)[i]) == top) first = min(first, (uint32_t)i);
+  }
+  if (first != ~0u) atomicMin(&m.held, first);
+  __syncthreads();
+  put_token(a, row, (int)m.held, 0.f);
+  return true;
+}
+
+// The sum over the workgroup, in every thread.
+__device__ __forceinline__ uint64_t block_sum(uint64_t v, uint64_t* part) {
+  v = wave_sum64(v);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < kRowThreads / 64; ++w) v += part[w];
+  __syncthreads();
+  return v;
+}
+
+// The list's element that a thread holds: its key in as few bits as its type
+// and the vocabulary need (value above index_bits, the index's complement below).
+struct Held {
+  uint64_t key;
+  int bin;      // -1: none, or not of a wanted bin
+  uint32_t m;
+  bool near;    // min-p keeps it
+};
+template <class T>
+__device__ __forceinline__ uint64_t short_key(uint32_t order, uint32_t index, int index_bits) {
+  return ((uint64_t)(order >> T::kZeroBits) << index_bits) | (~index & ((1u << index_bits) - 1u));
+}
+
+// In the list's elements of one bin, in descending order, the first with which
+// past(their count, their sum of M) holds; mass: the M up to and with it.  range:
+// of the bin's logits, whose keys share the bits above the first digit; alone:
+// the bin has one element.  digits
+// all zero on entry and exit; one barrier a digit: a digit's counts go to one of
+// three arrays, the next one's is cleared meanwhile.
+template <class T, class F>
+__device__ __forceinline__ Found search_bin(const Held (&c)[kListPer], int bin, const Range& range, int index_bits,
+                                            bool alone, uint64_t (&digits)[3][256], uint64_t (&found)[2], F past) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (alone) {  // whoever holds it says so
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j)
+      if (c[j].bin == bin) {
+        found[0] = c[j].key;
+        found[1] = c[j].m;
+      }
+    __syncthreads();
+    const Found f = {found[0], found[1]};
+    __syncthreads();
+    return f;
+  }
+  const uint64_t hi = short_key<T>(order_bits(range.hi), 0u, index_bits), lo = short_key<T>(order_bits(range.lo), ~0u, index_bits);
+  int top = hi == lo ? 1 : 64 - __builtin_clzll(hi ^ lo);  // bits that may differ
+  uint64_t prefix = hi >> top, before = 0;                 // before: count and sum above the prefix
+  for (int turn = 0;; turn = turn == 2 ? 0 : turn + 1) {
+    const int width = min(8, top), shift = top - width;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j)
+      if (c[j].bin == bin && (c[j].key >> top) == prefix)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&digits[turn][(c[j].key >> shift) & ((1u << width) - 1u)]),
+                  (1ull << kCount) | c[j].m);
+    if (tid < 256) digits[turn == 2 ? 0 : turn + 1][tid] = 0;
+    __syncthreads();
+    // lane l: digits 255 - 4 l down to 252 - 4 l
+    uint64_t own[4], sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      own[j] = digits[turn][255 - 4 * lane - j];
+      sum += own[j];
+    }
+    uint64_t upto = before + wave_scan64(sum) - sum, at = 0, in = 0;
+    uint32_t digit = 256;
+    // (rounding may have moved the target past the end: then the last element)
+    uint64_t last_at = 0, last_in = 0;
+    uint32_t last = 256;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t next = upto + own[j];
+      if (own[j] != 0) {
+        last = 255 - 4 * lane - j;
+        last_at = upto;
+        last_in = own[j];
+        if (digit == 256 && past((uint32_t)(next >> kCount), next & kSum)) {
+          digit = last;
+          at = upto;
+          in = own[j];
+        }
+      }
+      upto = next;
+    }
+    const uint64_t who = __builtin_amdgcn_ballot_w64(digit != 256), some = __builtin_amdgcn_ballot_w64(last != 256);
+    const int w = who ? __builtin_ctzll(who) : some ? 63 - __builtin_clzll(some) : 0;
+    before = lane64(who ? at : last_at, w);
+    in = lane64(who ? in : last_in, w);
+    prefix = (prefix << width) | (uint32_t)__builtin_amdgcn_readlane((int)(who ? digit : last), w);
+    top = shift;
+    if (top > 0 && in >> kCount > 1) continue;
+    // the one element left: whoever holds it says so
+    __syncthreads();  // (every wave has read the digits)
+    if (tid < 256) digits[0][tid] = digits[1][tid] = digits[2][tid] = 0;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j)
+      if (c[j].bin == bin && (c[j].key >> top) == prefix) found[0] = c[j].key;
+    __syncthreads();
+    const uint64_t key = found[0];
+    return {key, (before + in) & kSum};
+  }
+}
+
+// The row's token once its bins' prefix sums and ends are known.  groups: the
+// largest logit of every kGroup ones.
+template <class T>
+__device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& r, float top, const float* groups,
+                                       const Ends& e, uint32_t wanted, Select& m) {
+  Prefix& s = m.s;
+  const int tid = threadIdx.x;
+  const double zmax = (double)top;
   const double most = r.min_p > 0.f ? -log2((double)fminf(r.min_p, 1.f)) : 0.0;  // largest depth that min-p keeps
-  uint32_t wanted;
-  const Ends e = find_ends<kFinishThreads>(a, row, r, s, wanted);
-  uint64_t total, token;
-  if (wanted <= (uint32_t)kSampleList) {
-    const int n = (int)wanted;
-    int size = 64;
-    while (size < n) size *= 2;
-    for (int i = tid; i < size; i += kFinishThreads) list[i] = i < n ? row_list(a, row)[i] : 0;
-    if (tid == 0) {
-      got[0] = s.mass[e.kb + 1];
-      got[1] = ~0ull;
-      got[2] = e.mb >= 0 ? s.mass[e.mb] : ~0ull;
-      got[3] = top;
-    }
-    // descending order
-    for (int k = 2; k <= size; k *= 2)
-      for (int j = k / 2; j > 0; j /= 2) {
-        __syncthreads();
-        for (int t = tid; t < size / 2; t += kFinishThreads) {
-          const int i = 2 * t - (t & (j - 1)), o = i + j;
-          const uint64_t x = list[i], y = list[o];
-          if ((x < y) == ((i & k) == 0)) {
-            list[i] = y;
-            list[o] = x;
+  const auto* z = row_logits<T>(a, row);
+  const double step = 1.0 / (kPerOctave * r.inv);
+  bool listed = wanted <= (uint32_t)kSampleList;
+  const int index_bits = 32 - __builtin_clz((uint32_t)a.vocab);
+  Held c[kListPer];
+#pragma unroll
+  for (int j = 0; j < kListPer; ++j) c[j] = {0, -1, 0, false};
+  if (listed) {
+    if (tid == 0) m.held = 0;
+    if (tid < 256) m.digit[0][tid] = m.digit[1][tid] = m.digit[2][tid] = 0;
+    __syncthreads();
+    // the filters' bins, and the token's
+    int b0 = kBins, b1 = -1;
+    for (int b : {e.cut ? e.kb : -1, e.p0, e.p1, e.mb})
+      if (b >= 0) {
+        b0 = min(b0, b);
+        b1 = max(b1, b);
+      }
+    const Range x = range_of(zmax, step, e.u0, e.u1), y = range_of(zmax, step, b0, b1);
+    const float least = fminf(x.lo, y.lo);
+    const int wv = tid >> 6, lane = tid & 63, bulk = a.vocab & ~7;
+    auto put = [&](float value, int i) {
+      const uint32_t slot = atomicAdd(&m.held, 1u);
+      if (slot < (uint32_t)kSampleList) m.list[slot] = make_uint2(__builtin_bit_cast(uint32_t, value), (uint32_t)i);
+    };
+    for (int g0 = 0; bulk > 0 && g0 < a.ngroup; g0 += kRowThreads) {
+      // groups g0 + 16 l + wv that reach the wanted bins
+      const int own = g0 + (kRowThreads / 64) * lane + wv;
+      uint64_t left = __builtin_amdgcn_ballot_w64(own < a.ngroup && groups[min(own, a.ngroup - 1)] >= least);
+      int group[kAhead];  // -1: none left
+      raw8_t<T> v[kAhead];
+      auto next = [&](int u) {
+        group[u] = left ? g0 + (kRowThreads / 64) * __builtin_ctzll(left) + wv : -1;
+        left &= left - 1;
+        v[u] = load_below<T>(z, kGroup * max(group[u], 0) + 8 * lane, bulk);
+      };
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) next(u);
+      while (group[0] >= 0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (group[u] < 0) break;
+          const int at = kGroup * group[u] + 8 * lane;
+          uint32_t hits = 0;  // (no branch per logit)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float value = T::value(v[u][j]);
+            hits |= x.has(value) | y.has(value) ? 1u << j : 0u;
           }
+          hits = at < bulk ? hits : 0u;
+#pragma unroll 1
+          while (hits) {
+            const int j = __builtin_ctz(hits);
+            hits &= hits - 1;
+            float value = T::value(v[u][0]);
+#pragma unroll
+            for (int o = 1; o < 8; ++o) value = j == o ? T::value(v[u][o]) : value;
+            put(value, at + j);
+          }
+          next(u);
         }
       }
-    __syncthreads();
-    // count and mass up to and with every element: its bin's start plus the
-    // list's own prefix sums
-    uint64_t w[kPer], sum = 0;
-    int b[kPer];
-    double d[kPer];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = tid * kPer + j;
-      d[j] = i < n ? depth(zmax, key_value(list[i]), r.inv) : 0.0;
-      b[j] = bin_of(d[j]);
-      w[j] = i < n ? weight_of(d[j], a.unit) : 0;
-      sum += w[j];
     }
-    const uint64_t upto = wave_scan64(sum);
-    if ((tid & 63) == 63) part[tid >> 6] = upto;
-    __syncthreads();
-    uint64_t before = upto - sum;
-    for (int v = 0; v < (tid >> 6); ++v) before += part[v];
-    uint64_t p = before;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = tid * kPer + j;
-      if (i < n && (i == 0 || bin_of(depth(zmax, key_value(list[i - 1]), r.inv)) != b[j])) {
-        start[b[j]] = (uint32_t)i;
-        start_mass[b[j]] = p;
-      }
-      p += w[j];
+    if (bulk + tid < a.vocab) {
+      const float value = T::value(z[bulk + tid]);
+      if (x.has(value) || y.has(value)) put(value, bulk + tid);
     }
     __syncthreads();
-    uint64_t m[kPer];
-    p = before;
+    // a range of bins may hold others between the wanted ones: more than the list takes
+    listed = m.held <= (uint32_t)kSampleList;
+    const int n = (int)min(m.held, (uint32_t)kSampleList);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = tid * kPer + j;
-      p += w[j];
-      if (i >= n) continue;
-      m[j] = s.mass[b[j]] + p - start_mass[b[j]];
-      if (e.cut && b[j] == e.kb && s.count[b[j]] + i - start[b[j]] + 1 == r.k) got[0] = m[j];
-      if (b[j] == e.mb && d[j] <= most) atomicMax(reinterpret_cast<unsigned long long*>(&got[2]), (unsigned long long)m[j]);
+    for (int j = 0; j < kListPer; ++j) {
+      const int i = kRowThreads * j + tid;
+      if (kRowThreads * j >= n) continue;
+      const uint2 x = i < n ? m.list[i] : make_uint2(0, 0);
+      const float value = __builtin_bit_cast(float, x.x);
+      const double d = depth(zmax, value, r.inv);
+      const Place p = place_of(d);
+      c[j].key = short_key<T>(order_bits(value + 0.f), x.y, index_bits);
+      c[j].bin = i < n && e.wanted(p.bin) ? p.bin : -1;
+      c[j].m = p.m;
+      c[j].near = d <= most;
     }
     __syncthreads();
-    if (e.p0 >= 0) {
-      const double t = fmax((double)r.top_p * (double)got[0], 1.0);
+  }
+  // one search after the other: top-k, top-p, (min-p), the token; in the list,
+  // in the bin that the target lies in, or over the whole row
+  uint64_t total = s.mass[e.kb + 1], kept = ~0ull, token = 0;
+#pragma unroll 1
+  for (int turn = e.cut ? 0 : e.p0 >= 0 ? 1 : 2; turn < 3; ++turn) {
+    if (turn == 1 && e.p0 < 0) continue;
+    if (turn == 2) {
+      if (e.mb >= 0) {
+        uint64_t sum = 0;
+        if (listed) {
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (tid * kPer + j < n && (double)(m[j] - w[j]) < t && (double)m[j] >= t) got[1] = m[j];
-      __syncthreads();
-    }
-    total = min(min(got[0], got[1]), got[2]);
-    const double t = (double)r.u * (double)total;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (tid * kPer + j < n && (double)(m[j] - w[j]) <= t && (double)m[j] > t) got[3] = list[tid * kPer + j];
-    __syncthreads();
-    token = got[3];
-  } else {
-    const auto* z = reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
-    total = s.mass[e.kb + 1];
-    if (e.cut) total = search_row<T>(a, z, zmax, r, digits, [&](uint64_t c, uint64_t) { return c >= r.k; }).mass;
-    uint64_t kept = total;
-    if (e.p0 >= 0) {
-      const double t = fmax((double)r.top_p * (double)total, 1.0);
-      kept = search_row<T>(a, z, zmax, r, digits, [&](uint64_t, uint64_t m) { return (double)m >= t; }).mass;
-    }
-    if (e.mb >= 0) {
-      uint64_t sum = 0;
-      each8<T, kFinishThreads>(z, 0, a.vocab, [&](const float(&v)[8], int, int n) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const double d = depth(zmax, v[j], r.inv);
-          if (j < n && d <= most) sum += weight_of(d, a.unit);
+          for (int j = 0; j < kListPer; ++j)
+            if (c[j].bin == e.mb && c[j].near) sum += c[j].m;
+          sum = mass_of(block_sum(sum, m.part), e.mb, a.unit) + s.mass[e.mb];
+        } else {
+          each<T, kRowThreads>(z, 0, a.vocab, [&](float value, int) {
+            const double d = depth(zmax, value, r.inv);
+            const Place p = place_of(d);
+            if (d <= most) sum += mass_of(p.m, p.bin, a.unit);
+          });
+          sum = block_sum(sum, m.part);
         }
+        kept = min(kept, sum);
+      }
+      total = min(total, kept);
+    }
+    const double t = turn == 1 ? fmax((double)r.top_p * (double)total, 1.0) : (double)r.u * (double)total;
+    auto past = [&](uint32_t count, uint64_t mass) {
+      return turn == 0 ? count >= r.k : turn == 1 ? (double)mass >= t : (double)mass > t;
+    };
+    Found f;
+    if (listed) {
+      int b = turn == 0 ? e.kb : turn == 1 ? e.p0 : e.u0;
+      const int last = turn == 0 ? e.kb : turn == 1 ? e.p1 : e.u1;
+      while (b < last && !past(s.count[b + 1], s.mass[b + 1])) ++b;
+      const uint64_t base = s.mass[b];
+      const uint32_t before = s.count[b];
+      const bool alone = s.count[b + 1] - before == 1;
+      f = search_bin<T>(c, b, range_of(zmax, step, b, b), index_bits, alone, m.digit, m.found, [&](uint32_t count, uint64_t sum) {
+        return past(before + count, base + mass_of(sum, b, a.unit));
       });
-      sum = wave_sum64(sum);
-      if ((tid & 63) == 0) part[tid >> 6] = sum;
-      __syncthreads();
-      sum = 0;
-      for (int v = 0; v < kFinishThreads / 64; ++v) sum += part[v];
-      kept = min(kept, sum);
-      __syncthreads();
+      f.mass = base + mass_of(f.mass, b, a.unit);
+    } else {
+      f = search_row<T>(a, z, zmax, r, m.digits, past);
     }
-    total = min(total, kept);
-    const double t = (double)r.u * (double)total;
-    token = search_row<T>(a, z, zmax, r, digits, [&](uint64_t, uint64_t m) { return (double)m > t; }).key;
+    if (turn == 0) total = f.mass;
+    if (turn == 1) kept = f.mass;
+    token = f.key;
   }
-  if (tid == 0) {
-    a.tokens[row] = (int)key_index(token);
-    // log of the weight over the kept total, both relative to the largest weight
-    if (a.logprobs)
-      a.logprobs[row] = (float)(-0.6931471805599453 * depth(zmax, key_value(token), r.inv) - log(ldexp((double)total, -a.unit)));
+  if (listed) {
+    // back to a whole key (the dropped bits of a negative value's are ones)
+    const uint32_t order = (uint32_t)(token >> index_bits) << T::kZeroBits;
+    token = ((uint64_t)(order & 0x80000000u ? order : order | ((1u << T::kZeroBits) - 1u)) << 32) |
+            (uint32_t)(token | (~0u << index_bits));
   }
+  // log of the weight over the kept total, both relative to the largest weight
+  put_token(a, row, (int)key_index(token),
+            (float)(-0.6931471805599453 * depth(zmax, key_value(token), r.inv) - log(ldexp((double)total, -a.unit))));
+}
+
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a) {
+  __shared__ Select m;
+  const int row = blockIdx.x;
+  const Row r = row_of(a, row);
+  const float top = join_top<kRowThreads>(a, row, m.top);
+  if (simple_row<T>(a, row, r, top, row_groups(a, row), m)) return;
+  uint32_t wanted;
+  const bool wide = a.vocab > kSampleNarrow;
+  const Ends e = find_ends(a, r, m.s, wanted, [&](int b, uint32_t& count, uint64_t& sum) {
+    const uint64_t x = row_bins(a, row)[b];
+    count = wide ? row_count(a, row)[b] : (uint32_t)(x >> kCount);
+    sum = wide ? x : x & kSum;
+  });
+  select<T>(a, row, r, top, row_groups(a, row), e, wanted, m);
+}
+
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
+  __shared__ Select m;
+  __shared__ float groups[kSampleNarrow / kGroup];
+  const int row = blockIdx.x;
+  const Row r = row_of(a, row);
+  for (int b = threadIdx.x; b < kBins; b += kRowThreads) m.bins[b] = 0;
+  const float top = top_of<T, kRowThreads>(row_logits<T>(a, row), 0, a.vocab, groups, m.top);
+  if (simple_row<T>(a, row, r, top, groups, m)) return;
+  count_bins<T, kRowThreads>(row_logits<T>(a, row), 0, a.vocab, (double)top, r.inv, m.bins);
+  __syncthreads();
+  uint32_t wanted;
+  const Ends e = find_ends(a, r, m.s, wanted, [&](int b, uint32_t& count, uint64_t& sum) {
+    count = (uint32_t)(m.bins[b] >> kCount);
+    sum = m.bins[b] & kSum;
+  });
+  select<T>(a, row, r, top, groups, e, wanted, m);
 }
 
 template <class T>
 int launch_type(const SampleArgs& a, void* stream) {
   const hipStream_t st = (hipStream_t)stream;
+  if (a.nchunk == 0) {
+    hipLaunchKernelGGL(sample_row_kernel<T>, dim3(a.batch), dim3(kRowThreads), 0, st, a);
+    return (int)hipGetLastError();
+  }
   const dim3 chunks(a.batch * a.nchunk);
   hipLaunchKernelGGL(sample_max_kernel<T>, chunks, dim3(kThreads), 0, st, a);
   hipLaunchKernelGGL(sample_bins_kernel<T>, chunks, dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL(sample_gather_kernel<T>, chunks, dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL(sample_finish_kernel<T>, dim3(a.batch), dim3(kFinishThreads), 0, st, a);
+  hipLaunchKernelGGL(sample_finish_kernel<T>, dim3(a.batch), dim3(kRowThreads), 0, st, a);
   return (int)hipGetLastError();
 }
 

@@ -272,7 +272,8 @@ int launch_sample(const SampleArgs& a, int type, void*) {
   if (a.unit < 24 || ((double)a.vocab * (double)(1ull << a.unit)) > 9.2e18 || (a.unit + 1) * 40 >= kSampleBins) std::abort();
   for (int r = 0; r < a.batch; ++r) {
     rd(static_cast<const uint8_t*>(a.logits) + (size_t)r * a.row_stride * size, a.vocab * size);
-    wr(a.ws + (size_t)r * a.row_bytes, 8 * (size_t)(kSampleBins + kSampleList + a.nchunk) + 4 * (kSampleBins + 1));
+    wr(a.ws + (size_t)r * a.row_bytes, 12 * (size_t)kSampleBins + 4 * (size_t)(a.ngroup + a.nchunk));
+    if (a.ngroup * kSampleGroup < a.vocab || (a.nchunk && a.chunk % kSampleGroup != 0)) std::abort();
   }
   for (const void* p : {(const void*)a.temperature, (const void*)a.top_k, (const void*)a.top_p, (const void*)a.min_p, (const void*)a.uniform})
     if (p) rd(p, 4 * (size_t)a.batch);
