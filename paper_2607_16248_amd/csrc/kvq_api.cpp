@@ -296,6 +296,21 @@ uint64_t sample_row_bytes(int vocab) {
   return kvq::align_up(12 * kvq::kSampleBins + 4 * (ngroup + nchunk), kvq::kAlign);
 }
 
+// Whether loss and gradient of rows that fit a workgroup's registers come from one
+// pass over them, else from three launches that read them twice.  One pass for
+// short rows, whose three launches cost more than their work (rows of 32768: 64 fp32
+// 13.1 us and 19.9, 1024 57 and 69; bf16 256 16 and 19, 512 and 3000 alike), and for
+// more logits than stay in the 256 MiB cache beside their gradient (128256 bf16: 3000
+// rows 335 us and 438, 1024 127 and 157, 512, which are 131 MB, 68 and 69, 128 23 and
+// 24 but 64 30 and 19; 152064 f16 with 256 entries: 512, 156 MB, 98 and 83, 1024 175
+// and 197).  The loss alone reads them once either way, faster by chunks (3000 rows
+// of 128256 bf16 137 us and 191).
+bool distill_whole_rows(int type, int64_t rows, int64_t vocab) {
+  const bool f32 = type == DGAP_F32;
+  if (vocab < 8 || vocab > (f32 ? kvq::kDistillRow32 : kvq::kDistillRow16)) return false;
+  return vocab <= 32768 || rows * vocab * (f32 ? 4 : 2) > (int64_t)192 << 20;
+}
+
 kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* grad, int64_t grad_row_stride,
                         const float* grad_loss, bool need_grad) {
   if (!p) return fail(KVQ_ERR_ARG, "parameters are NULL");
@@ -312,7 +327,6 @@ kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* g
     return fail(KVQ_ERR_ARG, "grad must be aligned to its type");
   if (grad == p->logits && grad && grad_row_stride != p->row_stride)
     return fail(KVQ_ERR_ARG, "a gradient in the logits' place needs their row stride");
-  const double c = 1.4426950408889634 / (double)p->temperature;
   a.logits = p->logits;
   a.teacher = p->teacher;
   a.index = p->index;
@@ -322,9 +336,10 @@ kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* g
   a.grad_stride = grad_row_stride;
   a.rows = p->rows; a.vocab = p->vocab; a.k = p->k;
   a.nchunk = (p->vocab + kvq::kDistillChunk - 1) / kvq::kDistillChunk;
+  a.whole_rows = grad && !need_grad && distill_whole_rows(p->type, p->rows, p->vocab);
+  a.compute_units = (int32_t)target_workgroups(1);
   a.temperature = p->temperature;
-  a.c = (float)c;
-  a.c_low = (float)(c - (double)a.c);
+  a.c = (float)(1.4426950408889634 / (double)p->temperature);
   return KVQ_OK;
 }
 

@@ -283,6 +283,7 @@ struct SampleArgs {
 
 constexpr int kDistillChunk = 8192;  // logits per workgroup
 constexpr int kDistillMaxK = 256;    // teacher entries per row
+constexpr int kDistillRow16 = 20 * 8192, kDistillRow32 = 8 * 8192;  // longest rows in registers, 16- and 32-bit logits
 
 struct DistillArgs {
   const void* logits;
@@ -296,7 +297,9 @@ struct DistillArgs {
   float* row_sum;           // per row: the same m, and the sum's log2
   int64_t row_stride, grad_stride;
   int32_t rows, vocab, nchunk, k;
-  float temperature, c, c_low;  // c + c_low = log2(e) / T
+  int32_t whole_rows;       // rows in a workgroup's registers (loss and grad not null), on so many
+  int32_t compute_units;
+  float temperature, c;     // c = log2(e) / T
 };
 
 // ---------------------------------------------------------------- dequant

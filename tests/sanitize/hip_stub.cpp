@@ -283,6 +283,7 @@ int launch_sample(const SampleArgs& a, int type, void*) {
 }
 int launch_distill(const DistillArgs& a, int type, void*) {
   const size_t size = type == 0 ? 4 : 2;
+  if (a.whole_rows && (!a.grad || !a.loss || a.vocab < 8 || a.vocab > (type == 0 ? kDistillRow32 : kDistillRow16))) std::abort();
   rd(a.teacher, 4 * (size_t)a.rows * a.k);
   rd(a.index, 4 * (size_t)a.rows * a.k);
   if (a.grad_loss) rd(a.grad_loss, 4 * (size_t)a.rows);
