@@ -38,6 +38,7 @@ struct kvq_cache {
   std::vector<HeadLayout> lay;
   std::vector<int32_t> L, Lq;
   std::vector<uint8_t> matrix;  // 1: the kernels of decode_mfma.hip (else decode_exact.hip)
+  std::vector<uint8_t> window;  // 1: the many-row kernel serves its windowed queries
   std::vector<int> occupancy;    // resident decode workgroups per compute unit, per sequence's kernel
   int32_t split_tokens = 0;
   // paged layout: block table on the device (pm.table), page lists and the
@@ -348,8 +349,11 @@ kvq_status distill_args(kvq::DistillArgs& a, const dgap_distillation* p, void* g
 namespace kvq {
 int matrix_decode_occupancy(int bk, int bv, int gk, int gq) { return matrix_waves(bk, bv, gk / 32, gq); }
 
+bool window_rows_supported(int gq, int gk, int gv, uint64_t head_bytes) {
+  return matrix_heads(gq, gk) && gv >= 32 && head_bytes <= 0xFFFFFFFFull;
+}
 bool matrix_decode_supported(int bk, int bv, int gq, int gk, int gv, uint64_t head_bytes) {
-  return matrix_heads(gq, gk) && matrix_bits(bk, bv) && gv >= 32 && head_bytes <= 0xFFFFFFFFull;
+  return matrix_bits(bk, bv) && window_rows_supported(gq, gk, gv, head_bytes);
 }
 }  // namespace kvq
 
@@ -414,12 +418,12 @@ kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena,
   }
   c->L.assign(d->batch, 0);
   c->Lq.assign(d->batch, 0);
-  for (int i = 0; i < d->batch; ++i)
-    c->matrix.push_back(kvq::matrix_decode_supported(c->bk[i], c->bv[i], d->num_q_heads / d->num_kv_heads,
-                                                     d->key_group,
-                                                     d->value_group, c->paged ? packed_bytes : c->lay[i].stride)
-                            ? 1
-                            : 0);
+  for (int i = 0; i < d->batch; ++i) {
+    const int gq = d->num_q_heads / d->num_kv_heads;
+    const uint64_t head_bytes = c->paged ? packed_bytes : c->lay[i].stride;
+    c->matrix.push_back(kvq::matrix_decode_supported(c->bk[i], c->bv[i], gq, d->key_group, d->value_group, head_bytes) ? 1 : 0);
+    c->window.push_back(kvq::window_rows_supported(gq, d->key_group, d->value_group, head_bytes) ? 1 : 0);
+  }
   // the split plan of a launch fills one round of its kernel's workgroups
   for (int i = 0; i < d->batch; ++i)
     c->occupancy.push_back(c->matrix[i] ? kvq::matrix_decode_occupancy(c->bk[i], c->bv[i], d->key_group,
@@ -903,14 +907,15 @@ kvq_status run_merge(const kvq_cache* c, const SplitPlan& p, const void* ws, flo
 // (query, head) rows per kv head.  One sequence of four heads per kv head, 16-row
 // groups against many rows: windows of 512 tokens 128 rows 19 and 23 us, 256 rows
 // 19 and 20, 512 rows 27 and 22; windows of 4096 128 rows 29 and 32, 256 rows 40
-// and 28, 4096 rows 626 and 123 (K2V2; the other classes alike).
+// and 28, 4096 rows 626 and 123 (K2V2; the other classes alike, K2V4's 256 rows
+// 19 and 21, 43 and 29).
 constexpr int kWindowManyRows = 256;
 constexpr double kWindowBlockUs2 = 2.0;  // a block of 4- or 8-bit operands with the values' low halves
 
 // Whether a class's windowed queries go to the many-row kernel, which reads a
 // block once for 256 rows.
 bool window_many(const kvq_cache* c, int seq0, int nqry) {
-  return c->matrix[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyRows;
+  return c->window[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyRows;
 }
 
 // Rows of a class's windowed launch: one query's heads, 16 rows of whole

@@ -353,6 +353,8 @@ int launch_decode_matrix(const DecodeArgs& a, int bk, int bv, int gq, void* stre
 // (sequence, head) block that one buffer resource covers; decode_exact.hip
 // serves every other.
 bool matrix_decode_supported(int bk, int bv, int gq, int gk, int gv, uint64_t head_bytes);
+// Whether the many-row kernel serves windowed queries: any bit class, else as above.
+bool window_rows_supported(int gq, int gk, int gv, uint64_t head_bytes);
 // Waves per SIMD of that kernel for this bit class (2, 3 or 4); the others run
 // two.
 int matrix_decode_occupancy(int bk, int bv, int gk, int gq);

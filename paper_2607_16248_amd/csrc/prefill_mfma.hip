@@ -720,6 +720,16 @@ int launch_window_rows(const DecodeArgs& a, int bk, int bv, void* stream) {
 int launch_prefill(const DecodeArgs& a, int bk, int bv, void* stream) {
 #endif
   if (a.total_wg <= 0) return 0;
+#ifdef KVQ_WINDOW  // (without windows these classes' blocks stay with the exact kernel)
+  if (bk == 1 && bv == 4) return launch_pages<1, 4>(a, stream);
+  if (bk == 1 && bv == 8) return launch_pages<1, 8>(a, stream);
+  if (bk == 2 && bv == 4) return launch_pages<2, 4>(a, stream);
+  if (bk == 2 && bv == 8) return launch_pages<2, 8>(a, stream);
+  if (bk == 4 && bv == 1) return launch_pages<4, 1>(a, stream);
+  if (bk == 4 && bv == 2) return launch_pages<4, 2>(a, stream);
+  if (bk == 8 && bv == 1) return launch_pages<8, 1>(a, stream);
+  if (bk == 8 && bv == 2) return launch_pages<8, 2>(a, stream);
+#endif
   if (bk == 1 && bv == 1) return launch_pages<1, 1>(a, stream);
   if (bk == 1 && bv == 2) return launch_pages<1, 2>(a, stream);
   if (bk == 2 && bv == 1) return launch_pages<2, 1>(a, stream);

@@ -137,7 +137,8 @@ def test_window_matches_oracle(name, kw, n_q, window, sinks):
     assert (got.view(np.uint32) == again.view(np.uint32)).all()
 
 
-@pytest.mark.parametrize("bk,bv", [(1, 1), (1, 2), (2, 1), (2, 2), (4, 4), (4, 8), (8, 4), (8, 8), (1, 4), (8, 2), (2, 8), (4, 1)])
+@pytest.mark.parametrize("bk,bv", [(1, 1), (1, 2), (2, 1), (2, 2), (4, 4), (4, 8), (8, 4), (8, 8), (1, 4), (8, 2), (2, 8), (4, 1), (1, 8),
+                                   (8, 1), (4, 2), (2, 4)])
 def test_every_class(bk, bv):
     c = Setup((420, 77), bk, bv, R=3)
     q = c.queries(1)
@@ -156,6 +157,15 @@ def test_small_and_large_numbers(kw, bits):
     for n_q in (1, 6, 70):
         q = c.queries(n_q)
         c.check(q, run(c, q, 120, 4), 120, 4)
+
+
+@pytest.mark.parametrize("kw", [dict(vmul=2e-7), dict(vmul=5000.0), dict(kmul=1e-5), dict(vadd=3000.0)], ids=str)
+@pytest.mark.parametrize("bk,bv", [(1, 4), (2, 8), (4, 2), (8, 1)])
+def test_small_and_large_numbers_of_mixed_bits(kw, bk, bv):
+    # keys of one or two fp16 parts beside values of the other
+    c = Setup((330, 200), bk, bv, R=20, **kw)
+    q = c.queries(70)
+    c.check(q, run(c, q, 120, 4), 120, 4)
 
 
 def test_forced_splits_and_growing_cache():
