@@ -46,7 +46,7 @@ SOURCES = [
 ] + [("decode_mfma.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}", f"-DKVQ_BV={bv}"], f"decode_mfma_k{bk}v{bv}.o")
      for bk, bv in MATRIX_CLASSES] + [
     ("decode_exact.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}"], f"decode_exact_k{bk}.o") for bk in (1, 2, 4, 8)] + [
-    ("decode_exact.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}", "-DKVQ_WINDOW"], f"window_k{bk}.o") for bk in (1, 2, 4, 8)]
+    ("window.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}"], f"window_k{bk}.o") for bk in (1, 2, 4, 8)]
 
 
 def _compile(src, extra, verbose, obj_name=None):
@@ -67,7 +67,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     workers = min(len(SOURCES), max(2, os.cpu_count() or 2))
     # the long compiles first, so that they start at once
-    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip"))
+    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip", "window.hip"))
     with cf.ThreadPoolExecutor(max_workers=workers) as ex:
         done = dict(zip(order, ex.map(lambda i: _compile(SOURCES[i][0], SOURCES[i][1], verbose, SOURCES[i][2]),
                                       order)))

@@ -67,11 +67,21 @@ struct Work {
 
 // CHUNK = false: single-token decode (one query, one row group of the kv
 // head's GQ query heads), where the row arithmetic reduces to h * GQ + g.
-template <bool CHUNK>
+// AT_ONCE: a lane per sequence looks whether the workgroup is the sequence's or a
+// later one's (one load's latency, not one per sequence).
+template <bool CHUNK, bool AT_ONCE = false>
 __device__ __forceinline__ Work find_work(const DecodeArgs& a) {
   const int wg = blockIdx.x;
   int si = 0;
-  for (int i = 1; i < a.nseq; ++i) si = (a.seq[i].wg_begin <= wg) ? i : si;
+  if constexpr (AT_ONCE) {
+    static_assert(kMaxSeqPerLaunch <= 64, "one lane per sequence");
+    const int lane = threadIdx.x & 63;
+    const auto* args = (const DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();  // (indexed by lane, `a` would be copied)
+    const int begin = args->seq[min(lane, kMaxSeqPerLaunch - 1)].wg_begin;
+    si = __popcll(__builtin_amdgcn_ballot_w64(lane < a.nseq && begin <= wg)) - 1;
+  } else {
+    for (int i = 1; i < a.nseq; ++i) si = (a.seq[i].wg_begin <= wg) ? i : si;
+  }
   const int local = wg - a.seq[si].wg_begin;
   const int ns = a.seq[si].nsplit;
   const int hv = local / ns;

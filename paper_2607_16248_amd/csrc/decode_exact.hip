@@ -62,9 +62,7 @@ struct ValueMeta {
   u4_t s[FINE ? 8 : 4], zz, zs;
 };
 
-// WINDOW: windowed attention (every class; the splits count the key groups that
-// the row group's windows and the sinks touch).
-template <int BK, int BV, bool FINE, bool WINDOW>
+template <int BK, int BV, bool FINE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void decode_exact_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) Reduce<kPartRows> red;
   __shared__ float zsh[kWaves][16][17];  // value zero-point terms: [group][row]
@@ -101,7 +99,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   if (wk.sp >= S.nq) {  // fp16 tail tokens
     TailState<1> st;
-    tail_split<1, 16, true, 4, WINDOW>(a, S, wk.h, wk.rg, ring, st, lane, wv);
+    tail_split<1, 16, true>(a, S, wk.h, wk.rg, ring, st, lane, wv);
     for (int r0 = 0; r0 < rows; r0 += kPartRows) {
       __syncthreads();
       stage_tail<kPartRows, 1>(st, 0, r0, red, lane, wv);
@@ -130,28 +128,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int first_limit = seen0 + min(wk.rg * a.qpr, a.nqry - 1);
 
   const int ng = kHeadDim / a.gv, gsh = __builtin_ctz(a.gk), bsh = gsh - 5;
+  const int t0 = wk.sp * a.split_tokens, t1 = min(S.Lq, t0 + a.split_tokens);
   const int wslot = (wv + 2 * ((int)blockIdx.x >> 8)) & (kWaves - 1);
-  int j0, jend;
-  [[maybe_unused]] WindowGroups wg{};
-  [[maybe_unused]] int last_limit = 0;  // the last query's
-  if constexpr (WINDOW) {
-    last_limit = seen0 + min(wk.rg * a.qpr + a.qpr - 1, a.nqry - 1);
-    wg = window_groups(first_limit, last_limit, S.Lq, gsh, a.window, a.sinks);
-    const int gps = a.split_tokens >> gsh;
-    j0 = wk.sp * gps + wslot;
-    jend = min(wg.count, wk.sp * gps + gps);
-  } else {
-    const int t0 = wk.sp * a.split_tokens, t1 = min(S.Lq, t0 + a.split_tokens);
-    j0 = (t0 >> gsh) + wslot;
-    jend = t1 >> gsh;
-  }
+  const int j0 = (t0 >> gsh) + wslot, jend = t1 >> gsh;
   const int ngroups = j0 < jend ? (jend - j0 + kWaves - 1) / kWaves : 0;
   const int nblocks = ngroups << bsh;
-  auto token_of = [&](int i) {
-    int j = j0 + kWaves * (i >> bsh);
-    if constexpr (WINDOW) j += j < wg.sink ? 0 : wg.first - wg.sink;
-    return (j << gsh) + ((i & ((1 << bsh) - 1)) << 5);
-  };
+  auto token_of = [&](int i) { return ((j0 + kWaves * (i >> bsh)) << gsh) + ((i & ((1 << bsh) - 1)) << 5); };
 
   int vgl[FINE ? 8 : 4];  // byte offset of each scale row's 8 tokens
 #pragma unroll
@@ -269,13 +251,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       return t[0];
     };
     const int tok = token_of(i), left = lim - tok - 4 * blk;  // token 16mb + 4blk + r is visible below it
-    // windowed attention: and from `from` on, or below `sunk`
-    const int from = WINDOW ? max(lim - a.window, 0) - tok - 4 * blk : 0, sunk = WINDOW ? a.sinks - tok - 4 * blk : 0;
-    const bool masked = tok + 32 > first_limit || (WINDOW && tok < last_limit - a.window && tok + 32 > a.sinks);
-    auto seen = [&](int e) {
-      const int i = 16 * (e >> 2) + (e & 3);
-      return i < left && (!WINDOW || i >= from || i < sunk);
-    };
+    const bool masked = tok + 32 > first_limit;
     float s[8];
     if (LIFT && (any_half(cur.cs, 1u, kTinyScale) || any_half(cur.cz & 0x7FFF7FFFu, 1u, 0x0400u))) {
       // the small numbers lifted, apart from the others
@@ -332,7 +308,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
     if (masked) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = seen(e) ? s[e] : kNoScore;
+      for (int e = 0; e < 8; ++e) s[e] = 16 * (e >> 2) + (e & 3) < left ? s[e] : kNoScore;
     }
     float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     most = fmaxf(most, top);
@@ -355,8 +331,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int t = 0; t < 4; ++t) {
       float p0 = __builtin_amdgcn_exp2f(s[2 * t] - m), p1 = __builtin_amdgcn_exp2f(s[2 * t + 1] - m);
       if (masked) {
-        p0 = seen(2 * t) ? p0 : 0.f;
-        p1 = seen(2 * t + 1) ? p1 : 0.f;
+        p0 = 16 * (t >> 1) + ((2 * t) & 3) < left ? p0 : 0.f;
+        p1 = 16 * (t >> 1) + ((2 * t + 1) & 3) < left ? p1 : 0.f;
       }
       l += p0 + p1;
       const h2_t hi = {(_Float16)p0, (_Float16)p1};
@@ -485,22 +461,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 }
 
-#ifdef KVQ_WINDOW
-constexpr bool kWindow = true;
-#else
-constexpr bool kWindow = false;
-#endif
-
 template <int BK, int BV>
 int launch_fine(const DecodeArgs& a, void* stream) {
   if (a.gv < 32)
-    hipLaunchKernelGGL((decode_exact_kernel<BK, BV, true, kWindow>), dim3(a.total_wg), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((decode_exact_kernel<BK, BV, true>), dim3(a.total_wg), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
   else
-    hipLaunchKernelGGL((decode_exact_kernel<BK, BV, false, kWindow>), dim3(a.total_wg), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((decode_exact_kernel<BK, BV, false>), dim3(a.total_wg), dim3(64 * kWaves), 0, (hipStream_t)stream, a);
   return (int)hipGetLastError();
 }
 
-int launch_bits(const DecodeArgs& a, int bv, void* stream) {
+}  // namespace
+
+// This source is compiled once per key width (KVQ_BK, set by the build).
+template <>
+int launch_exact_class<KVQ_BK>(const DecodeArgs& a, int bv, void* stream) {
   switch (bv) {
     case 1: return launch_fine<KVQ_BK, 1>(a, stream);
     case 2: return launch_fine<KVQ_BK, 2>(a, stream);
@@ -509,21 +483,5 @@ int launch_bits(const DecodeArgs& a, int bv, void* stream) {
     default: return (int)hipErrorInvalidValue;
   }
 }
-
-}  // namespace
-
-// This source is compiled once per key width (KVQ_BK, set by the build), and
-// once more each for windowed attention (KVQ_WINDOW).
-#ifdef KVQ_WINDOW
-template <>
-int launch_window_class<KVQ_BK>(const DecodeArgs& a, int bv, void* stream) {
-  return launch_bits(a, bv, stream);
-}
-#else
-template <>
-int launch_exact_class<KVQ_BK>(const DecodeArgs& a, int bv, void* stream) {
-  return launch_bits(a, bv, stream);
-}
-#endif
 
 }  // namespace kvq

@@ -918,16 +918,16 @@ bool window_many(const kvq_cache* c, int seq0, int nqry) {
   return c->window[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyRows;
 }
 
-// Rows of a class's windowed launch: one query's heads, 16 rows of whole
-// queries, or row groups of 32 of the many-row kernel (the last group may
-// repeat the last query in its spare rows).
+// Rows of a class's windowed launch: one query's heads, a tile of 16 rows of whole
+// queries where they fit one, else row groups of 32 (the last group may repeat the
+// last query in its spare rows).
 Rows window_rows(const kvq_cache* c, int seq0, int nqry) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
   Rows r;
   r.nqry = nqry;
   r.many = window_many(c, seq0, nqry);
   r.rows = r.many ? 32 : 16;
-  r.qpr = nqry == 1 ? 1 : r.rows / gqh;
+  r.qpr = std::min(nqry, r.rows / gqh);
   r.nrg = (nqry + r.qpr - 1) / r.qpr;
   return r;
 }
@@ -952,18 +952,31 @@ int32_t window_reach(const kvq_cache* c, int i, const Rows& r, int32_t window, i
 
 // Most splits of a sequence in a windowed call, at any lengths.
 int64_t window_splits(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
-  const int64_t gk = c->d.key_group, qpr = 16 / (c->d.num_q_heads / c->d.num_kv_heads);
+  const int64_t gk = c->d.key_group, qpr = std::min(nqry, 32 / (c->d.num_q_heads / c->d.num_kv_heads));
   // a range of n tokens touches at most (n + gk - 2) / gk + 1 key groups
-  const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + (nqry > 1 ? qpr : 1) - 1 + gk - 2) / gk + 1);
+  const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + qpr - 1 + gk - 2) / gk + 1);
   const int64_t per = c->split_tokens > 0 ? c->split_tokens / gk : kMinGroupsPerSplit;
-  return std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
+  return std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, (reach + per - 1) / per));
 }
 
-// The split plan of a windowed call.  16-row groups: every class's splits take
-// the same number of key groups, as many as leave two workgroups per compute
-// unit (what the kernel's registers allow at once) and no fewer than one group
-// per wave.  Many rows: the splits with the smallest estimated time, as for
-// chunk queries.
+// Estimated time of a windowed launch of 16-row groups: workgroups, key blocks that a
+// wave of the longest takes, rows to merge.  A compute unit holds two workgroups,
+// but one already keeps its vector units near half busy, so each further one costs
+// 0.85 of the first.  Splits are joined by a launch of their own.  Against forced
+// splits (1 to 128 sequences of 8 kv heads, windows of 1024 to 16384 tokens, K2V2 to
+// K8V8) the plan is within 8% of the fastest: 64 windows of 1024 tokens, K4V4, 31 us
+// in one split each and 42 in two; 8 of 4096, K2V2, 23 in four, 26 in eight, 46 in
+// one; 32 of 8192, K8V8 of five heads, 130 in one, 146 in two, 155 in six.
+double window_us(int64_t wgs, int64_t blocks, int64_t merged_rows) {
+  const int64_t cus = target_workgroups(1), rounds = (wgs + cus - 1) / cus;
+  return 4.0 + (4.0 + 1.15 * (double)blocks) * (rounds > 1 ? 0.85 * (double)rounds : 1.0) +
+         (merged_rows > 0 ? 5.0 + 3e-3 * (double)merged_rows : 0.0);
+}
+
+// The split plan of a windowed call: the splits with the smallest estimated time,
+// every sequence's of the same number of key groups (16-row groups: no fewer than
+// one per wave; many rows: blocks, as for chunk queries).  The fp16 tail belongs to
+// a sequence's last split; a sequence of one split needs no merge.
 SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   SplitPlan p;
   p.nqry = nqry;
@@ -980,12 +993,10 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   for (auto& cl : classes) {
     const Rows r = window_rows(c, cl.second[0], nqry);
     const int64_t units = (int64_t)c->d.num_kv_heads * (r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg);
-    int64_t total = 0, tails = 0, longest = 0;
+    int64_t longest = 0;
     for (int i : cl.second) {
       p.nq[i] = window_reach(c, i, r, window, sinks);
-      total += p.nq[i] * units;
       longest = std::max<int64_t>(longest, p.nq[i]);
-      if (c->L[i] > c->Lq[i]) tails += units;
     }
     if (r.many) {
       const double block_us = cl.first.first + cl.first.second <= 4 ? kBlockUs : kWindowBlockUs2;
@@ -1012,21 +1023,37 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
       }
       continue;
     }
-    const int64_t round = target_workgroups(2), target = std::max(round - tails, round / 2);
     int64_t groups = c->split_tokens / gk;
-    if (groups == 0) groups = std::max<int64_t>((total + target - 1) / target, kMinGroupsPerSplit);
+    if (groups == 0) {
+      groups = kMinGroupsPerSplit;
+      double best = 0.0;
+      for (int64_t ns = 1; ns <= std::min<int64_t>(longest, 64); ++ns) {
+        const int64_t n = std::max<int64_t>((longest + ns - 1) / ns, kMinGroupsPerSplit);
+        int64_t wgs = 0, rows = 0;
+        for (int i : cl.second) {
+          const int64_t k = std::max<int64_t>(1, (p.nq[i] + n - 1) / n);
+          wgs += units * k;
+          rows += k > 1 ? (int64_t)nqry * c->d.num_q_heads : 0;
+        }
+        const double t = window_us(wgs, (n + kMinGroupsPerSplit - 1) / kMinGroupsPerSplit * (gk / 32), rows);
+        if (ns == 1 || t < best) best = t, groups = n;
+        if (n == kMinGroupsPerSplit) break;
+      }
+    }
     groups = std::max(groups, (longest + kMaxSplits - 1) / kMaxSplits);
     for (int i : cl.second) {
       p.st[i] = (int32_t)(groups * gk);
       p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
-      p.ns[i] = p.nq[i] + (c->L[i] > c->Lq[i] ? 1 : 0);
+      p.ns[i] = std::max(p.nq[i], 1);
+      p.direct[i] = p.ns[i] == 1;
+      p.required += p.direct[i];  // (a workspace is asked for whether or not the lengths leave it unused)
     }
   }
   for (int i = 0; i < B; ++i) {
     p.base[i] = (int32_t)p.records;
     p.records += p.direct[i] ? 0 : p.ns[i];
   }
-  p.required = p.records;
+  p.required += p.records;
   return p;
 }
 
@@ -1044,7 +1071,7 @@ kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int
     a.split_tokens = p.st[cls.second[0]];
     a.window = window;
     a.sinks = sinks;
-    if (r.many) a.out = out;
+    a.out = out;
     fill_seqs(a, c, cls.second, p, r);
     const int e = r.many ? kvq::launch_window_rows(a, cls.first.first, cls.first.second, stream)
                          : kvq::launch_window(a, cls.first.first, cls.first.second, stream);

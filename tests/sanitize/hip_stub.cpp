@@ -232,7 +232,7 @@ static void touch_window(const DecodeArgs& a, int bk, int bv, int step, bool man
     }
     for (int h = 0; h < a.hkv; ++h) ring_ranges(a, S.head0, h, S.Lq, S.L, rd);
     rd(a.q + (size_t)S.seq * rows * kHeadDim, rows * kTokenBytes);
-    if (many && S.nsplit == 1)
+    if (S.nsplit == 1)
       wr(a.out + (size_t)S.seq * rows * kHeadDim, rows * kHeadDim * 4);
     else
       wr(a.ws + (size_t)S.ws_base * rows * kRecFloats, S.nsplit * rows * kRecFloats * 4);
