@@ -956,7 +956,7 @@ int64_t window_splits(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   // a range of n tokens touches at most (n + gk - 2) / gk + 1 key groups
   const int64_t reach = std::min<int64_t>(c->cq / gk, (sinks + gk - 1) / gk + (window + qpr - 1 + gk - 2) / gk + 1);
   const int64_t per = c->split_tokens > 0 ? c->split_tokens / gk : kMinGroupsPerSplit;
-  return std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, (reach + per - 1) / per));
+  return std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
 }
 
 // Estimated time of a windowed launch of 16-row groups: workgroups, key blocks that a
@@ -975,8 +975,11 @@ double window_us(int64_t wgs, int64_t blocks, int64_t merged_rows) {
 
 // The split plan of a windowed call: the splits with the smallest estimated time,
 // every sequence's of the same number of key groups (16-row groups: no fewer than
-// one per wave; many rows: blocks, as for chunk queries).  The fp16 tail belongs to
-// a sequence's last split; a sequence of one split needs no merge.
+// one per wave; many rows: blocks, as for chunk queries).  The fp16 tail has a
+// workgroup of its own where a compute unit is idle and the splits are merged anyway
+// (one window of 1024 tokens, K2V2: the launch 8 us, 11 otherwise), else it belongs to
+// the last split (64 of them: 34 us, 58 otherwise); a sequence of one split needs no
+// merge.
 SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   SplitPlan p;
   p.nqry = nqry;
@@ -1041,10 +1044,16 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
       }
     }
     groups = std::max(groups, (longest + kMaxSplits - 1) / kMaxSplits);
+    int64_t wgs = 0, tails = 0;
+    for (int i : cl.second) {
+      p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
+      wgs += units * std::max(p.nq[i], 1);
+      if (p.nq[i] > 1 && c->L[i] > c->Lq[i]) tails += units;
+    }
+    const bool own_tails = wgs + tails <= target_workgroups(1);
     for (int i : cl.second) {
       p.st[i] = (int32_t)(groups * gk);
-      p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
-      p.ns[i] = std::max(p.nq[i], 1);
+      p.ns[i] = std::max(p.nq[i], 1) + (own_tails && p.nq[i] > 1 && c->L[i] > c->Lq[i] ? 1 : 0);
       p.direct[i] = p.ns[i] == 1;
       p.required += p.direct[i];  // (a workspace is asked for whether or not the lengths leave it unused)
     }

@@ -552,7 +552,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       const int g = (FINE ? 16 * t + 4 * blk + r : 16 * t) >> gvsh;
       st.acc[0][t][r] = fmaf(acc[t][r], unit, zsh[wv][g][col]) * to_max;
     }
-  if (S.L > S.Lq && wk.sp == S.nsplit - 1) {  // the last split's: the fp16 tail
+  if (S.L > S.Lq && wk.sp == S.nsplit - 1) {  // the fp16 tail: the last split's, or all of it
     TailState<1> tail;
     tail_split<1, 16, true, 4, true>(a, S, wk.h, wk.rg, ring, tail, lane, wv);
     const float top = fmaxf(st.m[0], tail.m[0]);  // (-inf in a wave that read nothing)

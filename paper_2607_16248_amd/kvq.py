@@ -244,14 +244,37 @@ def kvq_window_workspace_bytes(cache: int, n_q: int, window: int, sinks: int = 0
     return int(lib().kvq_window_workspace_bytes(cache, int(n_q), int(window), int(sinks)))
 
 
+def _on_device(stream, call, *tensors) -> None:
+    """call(stream) on the tensors' device: one of them all, which need not be the current one."""
+    device = None
+    for x in tensors:
+        if x is None or isinstance(x, int):
+            continue
+        at = x.get_device()
+        if at < 0:
+            raise ValueError("tensors must be on a GPU")
+        if device is not None and at != device:
+            raise ValueError("tensors are on different devices")
+        device = at
+    if device is None:  # (addresses only)
+        return call(_stream(stream))
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if device == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        call(_stream(stream))
+
+
 def kvq_window_attention(cache: int, q, n_q: int, window: int, sinks: int, out, ws, ws_bytes: Optional[int] = None,
                          stream=None) -> None:
     """The last n_q tokens of every sequence attend over the last ``window`` tokens up to their own and the first
     ``sinks`` ones: q fp16 [batch][n_q][Hq][d], out fp32 [batch][n_q][Hq][d]."""
     if ws_bytes is None:
         ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().kvq_window_attention(cache, _ptr(q), int(n_q), int(window), int(sinks), _ptr(out), _ptr(ws),
-                                      int(ws_bytes), _stream(stream)))
+    _on_device(stream, lambda st: _check(lib().kvq_window_attention(
+        cache, _ptr(q), int(n_q), int(window), int(sinks), _ptr(out), _ptr(ws), int(ws_bytes), st)), q, out, ws)
 
 
 def kvq_append_decode(cache: int, K, V, n_new: Sequence[int], q, out, ws, ws_bytes: Optional[int] = None,
@@ -506,8 +529,9 @@ def dgap_sample(logits, uniform, tokens, ws, temperature=None, top_k=None, top_p
                      _per_row("uniform", uniform, n, f32))
     if ws_bytes is None:
         ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().dgap_sample(ctypes.byref(p), _per_row("tokens", tokens, n, i32), _per_row("logprobs", logprobs, n, f32),
-                             _ptr(ws), int(ws_bytes), _stream(stream)))
+    out = _per_row("tokens", tokens, n, i32), _per_row("logprobs", logprobs, n, f32)
+    _on_device(stream, lambda st: _check(lib().dgap_sample(ctypes.byref(p), *out, _ptr(ws), int(ws_bytes), st)),
+               logits, uniform, tokens, ws, temperature, top_k, top_p, min_p, logprobs)
 
 
 def dgap_distill_workspace_bytes(rows: int, vocab: int) -> int:
@@ -538,15 +562,16 @@ def dgap_distill(logits, teacher, index, temperature: float, loss, ws, lse=None,
     n, f32 = p.rows, "torch.float32"
     if ws_bytes is None:
         ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().dgap_distill(ctypes.byref(p), _per_row("loss", loss, n, f32), _per_row("lse", lse, n, f32), _ptr(grad),
-                              grad_stride, _per_row("grad_loss", grad_loss, n, f32), _ptr(ws), int(ws_bytes),
-                              _stream(stream)))
+    out = _per_row("loss", loss, n, f32), _per_row("lse", lse, n, f32), _ptr(grad), grad_stride
+    scale = _per_row("grad_loss", grad_loss, n, f32)
+    _on_device(stream, lambda st: _check(lib().dgap_distill(ctypes.byref(p), *out, scale, _ptr(ws), int(ws_bytes), st)),
+               logits, teacher, index, loss, ws, lse, grad, grad_loss)
 
 
 def dgap_distill_backward(logits, teacher, index, temperature: float, lse, grad, grad_loss=None, stream=None) -> None:
     """The gradient alone, from the ``lse`` that dgap_distill wrote for these logits."""
     p, grad_stride = _distillation(logits, teacher, index, temperature, grad)
     n, f32 = p.rows, "torch.float32"
-    _check(lib().dgap_distill_backward(ctypes.byref(p), _per_row("lse", lse, n, f32),
-                                       _per_row("grad_loss", grad_loss, n, f32), _ptr(grad), grad_stride,
-                                       _stream(stream)))
+    args = _per_row("lse", lse, n, f32), _per_row("grad_loss", grad_loss, n, f32), _ptr(grad), grad_stride
+    _on_device(stream, lambda st: _check(lib().dgap_distill_backward(ctypes.byref(p), *args, st)),
+               logits, teacher, index, lse, grad, grad_loss)
