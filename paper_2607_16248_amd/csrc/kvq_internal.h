@@ -186,7 +186,9 @@ struct DecodeArgs {
   float* out;         // fp32 [batch][nqry][Hq][128]
   // windowed attention (launch_window): query position p sees token t <= p when
   // t > p - window or t < sinks; nq counts splits of split_tokens over the row
-  // group's visible key groups (WindowGroups).  window = 0 elsewhere.
+  // group's visible key groups (WindowGroups), nsplit one more where the fp16 tail has
+  // a workgroup of its own, else the last split adds it; a sequence of one split is
+  // written to out.  window = 0 elsewhere.
   int32_t window, sinks;
 };
 
@@ -373,7 +375,7 @@ int launch_matrix_class(const DecodeArgs& a, int gq, void* stream);
 template <int BK>
 int launch_exact_class(const DecodeArgs& a, int bv, void* stream);
 // Windowed attention (a.window > 0) of every class, 16 rows per workgroup, by
-// key bits (decode_exact.hip).
+// key bits (window.hip).
 int launch_window(const DecodeArgs& a, int bk, int bv, void* stream);
 // The same of many rows: kPrefillWaves row groups of 32 rows per workgroup; per
 // sequence, nq is the blocks per split of its workgroups' lists (prefill_mfma.hip).

@@ -1,6 +1,6 @@
 // Launch of the matrix-core decode kernels: the bit class picks the object
-// (decode_mfma.hip, compiled once per class; decode_exact.hip, once per key
-// width) whose kernels run.
+// (decode_mfma.hip, compiled once per class; decode_exact.hip and window.hip, once
+// per key width) whose kernels run.
 #include <hip/hip_runtime.h>
 
 #include "kvq_internal.h"
