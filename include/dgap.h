@@ -139,7 +139,7 @@ size_t dgap_sample_workspace_bytes(int32_t batch, int32_t vocab);
  * aligned, contents undefined on entry and exit; calls that may overlap take
  * one each.  Errors: KVQ_ERR_ARG (null pointers, shapes or type out of range,
  * misaligned logits or workspace), KVQ_ERR_CAPACITY (workspace too small),
- * KVQ_ERR_UNSUPPORTED (vocab above 2^24, more than 2^31 chunks of 8192 logits),
+ * KVQ_ERR_UNSUPPORTED (vocab above 2^24, 2^22 chunks of 8192 logits or more),
  * KVQ_ERR_HIP.  Results are bitwise reproducible. */
 kvq_status dgap_sample(const dgap_sampling* p, int32_t* tokens, float* logprobs, void* ws, size_t ws_bytes,
                        void* stream);
@@ -188,7 +188,7 @@ size_t dgap_distill_workspace_bytes(int32_t rows, int32_t vocab);
  * reproducible.  Errors: KVQ_ERR_ARG (null pointers, shapes, type or
  * temperature out of range, misaligned logits, grad or workspace),
  * KVQ_ERR_CAPACITY (workspace too small), KVQ_ERR_UNSUPPORTED (vocab above 2^24,
- * more than 2^31 chunks of 8192 logits), KVQ_ERR_HIP. */
+ * 2^22 chunks of 8192 logits or more), KVQ_ERR_HIP. */
 kvq_status dgap_distill(const dgap_distillation* p, float* loss, float* lse, void* grad, int64_t grad_row_stride,
                         const float* grad_loss, void* ws, size_t ws_bytes, void* stream);
 

@@ -271,7 +271,8 @@ kvq_status check_rows(const void* logits, int type, int64_t row_stride, int rows
   if (vocab < 1) return fail(KVQ_ERR_ARG, "vocab must be >= 1 (got %d)", vocab);
   if (vocab > 1 << 24) return fail(KVQ_ERR_UNSUPPORTED, "vocab %d above 2^24", vocab);
   if (row_stride < vocab) return fail(KVQ_ERR_ARG, "row_stride %lld smaller than vocab %d", (long long)row_stride, vocab);
-  if ((int64_t)rows * ((vocab + 8191) / 8192) > INT32_MAX)
+  // (a launch's threads, up to 1024 for 8192 logits, stay below 2^32)
+  if ((int64_t)rows * ((vocab + 8191) / 8192) >= (int64_t)1 << 22)
     return fail(KVQ_ERR_UNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
   const int size = type == DGAP_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(logits) % size != 0) return fail(KVQ_ERR_ARG, "logits must be aligned to their type");

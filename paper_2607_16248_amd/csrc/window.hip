@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const h2_t lift_s = {(_Float16)ldexpf(1.f, X), (_Float16)ldexpf(1.f, X)};
   const Fields<BK> fk;
   Fields<BV> fv;
-  if constexpr (BV == BK) fv = *reinterpret_cast<const Fields<BV>*>(&fk);
+  if constexpr (BV == BK) fv = fk;  // (one set of registers)
   // raw = alpha sum q z + beta sum q s + sum q K', score = ksc raw (q as held)
   constexpr float kAlpha = BK == 1 ? -2.f : 0.5f, kBeta = BK == 1 ? -1.f : Code<BK>::c0 * 0.5f;
   const float ksc = (BK == 1 ? 0.5f : 2.f) * a.qscale;

@@ -407,10 +407,14 @@ class KVCache:
     def window(self, q, window, sinks=0, out=None, stream=None):
         """Attention of the last q.shape[1] tokens over a sliding window and the first ``sinks`` tokens."""
         import torch
+        shape = (self.batch, q.shape[1], self.num_q_heads, self.head_dim)
+        if q.dtype != torch.float16 or q.shape != shape or not q.is_contiguous():
+            raise ValueError(f"q must be a contiguous float16 tensor of shape {shape}")
         n_q = int(q.shape[1])
         if out is None:
-            out = torch.empty((self.batch, n_q, self.num_q_heads, self.head_dim), dtype=torch.float32,
-                              device=q.device)
+            out = torch.empty(shape, dtype=torch.float32, device=q.device)
+        elif out.dtype != torch.float32 or out.shape != shape or not out.is_contiguous():
+            raise ValueError(f"out must be a contiguous float32 tensor of shape {shape}")
         need = kvq_window_workspace_bytes(self.handle, n_q, window, sinks)
         ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
         kvq_window_attention(self.handle, q, n_q, window, sinks, out, ws, stream=stream)

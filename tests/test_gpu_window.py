@@ -168,6 +168,22 @@ def test_small_and_large_numbers_of_mixed_bits(kw, bk, bv):
     c.check(q, run(c, q, 120, 4), 120, 4)
 
 
+@pytest.mark.parametrize("n,n_q", [(64, 1), (65, 1), (130, 1), (67, 4)])
+def test_more_sequences_than_a_launch_describes(n, n_q):
+    lens = [n_q + (37 * i) % 150 for i in range(n)]
+    c = Setup(tuple(lens), [(1, 2, 4, 8)[i % 4 if n == 130 else 1] for i in range(n)], 2, gq=1, R=33)
+    q = c.queries(n_q)
+    c.check(q, run(c, q, 60, 4), 60, 4)
+
+
+def test_few_queries_over_long_and_short_sequences():
+    # one sequence of many splits beside one of a single split, in and out of the tail's own workgroups
+    for lens, window in (((9000, 12), 8192), ((9000, 12, 40, 3000), 4096), ((20000,), 20000)):
+        c = Setup(lens, 2, 4, R=64)
+        q = c.queries(1)
+        c.check(q, run(c, q, window, 4), window, 4)
+
+
 def test_forced_splits_and_growing_cache():
     # every length around a key group's end, splits of one and of two groups
     c = Setup((60,), 2, 2, R=8, cap=200)

@@ -30,7 +30,7 @@ def sampling(**kw):
 
 @pytest.mark.parametrize("kw", [dict(logits=None), dict(uniform=None), dict(type=3), dict(type=-1), dict(batch=0), dict(batch=-4),
                                 dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(row_stride=999), dict(logits=FAKE + 2),
-                                dict(type=1, logits=FAKE + 1)], ids=str)
+                                dict(batch=1 << 22), dict(batch=1 << 11, vocab=1 << 24, row_stride=1 << 24), dict(type=1, logits=FAKE + 1)], ids=str)
 def test_sample_refuses(kw):
     p = sampling(**kw)
     refused(kvq.lib().dgap_sample(ctypes.byref(p), FAKE, None, FAKE, 1 << 40, None))
@@ -54,7 +54,7 @@ def distillation(**kw):
     return kvq.DgapDistillation(**p)
 
 
-BAD = [dict(logits=None), dict(teacher=None), dict(index=None), dict(type=3), dict(rows=0), dict(rows=-1), dict(vocab=0),
+BAD = [dict(rows=1 << 22), dict(rows=1 << 11, vocab=1 << 24, row_stride=1 << 24), dict(logits=None), dict(teacher=None), dict(index=None), dict(type=3), dict(rows=0), dict(rows=-1), dict(vocab=0),
        dict(vocab=(1 << 24) + 1), dict(k=0), dict(k=257), dict(row_stride=999), dict(temperature=0.0), dict(temperature=-1.0),
        dict(temperature=math.inf), dict(temperature=math.nan), dict(temperature=1e-45), dict(logits=FAKE + 2)]
 
@@ -97,6 +97,18 @@ def test_window_refuses():
     # enough for any lengths, and no more than a window of everything needs
     assert 0 < bytes_of(1, 1, 0) <= bytes_of(1, 64, 0) <= bytes_of(1, 64, 40) <= bytes_of(1, 1 << 30, 0) == bytes_of(1, 1 << 30, 1 << 30)
     kvq.kvq_cache_destroy(h)
+
+
+def test_window_binding_refuses_tensors():
+    c = object.__new__(kvq.KVCache)  # (the checks come before anything of a cache but its shape)
+    c.batch, c.num_q_heads, c.head_dim, c.handle = 2, 8, 128, None
+    q = torch.zeros((2, 1, 8, 128), dtype=torch.half)
+    for bad in (q.float(), q[:1], q[:, :, :4], q[..., :64], q.transpose(2, 3).contiguous().transpose(2, 3), torch.zeros((2, 8, 128)).half()):
+        with pytest.raises((ValueError, IndexError)):
+            c.window(bad, 8)
+    for bad in (q, q.float()[:, :, :4], q.float()[:1]):
+        with pytest.raises(ValueError):
+            c.window(q, 8, out=bad)
 
 
 def test_bindings_refuse_tensors():
