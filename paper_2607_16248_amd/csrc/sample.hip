@@ -276,20 +276,23 @@ struct Prefix {
   int found[6];
 };
 
-// read(bin): its count and sum of M
-template <class F>
-__device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Prefix& s, uint32_t& wanted, F read) {
-  constexpr int NT = kRowThreads, kPer = kBins / NT;
+// A thread's bins (kPer * tid on): their counts and sums of M.
+constexpr int kPer = kBins / kRowThreads;
+struct OwnBins {
+  uint32_t count[kPer];
+  uint64_t sum[kPer];
+};
+
+__device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Prefix& s, uint32_t& wanted, const OwnBins& own) {
+  constexpr int NT = kRowThreads;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   uint64_t m[kPer], msum = 0;
-  uint32_t c[kPer], csum = 0;
+  uint32_t csum = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    uint64_t sum;
-    read(tid * kPer + j, c[j], sum);
-    m[j] = mass_of(sum, tid * kPer + j, a.unit);
+    m[j] = mass_of(own.sum[j], tid * kPer + j, a.unit);
     msum += m[j];
-    csum += c[j];
+    csum += own.count[j];
   }
   const uint64_t mi = wave_scan64(msum), ci = wave_scan64(csum);
   if (lane == 63) {
@@ -298,33 +301,35 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Pre
   }
   if (tid < 6) s.found[tid] = -1;
   __syncthreads();
-  uint64_t mb = mi - msum, cb = ci - csum;
-  for (int w = 0; w < wv; ++w) {
-    mb += s.part[w][0];
-    cb += s.part[w][1];
+  uint64_t mass[kPer + 1], mb = mi - msum, cb = ci - csum;
+  uint32_t count[kPer + 1];
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    const uint64_t x = s.part[w][0], y = s.part[w][1];
+    mb += w < wv ? x : 0;
+    cb += w < wv ? y : 0;
   }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    s.mass[tid * kPer + j] = mb;
-    s.count[tid * kPer + j] = (uint32_t)cb;
+    s.mass[tid * kPer + j] = mass[j] = mb;
+    s.count[tid * kPer + j] = count[j] = (uint32_t)cb;
     mb += m[j];
-    cb += c[j];
+    cb += own.count[j];
   }
+  mass[kPer] = mb;
+  count[kPer] = (uint32_t)cb;
   if (tid == NT - 1) {
     s.mass[kBins] = mb;
     s.count[kBins] = (uint32_t)cb;
   }
-  __syncthreads();
-  // the bin in which a test becomes true (test(b): it holds once bins 0 .. b - 1 are in)
+  // the bin in which a test becomes true (of the count and mass before it, then with it)
   auto search = [&](int slot, auto test) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int b = tid * kPer + j;
-      if (!test(b) && test(b + 1)) s.found[slot] = b;
-    }
+    for (int j = 0; j < kPer; ++j)
+      if (!test(count[j], mass[j]) && test(count[j + 1], mass[j + 1])) s.found[slot] = tid * kPer + j;
   };
   Ends e;
-  search(0, [&](int b) { return s.count[b] >= r.k; });
+  search(0, [&](uint32_t n, uint64_t) { return n >= r.k; });
   __syncthreads();
   e.kb = s.found[0];
   // (the last bin has no mass: it is never cut)
@@ -333,8 +338,8 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Pre
   e.p0 = e.p1 = -1;
   if (r.top_p < 1.f) {
     const double t0 = fmax((double)r.top_p * lo, 1.0), t1 = fmax((double)r.top_p * hi, 1.0);
-    search(1, [&](int b) { return (double)s.mass[b] >= t0; });
-    search(2, [&](int b) { return (double)s.mass[b] >= t1; });
+    search(1, [&](uint32_t, uint64_t w) { return (double)w >= t0; });
+    search(2, [&](uint32_t, uint64_t w) { return (double)w >= t1; });
     __syncthreads();
     e.p0 = s.found[1];
     e.p1 = s.found[2];
@@ -359,22 +364,21 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Pre
   if (e.mb > end1) e.mb = -1;
   if (e.kb > end1 && e.p0 < 0) e.cut = false;
   const double t0 = (double)r.u * (double)s.mass[end0], t1 = (double)r.u * (double)s.mass[end1 + 1];
-  search(3, [&](int b) { return (double)s.mass[b] > t0; });
-  search(4, [&](int b) { return (double)s.mass[b] > t1; });
+  search(3, [&](uint32_t, uint64_t w) { return (double)w > t0; });
+  search(4, [&](uint32_t, uint64_t w) { return (double)w > t1; });
   __syncthreads();
   e.u0 = s.found[3];
   e.u1 = s.found[4];
-  uint32_t own = 0;
+  uint32_t held = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j)
-    if (e.wanted(tid * kPer + j)) own += c[j];
-  const uint64_t all = wave_sum64(own);
+    if (e.wanted(tid * kPer + j)) held += own.count[j];
+  const uint64_t all = wave_sum64(held);
   if (lane == 0) s.part[wv][0] = all;
   __syncthreads();
   wanted = 0;
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) wanted += (uint32_t)s.part[w][0];
-  __syncthreads();
   return e;
 }
 
@@ -614,11 +618,16 @@ __device__ __forceinline__ Found search_bin(const Held (&c)[kListPer], int bin, 
   }
 }
 
+// The group that a lane looks at, of those from g0 on.
+__device__ __forceinline__ int own_group(int g0) {
+  return g0 + (kRowThreads / 64) * (threadIdx.x & 63) + (threadIdx.x >> 6);
+}
+
 // The row's token once its bins' prefix sums and ends are known.  groups: the
-// largest logit of every kGroup ones.
+// largest logit of every kGroup ones; first: of own_group(0).
 template <class T>
 __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& r, float top, const float* groups,
-                                       const Ends& e, uint32_t wanted, Select& m) {
+                                       float first, const Ends& e, uint32_t wanted, Select& m) {
   Prefix& s = m.s;
   const int tid = threadIdx.x;
   const double zmax = (double)top;
@@ -650,8 +659,9 @@ __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& 
     };
     for (int g0 = 0; bulk > 0 && g0 < a.ngroup; g0 += kRowThreads) {
       // groups g0 + 16 l + wv that reach the wanted bins
-      const int own = g0 + (kRowThreads / 64) * lane + wv;
-      uint64_t left = __builtin_amdgcn_ballot_w64(own < a.ngroup && groups[min(own, a.ngroup - 1)] >= least);
+      const int own = own_group(g0);
+      if (g0 > 0) first = groups[min(own, a.ngroup - 1)];
+      uint64_t left = __builtin_amdgcn_ballot_w64(own < a.ngroup && first >= least);
       int group[kAhead];  // -1: none left
       raw8_t<T> v[kAhead];
       auto next = [&](int u) {
@@ -773,17 +783,24 @@ template <class T>
 __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a) {
   __shared__ Select m;
   const int row = blockIdx.x;
+  // what later steps read is under way from the start (greedy rows: contents undefined, unused)
+  const bool wide = a.vocab > kSampleNarrow;
+  const float* groups = row_groups(a, row);
+  const float first = groups[min(own_group(0), a.ngroup - 1)];
+  OwnBins own;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const uint64_t x = row_bins(a, row)[threadIdx.x * kPer + j];
+    const uint32_t n = row_count(a, row)[threadIdx.x * kPer + j];
+    own.count[j] = wide ? n : (uint32_t)(x >> kCount);
+    own.sum[j] = wide ? x : x & kSum;
+  }
   const Row r = row_of(a, row);
   const float top = join_top<kRowThreads>(a, row, m.top);
-  if (simple_row<T>(a, row, r, top, row_groups(a, row), m)) return;
+  if (simple_row<T>(a, row, r, top, groups, m)) return;
   uint32_t wanted;
-  const bool wide = a.vocab > kSampleNarrow;
-  const Ends e = find_ends(a, r, m.s, wanted, [&](int b, uint32_t& count, uint64_t& sum) {
-    const uint64_t x = row_bins(a, row)[b];
-    count = wide ? row_count(a, row)[b] : (uint32_t)(x >> kCount);
-    sum = wide ? x : x & kSum;
-  });
-  select<T>(a, row, r, top, row_groups(a, row), e, wanted, m);
+  const Ends e = find_ends(a, r, m.s, wanted, own);
+  select<T>(a, row, r, top, groups, first, e, wanted, m);
 }
 
 template <class T>
@@ -797,12 +814,16 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   if (simple_row<T>(a, row, r, top, groups, m)) return;
   count_bins<T, kRowThreads>(row_logits<T>(a, row), 0, a.vocab, (double)top, r.inv, m.bins);
   __syncthreads();
+  OwnBins own;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const uint64_t x = m.bins[threadIdx.x * kPer + j];
+    own.count[j] = (uint32_t)(x >> kCount);
+    own.sum[j] = x & kSum;
+  }
   uint32_t wanted;
-  const Ends e = find_ends(a, r, m.s, wanted, [&](int b, uint32_t& count, uint64_t& sum) {
-    count = (uint32_t)(m.bins[b] >> kCount);
-    sum = m.bins[b] & kSum;
-  });
-  select<T>(a, row, r, top, groups, e, wanted, m);
+  const Ends e = find_ends(a, r, m.s, wanted, own);
+  select<T>(a, row, r, top, groups, groups[min(own_group(0), a.ngroup - 1)], e, wanted, m);
 }
 
 template <class T>
