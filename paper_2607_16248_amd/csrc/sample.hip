@@ -26,14 +26,16 @@
 // chosen.  A row whose bins hold more elements than a list (thousands of equal
 // logits) is searched over all its logits, a digit of the keys at a time.
 //
-// What bounds it: latency, along one workgroup's dependent steps: of one row's 25
-// us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then ends 4, listing
-// 7 and the three searches 4, one step after the other at a few waves per SIMD.
-// Many rows: 256 flat ones of 128256 fp16 61 us, of which the bins are half (fp64
-// differences, an exponential and an LDS atomic per logit).  Each row is read once
-// from HBM (13 us of those 61).  Sorting the list took 5 to 22 us where the digit
-// searches take 4 to 8; straight-line code for every match of a load, run once
-// from a cold instruction cache, cost more than a loop.
+// What bounds it: latency, along one workgroup's dependent steps: of one row's 24
+// us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then the ends 3.5,
+// listing 6.6 (the compares, 60 instructions per 8 logits a lane at four waves per
+// SIMD: with every load asked for at once it takes as long) and the three searches 4,
+// one step after the other.  Many rows: 256 flat ones of 128256 fp16 61 us, of which
+// the bins are half: a 64-bit LDS atomic per logit (the differences without
+// conversions of 64-bit numbers, a third of the instructions: no faster).  Each row
+// is read once from HBM (13 us of those 61).  Sorting the list took 5 to 22 us where
+// the digit searches take 4 to 8; straight-line code for every match of a load, run
+// once from a cold instruction cache, cost more than a loop.
 #include <hip/hip_runtime.h>
 
 #include "decode_common.h"
