@@ -31,8 +31,9 @@
 // listing 6.6 (the compares, 60 instructions per 8 logits a lane at four waves per
 // SIMD: with every load asked for at once it takes as long) and the three searches 4,
 // one step after the other.  Many rows: 256 flat ones of 128256 fp16 61 us, of which
-// the bins are half: a 64-bit LDS atomic per logit (the differences without
-// conversions of 64-bit numbers, a third of the instructions: no faster).  Each row
+// 11 go to the first read and 21 to the bins, about twenty instructions a
+// logit (without their atomics, with all chains of a load side by side, or in fixed
+// point, 20 to 21); listing and searching 27.  Each row
 // is read once from HBM (13 us of those 61).  Sorting the list took 5 to 22 us where
 // the digit searches take 4 to 8; straight-line code for every match of a load, run
 // once from a cold instruction cache, cost more than a loop.
