@@ -26,17 +26,17 @@
 // chosen.  A row whose bins hold more elements than a list (thousands of equal
 // logits) is searched over all its logits, a digit of the keys at a time.
 //
-// What bounds it: latency, along one workgroup's dependent steps: of one row's 24
+// What bounds it: latency, along one workgroup's dependent steps: of one row's 23
 // us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then the ends 3.5,
-// listing 6.6 (the compares, 60 instructions per 8 logits a lane at four waves per
-// SIMD: with every load asked for at once it takes as long) and the three searches 4,
-// one step after the other.  Many rows: 256 flat ones of 128256 fp16 61 us, of which
-// 11 go to the first read and 21 to the bins, about twenty instructions a
-// logit (without their atomics, with all chains of a load side by side, or in fixed
-// point, 20 to 21); listing and searching 27.  Each row
-// is read once from HBM (13 us of those 61).  Sorting the list took 5 to 22 us where
-// the digit searches take 4 to 8; straight-line code for every match of a load, run
-// once from a cold instruction cache, cost more than a loop.
+// listing 6 (the compares, at four waves per SIMD: with every load asked for at
+// once it takes as long) and the three searches 4, one step after the other.  Many
+// rows: 256 flat ones of 128256 fp16 61 us, of which 11 go to the first read (all
+// that comes from HBM, 13 at a copy's rate), 21 to the bins, about twenty
+// instructions a logit (without their atomics, with the chains of a load side by
+// side, or in fixed point, 20 to 21), and 27 to listing and searching.  Sorting the
+// list took 5 to 22 us where the digit searches take 4 to 8; straight-line code for
+// every match of a load, run once from a cold instruction cache, cost more than a
+// loop.
 #include <hip/hip_runtime.h>
 
 #include "decode_common.h"
@@ -460,7 +460,8 @@ __device__ __forceinline__ Found search_row(const SampleArgs& a, const typename 
 // a step of fp32 at either end.  step: logits per bin.
 struct Range {
   float lo, hi;
-  __device__ __forceinline__ bool has(float v) const { return v >= lo && v <= hi; }
+  // (two instructions; none: +inf to +inf, which no listed logit is)
+  __device__ __forceinline__ bool has(float v) const { return __builtin_amdgcn_fmed3f(v, lo, hi) == v; }
 };
 __device__ __forceinline__ float step_from(float f, int by) {  // to the next float down (-1) or up (1)
   const int i = __builtin_bit_cast(int, f);
@@ -469,7 +470,7 @@ __device__ __forceinline__ float step_from(float f, int by) {  // to the next fl
   return __builtin_bit_cast(float, i + (i < 0 ? -by : by));
 }
 __device__ __forceinline__ Range range_of(double zmax, double step, int b0, int b1) {
-  if (b1 < b0) return {__builtin_inff(), -__builtin_inff()};
+  if (b1 < b0) return {__builtin_inff(), __builtin_inff()};
   return {step_from((float)(zmax - ((double)b1 + 1.01) * step), -1), step_from((float)(zmax - ((double)b0 - 0.01) * step), 1)};
 }
 
