@@ -664,6 +664,7 @@ Rows rows_for(const kvq_cache* c, bool matrix, int nqry, int bk, int bv) {
 struct SplitPlan {
   std::vector<int32_t> st, nq, ns, base;  // per sequence: split length, packed splits, all splits, first record
   std::vector<uint8_t> direct;            // per sequence: written by the split launch, not merged (empty: none)
+  std::vector<uint8_t> many;              // per sequence of a windowed call: on the many-row kernel
   int64_t records = 0;   // what the launches write
   int64_t required = 0;  // what the caller's workspace has to hold
   int nqry = 1;
@@ -905,29 +906,20 @@ kvq_status run_merge(const kvq_cache* c, const SplitPlan& p, const void* ws, flo
 
 // ------------------------------------------------------------ windowed attention
 
-// (query, head) rows per kv head.  One sequence of four heads per kv head, 16-row
-// groups against many rows: windows of 512 tokens 128 rows 19 and 23 us, 256 rows
-// 19 and 20, 512 rows 27 and 22; windows of 4096 128 rows 29 and 32, 256 rows 40
-// and 28, 4096 rows 626 and 123 (K2V2; the other classes alike, K2V4's 256 rows
-// 19 and 21, 43 and 29).
-constexpr int kWindowManyRows = 256;
-constexpr double kWindowBlockUs2 = 2.0;  // a block of 4- or 8-bit operands with the values' low halves
+// Fewest (query, head) rows per kv head for which the many-row kernel is considered
+// (its 256-row workgroup is then a quarter full; with fewer it never won).
+constexpr int kWindowManyFrom = 64;
+constexpr double kWindowBlockUs2 = 2.0;   // a block of 4- or 8-bit operands with the values' low halves
+constexpr double kWindowRecordUs = 5e-4;  // of one row and split, under 2048 rows
 
-// Whether a class's windowed queries go to the many-row kernel, which reads a
-// block once for 256 rows.
-bool window_many(const kvq_cache* c, int seq0, int nqry) {
-  return c->window[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyRows;
-}
-
-// Rows of a class's windowed launch: one query's heads, a tile of 16 rows of whole
-// queries where they fit one, else row groups of 32 (the last group may repeat the
-// last query in its spare rows).
-Rows window_rows(const kvq_cache* c, int seq0, int nqry) {
+// Rows of a class's windowed launch: 16-row groups of whole queries, or row groups
+// of 32 of the many-row kernel (the last group may repeat the last query).
+Rows window_rows(const kvq_cache* c, int nqry, bool many) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
   Rows r;
   r.nqry = nqry;
-  r.many = window_many(c, seq0, nqry);
-  r.rows = r.many ? 32 : 16;
+  r.many = many;
+  r.rows = many ? 32 : 16;
   r.qpr = std::min(nqry, r.rows / gqh);
   r.nrg = (nqry + r.qpr - 1) / r.qpr;
   return r;
@@ -973,6 +965,58 @@ double window_us(int64_t wgs, int64_t blocks, int64_t merged_rows) {
   return 4.0 + (4.0 + 1.15 * (double)blocks) * (rounds > 1 ? 0.85 * (double)rounds : 1.0) +
          (merged_rows > 0 ? 5.0 + 3e-3 * (double)merged_rows : 0.0);
 }
+// Of one on the many-row kernel, which reads a block once for 256 rows: blocks of the
+// longest workgroup, rows per kv head, records (rows times splits) and rows to merge
+// (few of those take the merge of a workgroup per 32 channels).  4- or 8-bit
+// operands: two halves.  The two estimates choose the kernel; against each alone (1,
+// 4 and 16 sequences of four heads per kv head, 8 to 512 queries, windows of 512 and
+// 4096, K2V2 and K4V4) within 10% of the better: one window of 512 tokens, K2V2, 256
+// queries 24 us in tiles and 26, 512 queries 40 and 33; of 4096 tokens 32 queries 27
+// and 30, 64 33 and 29, 512 134 and 77; 16 sequences of 4096, 16 queries 73 and 98, 32
+// 135 and 102, 128 499 and 217.
+double window_many_us(int64_t wgs, int64_t blocks, bool wide, int64_t head_rows, int64_t records, int64_t merged_rows) {
+  const int64_t cus = target_workgroups(1);
+  const double fill = 0.6 + 0.4 * (double)std::min<int64_t>(head_rows, 256) / 256;  // (waves without rows only unpack)
+  return (double)((wgs + cus - 1) / cus) * ((double)blocks * fill * (wide ? kWindowBlockUs2 : kBlockUs) + kSplitUs) +
+         (double)records * (merged_rows < 2048 ? kWindowRecordUs : kRecordUs);
+}
+
+// How a class's windowed launch is split: key groups (many rows: blocks) per split,
+// and its estimated time.  reach: of each of its sequences.
+struct WindowSplit {
+  Rows r;
+  std::vector<int32_t> reach;
+  int64_t per = 0;
+  double us = 0.0;
+};
+WindowSplit split_window(const kvq_cache* c, const std::vector<int>& seqs, int nqry, int32_t window, int32_t sinks, bool many,
+                         int64_t bound) {
+  WindowSplit w;
+  w.r = window_rows(c, nqry, many);
+  const int64_t units = (int64_t)c->d.num_kv_heads * (many ? (w.r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : w.r.nrg);
+  const int64_t least = many ? 1 : kMinGroupsPerSplit, rows = (int64_t)nqry * c->d.num_q_heads;
+  const bool wide = c->bk[seqs[0]] + c->bv[seqs[0]] > 4;
+  int64_t longest = 1;
+  for (int i : seqs) {
+    w.reach.push_back(window_reach(c, i, w.r, window, sinks));
+    longest = std::max<int64_t>(longest, w.reach.back());
+  }
+  for (int64_t ns = 1; ns <= std::min<int64_t>(bound, 64); ++ns) {
+    const int64_t n = std::max<int64_t>((longest + ns - 1) / ns, least);
+    int64_t wgs = 0, records = 0, merged = 0;
+    for (int32_t reach : w.reach) {
+      const int64_t k = std::max<int64_t>(1, (reach + n - 1) / n);
+      wgs += units * k;
+      records += k > 1 ? k * rows : 0;
+      merged += k > 1 ? rows : 0;
+    }
+    const double t = many ? window_many_us(wgs, n, wide, rows / c->d.num_kv_heads, records, merged)
+                          : window_us(wgs, (n + least - 1) / least * (c->d.key_group / 32), merged);
+    if (ns == 1 || t < w.us) w.us = t, w.per = n;
+    if (n == least) break;
+  }
+  return w;
+}
 
 // The split plan of a windowed call: the splits with the smallest estimated time,
 // every sequence's of the same number of key groups (16-row groups: no fewer than
@@ -990,73 +1034,37 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   p.ns.assign(B, 0);
   p.base.assign(B, 0);
   p.direct.assign(B, 0);
+  p.many.assign(B, 0);
   const int64_t bound = window_splits(c, nqry, window, sinks);
   std::map<std::pair<int, int>, std::vector<int>> classes;
   for (int i = 0; i < B; ++i)
     if (c->L[i] > 0) classes[{c->bk[i], c->bv[i]}].push_back(i);
   for (auto& cl : classes) {
-    const Rows r = window_rows(c, cl.second[0], nqry);
-    const int64_t units = (int64_t)c->d.num_kv_heads * (r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg);
-    int64_t longest = 0;
-    for (int i : cl.second) {
-      p.nq[i] = window_reach(c, i, r, window, sinks);
-      longest = std::max<int64_t>(longest, p.nq[i]);
+    const std::vector<int>& seqs = cl.second;
+    WindowSplit w = split_window(c, seqs, nqry, window, sinks, false, bound);
+    if (c->window[seqs[0]] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyFrom) {
+      WindowSplit other = split_window(c, seqs, nqry, window, sinks, true, bound);
+      if (other.us < w.us) w = std::move(other);
     }
-    if (r.many) {
-      const double block_us = cl.first.first + cl.first.second <= 4 ? kBlockUs : kWindowBlockUs2;
-      const int64_t cus = target_workgroups(1);
-      int64_t bps = longest;
-      double best = 0.0;
-      for (int64_t ns = 1; ns <= std::min<int64_t>(bound, 64); ++ns) {
-        const int64_t n = (longest + ns - 1) / ns;
-        int64_t wgs = 0, records = 0;
-        for (int i : cl.second) {
-          const int64_t k = (p.nq[i] + n - 1) / n;
-          wgs += units * k;
-          records += k > 1 ? k : 0;
-        }
-        const double t = (double)((wgs + cus - 1) / cus) * (n * block_us + kSplitUs) +
-                         records * (double)nqry * c->d.num_q_heads * kRecordUs;
-        if (ns == 1 || t < best) best = t, bps = n;
-      }
-      if (c->split_tokens > 0) bps = std::max<int64_t>(c->split_tokens / 32, (longest + bound - 1) / bound);
-      for (int i : cl.second) {
-        p.ns[i] = (int32_t)((p.nq[i] + bps - 1) / bps);
-        p.nq[i] = (int32_t)bps;
-        p.direct[i] = p.ns[i] <= 1;
-      }
-      continue;
-    }
-    int64_t groups = c->split_tokens / gk;
-    if (groups == 0) {
-      groups = kMinGroupsPerSplit;
-      double best = 0.0;
-      for (int64_t ns = 1; ns <= std::min<int64_t>(longest, 64); ++ns) {
-        const int64_t n = std::max<int64_t>((longest + ns - 1) / ns, kMinGroupsPerSplit);
-        int64_t wgs = 0, rows = 0;
-        for (int i : cl.second) {
-          const int64_t k = std::max<int64_t>(1, (p.nq[i] + n - 1) / n);
-          wgs += units * k;
-          rows += k > 1 ? (int64_t)nqry * c->d.num_q_heads : 0;
-        }
-        const double t = window_us(wgs, (n + kMinGroupsPerSplit - 1) / kMinGroupsPerSplit * (gk / 32), rows);
-        if (ns == 1 || t < best) best = t, groups = n;
-        if (n == kMinGroupsPerSplit) break;
-      }
-    }
-    groups = std::max(groups, (longest + kMaxSplits - 1) / kMaxSplits);
+    const int64_t longest = *std::max_element(w.reach.begin(), w.reach.end());
+    if (c->split_tokens > 0) w.per = c->split_tokens / (w.r.many ? 32 : gk);
+    w.per = w.r.many ? std::max(w.per, (longest + bound - 1) / bound) : std::max(w.per, (longest + kMaxSplits - 1) / kMaxSplits);
+    const int64_t units = (int64_t)c->d.num_kv_heads * w.r.nrg;
     int64_t wgs = 0, tails = 0;
-    for (int i : cl.second) {
-      p.nq[i] = (int32_t)((p.nq[i] + groups - 1) / groups);
-      wgs += units * std::max(p.nq[i], 1);
+    for (size_t k = 0; k < seqs.size(); ++k) {
+      const int i = seqs[k];
+      p.many[i] = w.r.many;
+      p.ns[i] = (int32_t)std::max<int64_t>(1, (w.reach[k] + w.per - 1) / w.per);
+      p.nq[i] = w.r.many ? (int32_t)w.per : (int32_t)((w.reach[k] + w.per - 1) / w.per);
+      p.st[i] = w.r.many ? 0 : (int32_t)(w.per * gk);
+      wgs += units * p.ns[i];
       if (p.nq[i] > 1 && c->L[i] > c->Lq[i]) tails += units;
     }
-    const bool own_tails = wgs + tails <= target_workgroups(1);
-    for (int i : cl.second) {
-      p.st[i] = (int32_t)(groups * gk);
-      p.ns[i] = std::max(p.nq[i], 1) + (own_tails && p.nq[i] > 1 && c->L[i] > c->Lq[i] ? 1 : 0);
+    const bool own_tails = !w.r.many && wgs + tails <= target_workgroups(1);
+    for (int i : seqs) {
+      if (own_tails && p.nq[i] > 1 && c->L[i] > c->Lq[i]) ++p.ns[i];
       p.direct[i] = p.ns[i] == 1;
-      p.required += p.direct[i];  // (a workspace is asked for whether or not the lengths leave it unused)
+      p.required += p.direct[i] && !w.r.many;  // (a workspace is asked for whether or not the lengths leave it unused)
     }
   }
   for (int i = 0; i < B; ++i) {
@@ -1076,7 +1084,7 @@ kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int
     if (c->L[i] > 0) seqs.push_back(i);
   for (auto& cls : bit_classes(c, seqs)) {
     kvq::DecodeArgs a{};
-    const Rows r = window_rows(c, cls.second[0], p.nqry);
+    const Rows r = window_rows(c, p.nqry, p.many[cls.second[0]] != 0);
     fill_args(a, c, cls.second[0], r, q, ws);
     a.split_tokens = p.st[cls.second[0]];
     a.window = window;

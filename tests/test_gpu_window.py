@@ -64,10 +64,12 @@ class Setup:
             out.append(oracle.dequant_head(img, self.lens[s], 128, *args))
         return np.stack([x[0] for x in out]), np.stack([x[1] for x in out])
 
-    def check(self, q, got, window, sinks):
+    def check(self, q, got, window, sinks, only=None):
         worst = 0.0
         assert np.isfinite(got).all()
         for s, n in enumerate(self.lens):
+            if only is not None and s not in only:
+                continue
             if n == 0:
                 assert (got[s] == 0).all()
                 continue
@@ -166,6 +168,46 @@ def test_small_and_large_numbers_of_mixed_bits(kw, bk, bv):
     c = Setup((330, 200), bk, bv, R=20, **kw)
     q = c.queries(70)
     c.check(q, run(c, q, 120, 4), 120, 4)
+
+
+def check_many(lens, n_q, window, sinks, **kw):
+    """Windows of a batch that keeps every compute unit busy, where long chunks take 256 rows per workgroup: the
+    sequences `lens` and short ones beside them."""
+    more = tuple(n_q + 20 + i % 60 for i in range(64 - len(lens)))
+    both = {x: kw.pop(x) for x in ("bk", "bv")}
+    c = Setup(tuple(lens) + more, both["bk"], both["bv"], **kw)
+    q = c.queries(n_q)
+    c.check(q, run(c, q, window, sinks), window, sinks, only=(*range(len(lens)), 40, 63))
+
+
+@pytest.mark.parametrize("bk", [1, 2, 4, 8])
+@pytest.mark.parametrize("bv", [1, 2, 4, 8])
+def test_many_rows_every_class(bk, bv):
+    check_many((420, 77), 70, 50, 4, bk=bk, bv=bv, R=3)
+
+
+@pytest.mark.parametrize("kw", [dict(vmul=1e-5), dict(vmul=2e-7), dict(vadd=3000.0), dict(vmul=5000.0), dict(kmul=1e-5),
+                                dict(kmul=20.0), dict(vmul=1e-3, vadd=1e-4)], ids=str)
+@pytest.mark.parametrize("bk,bv", [(1, 1), (8, 8), (2, 4), (4, 2)])
+def test_many_rows_small_and_large_numbers(kw, bk, bv):
+    check_many((330, 200), 70, 120, 4, bk=bk, bv=bv, R=20, **kw)
+
+
+@pytest.mark.parametrize("n_q,window,sinks,lens,kw", [
+    (70, 100, 4, (900, 71, 513), dict(bk=4, bv=4, page=64, R=32)),
+    (70, 130, 4, (900, 70), dict(bk=2, bv=2, gk=128, gv=128, page=128)),
+    (200, 40, 37, (500, 200), dict(bk=1, bv=1, gq=1)),
+    (100, 90, 0, (500, 333), dict(bk=2, bv=8, gq=2, gv=64)),
+    (70, 33, 3, (700, 301), dict(bk=2, bv=2, gq=5)),
+    (70, 150, 1, (700, 131), dict(bk=4, bv=4, gq=8, gk=64)),
+    (70, 1, 0, (300, 96), dict(bk=2, bv=2)),
+    (70, 1, 1, (300, 96), dict(bk=8, bv=4, R=17)),
+    (70, 20, 90, (250, 140), dict(bk=2, bv=2, R=100)),
+    (70, 1 << 30, 0, (400, 70), dict(bk=2, bv=1, R=64)),
+    (70, 64, 1 << 30, (400, 90), dict(bk=1, bv=4)),
+    (70, 30, 4, (260, 75), dict(bk=2, bv=2, R=300))], ids=lambda x: str(x).replace(" ", ""))
+def test_many_rows_layouts_and_masks(n_q, window, sinks, lens, kw):
+    check_many(lens, n_q, window, sinks, **kw)
 
 
 @pytest.mark.parametrize("n,n_q", [(64, 1), (65, 1), (130, 1), (67, 4)])
