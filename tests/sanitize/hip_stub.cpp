@@ -15,6 +15,7 @@
 #include "kvq_internal.h"
 
 int g_launches = 0;
+int g_window_rows = 0;  // launches of the many-row kernel's windows
 int g_row_plans = 0;  // chunk launches whose row groups were checked
 
 hipError_t hipGetDevice(int* dev) {
@@ -243,7 +244,7 @@ int launch_window(const DecodeArgs& a, int bk, int bv, void*) {
   return check_rows(a, 16), touch_window(a, bk, bv, a.qpr, false), 0;
 }
 int launch_window_rows(const DecodeArgs& a, int bk, int bv, void*) {
-  return check_rows(a, 32), touch_window(a, bk, bv, a.qpr * kPrefillWaves, true), 0;
+  return ++g_window_rows, check_rows(a, 32), touch_window(a, bk, bv, a.qpr * kPrefillWaves, true), 0;
 }
 int launch_export(const ExportArgs& a, void*) {
   check_regions(a, nullptr);

@@ -174,6 +174,30 @@ static void exercise(const kvq_cache_desc& d) {
 // A head whose value scales and fp16 ring lie past 4 GiB (the launch
 // stand-ins check the order of the regions).  The arena is reserved, never
 // filled.
+extern int g_window_rows;
+// Windows of a batch whose chunks fill every compute unit: 256 rows per workgroup.
+static void windows_of_many_rows(int bits_k, int bits_v, int hq, int hkv, int gk, int R, int page) {
+  constexpr int B = 48, nq = 70;
+  const std::vector<uint8_t> bk(B, (uint8_t)bits_k), bv(B, (uint8_t)bits_v);
+  const kvq_cache_desc d = desc(B, hq, hkv, 400, gk, 32, R, bk.data(), bv.data(), page);
+  const size_t bytes = kvq_cache_bytes(&d);
+  Buf arena(bytes);
+  kvq_cache* c = nullptr;
+  EXPECT(kvq_cache_init(&c, &d, arena.p, bytes) == KVQ_OK);
+  Buf kv((size_t)B * 400 * hkv * 128 * 2), q((size_t)B * nq * hq * 128 * 2), out((size_t)B * nq * hq * 128 * 4);
+  std::vector<int32_t> n(B);
+  for (int s = 0; s < B; ++s) n[s] = nq + s * 53 % 331;
+  EXPECT(kvq_append(c, kv.p, kv.p, 400, n.data(), nullptr) == KVQ_OK);
+  const int before = g_window_rows;
+  for (int window : {1, 40, 250, 1 << 30})
+    for (int sinks : {0, 4, 90}) {
+      Buf ws(kvq_window_workspace_bytes(c, nq, window, sinks));
+      EXPECT(kvq_window_attention(c, q.p, nq, window, sinks, out.as<float>(), ws.p, ws.n, nullptr) == KVQ_OK);
+    }
+  EXPECT(g_window_rows > before);
+  kvq_cache_destroy(c);
+}
+
 static void large_head(int bits_k, int bits_v, int gv, int max_tokens, int window, int page) {
   const uint8_t bk[1] = {(uint8_t)bits_k}, bv[1] = {(uint8_t)bits_v};
   const kvq_cache_desc d = desc(1, 4, 1, max_tokens, 32, gv, window, bk, bv, page, page ? 4 : 0);
@@ -232,6 +256,9 @@ int main() {
   exercise(desc(3, 32, 8, 900, 32, 32, 0, b8, b8, 64));        // paged
   exercise(desc(2, 32, 8, 800, 32, 32, 50, b1, b1, 128, 9));   // paged, shared pool smaller than capacity
   exercise(desc(1, 8, 8, 200, 32, 128, 0, b1, b1));            // one head per kv head
+  windows_of_many_rows(2, 2, 16, 4, 32, 0, 0);
+  windows_of_many_rows(8, 1, 8, 1, 64, 130, 0);
+  windows_of_many_rows(4, 4, 10, 2, 32, 33, 64);
   large_head(8, 8, 32, 1 << 24, 0, 0);
   large_head(2, 2, 8, 1 << 25, 0, 0);
   large_head(8, 1, 128, 1 << 24, 1 << 23, 0);
