@@ -95,8 +95,8 @@ struct Staged {
 // WINDOW: windowed attention.  The blocks of a split are those of the key groups
 // that the workgroup's windows and the sinks touch, as one list, and then the
 // tail's; b counts through the list, block_at gives a block's place.  Measured, 512
-// queries of four heads over windows of 4096 tokens, 8 kv heads: K2V2 83 us, K2V4 83
-// (tiles of 16 rows 342 and 357), 1024 queries K2V2 131 with their merge.
+// queries of four heads over windows of 4096 tokens, 8 kv heads: K2V2 76 us, K2V4 83
+// (tiles of 16 rows 134 and 148), 1024 queries K2V2 130 with their merge.
 template <int BK, int BV, bool PAGED, bool WINDOW>
 __global__ __launch_bounds__(64 * kNW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefill_mfma_kernel(DecodeArgs a) {
   constexpr int PK = Code<BK>::parts, PV = Code<BV>::parts, kZOp = 8 * PK + 8 * PV;
