@@ -19,12 +19,16 @@
 // A weight is a 24-bit number M 2^-n (n = floor(d), one hardware exponential of
 // the rest, d itself in 64 bits), and all elements of a bin share n, so a bin's
 // mass is a whole number, counted up with its elements in one 64-bit atomic;
-// masses across bins are whole numbers of 2^-unit of the largest weight.  Sums
+// masses across bins are whole numbers of 2^-unit of the largest weight (unit is
+// 45, 38 for the largest vocabularies): a sum of M is rounded down to them, never
+// an M alone, or the elements of deep bins would add up to less than the bin.  Sums
 // are exact: they depend neither on the order of the atomics nor on whether a
-// bin or the list summed an element.  Weights below 2^-unit count as 0 (unit is
-// 45, 38 for the largest vocabularies); they, and all of the last bin, are never
-// chosen.  A row whose bins hold more elements than a list (thousands of equal
-// logits) is searched over all its logits, a digit of the keys at a time.
+// bin, the list or a search over the row summed an element.  Elements of the last
+// bin, 51 octaves down, count as 0 and are never chosen.  Where the bins that the
+// searches end in, with what lies between the filters' ones, hold more elements
+// than a list (thousands of equal logits; top-k of thousands beside a top-p that
+// ends far above it), each search goes over all the row's logits, a digit of the
+// keys at a time.
 //
 // What bounds it: latency, along one workgroup's dependent steps: of one row's 23
 // us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then the ends 3.5,
@@ -385,11 +389,11 @@ __device__ __forceinline__ Ends find_ends(const SampleArgs& a, const Row& r, Pre
   return e;
 }
 
-// A search over all of a row's logits, a digit of the keys at a time: the first
-// element, in descending order, with which the count or the mass of the elements
-// so far is past a target.
+// A search over a row's elements of one bin that are not listed, a digit of the
+// keys at a time: the first element, in descending order, with which past(their
+// count, their sum of M) holds; mass: the M up to and with it.
 struct Found {
-  uint64_t key, mass;  // the element; the mass up to and with it
+  uint64_t key, mass;
 };
 struct Digits {
   uint64_t mass[256];
@@ -398,7 +402,7 @@ struct Digits {
   uint32_t digit;
 };
 template <class T, class F>
-__device__ __forceinline__ Found search_row(const SampleArgs& a, const typename T::raw* z, double zmax, const Row& r, Digits& s, F past) {
+__device__ __forceinline__ Found search_row(const SampleArgs& a, const typename T::raw* z, double zmax, const Row& r, int bin, Digits& s, F past) {
   uint64_t prefix = 0, mass = 0, count = 0;
   // (bits 24-31, of the index's complement, are ones: V <= 2^24)
   for (int shift = 56; shift >= 0; shift -= 8) {
@@ -416,11 +420,13 @@ __device__ __forceinline__ Found search_row(const SampleArgs& a, const typename 
       const int i = base + (int)threadIdx.x;
       const float value = i < a.vocab ? T::value(z[i]) : -__builtin_inff();
       const uint64_t key = make_key(value, i);
-      const bool in = i < a.vocab && (shift == 56 || (key >> (shift + 8)) == prefix);
+      bool in = i < a.vocab && (shift == 56 || (key >> (shift + 8)) == prefix);
+      if (!__builtin_amdgcn_ballot_w64(in)) continue;
+      const Place p = place_of(depth(zmax, value, r.inv));
+      in = in && p.bin == bin;
       const uint64_t some = __builtin_amdgcn_ballot_w64(in);
       if (!some) continue;
-      const Place p = place_of(depth(zmax, value, r.inv));
-      const uint64_t w = in ? mass_of(p.m, p.bin, a.unit) : 0;
+      const uint64_t w = in ? p.m : 0;
       const uint32_t digit = (uint32_t)(key >> shift) & 255u;
       const uint32_t common = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(some));
       if (__builtin_amdgcn_ballot_w64(in && digit != common) == 0) {
@@ -436,15 +442,17 @@ __device__ __forceinline__ Found search_row(const SampleArgs& a, const typename 
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-      int d = 255;
-      for (; d > 0; --d) {
-        if (past((uint32_t)count + s.count[d], mass + s.mass[d])) break;
-        count += s.count[d];
-        mass += s.mass[d];
+      // (rounding may have moved the target past the end: then the last element)
+      uint64_t n = count, m = mass;
+      for (int d = 255; d >= 0; --d) {
+        if (s.count[d] == 0) continue;
+        s.digit = (uint32_t)d;
+        s.before[0] = n;
+        s.before[1] = m;
+        n += s.count[d];
+        m += s.mass[d];
+        if (past((uint32_t)n, m)) break;
       }
-      s.digit = (uint32_t)d;
-      s.before[0] = count;
-      s.before[1] = mass;
     }
     __syncthreads();
     count = s.before[0];
@@ -736,15 +744,14 @@ __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& 
 #pragma unroll
           for (int j = 0; j < kListPer; ++j)
             if (c[j].bin == e.mb && c[j].near) sum += c[j].m;
-          sum = mass_of(block_sum(sum, m.part), e.mb, a.unit) + s.mass[e.mb];
         } else {
           each<T, kRowThreads>(z, 0, a.vocab, [&](float value, int) {
             const double d = depth(zmax, value, r.inv);
             const Place p = place_of(d);
-            if (d <= most) sum += mass_of(p.m, p.bin, a.unit);
+            if (p.bin == e.mb && d <= most) sum += p.m;
           });
-          sum = block_sum(sum, m.part);
         }
+        sum = mass_of(block_sum(sum, m.part), e.mb, a.unit) + s.mass[e.mb];
         kept = min(kept, sum);
       }
       total = min(total, kept);
@@ -753,21 +760,18 @@ __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& 
     auto past = [&](uint32_t count, uint64_t mass) {
       return turn == 0 ? count >= r.k : turn == 1 ? (double)mass >= t : (double)mass > t;
     };
+    int b = turn == 0 ? e.kb : turn == 1 ? e.p0 : e.u0;
+    const int last = turn == 0 ? e.kb : turn == 1 ? e.p1 : e.u1;
+    while (b < last && !past(s.count[b + 1], s.mass[b + 1])) ++b;
+    const uint64_t base = s.mass[b];
+    const uint32_t before = s.count[b];
+    auto past_in = [&](uint32_t count, uint64_t sum) { return past(before + count, base + mass_of(sum, b, a.unit)); };
     Found f;
-    if (listed) {
-      int b = turn == 0 ? e.kb : turn == 1 ? e.p0 : e.u0;
-      const int last = turn == 0 ? e.kb : turn == 1 ? e.p1 : e.u1;
-      while (b < last && !past(s.count[b + 1], s.mass[b + 1])) ++b;
-      const uint64_t base = s.mass[b];
-      const uint32_t before = s.count[b];
-      const bool alone = s.count[b + 1] - before == 1;
-      f = search_bin<T>(c, b, range_of(zmax, step, b, b), index_bits, alone, m.digit, m.found, [&](uint32_t count, uint64_t sum) {
-        return past(before + count, base + mass_of(sum, b, a.unit));
-      });
-      f.mass = base + mass_of(f.mass, b, a.unit);
-    } else {
-      f = search_row<T>(a, z, zmax, r, m.digits, past);
-    }
+    if (listed)
+      f = search_bin<T>(c, b, range_of(zmax, step, b, b), index_bits, s.count[b + 1] - before == 1, m.digit, m.found, past_in);
+    else
+      f = search_row<T>(a, z, zmax, r, b, m.digits, past_in);
+    f.mass = base + mass_of(f.mass, b, a.unit);
     if (turn == 0) total = f.mass;
     if (turn == 1) kept = f.mass;
     token = f.key;
