@@ -384,6 +384,28 @@ class KVCache:
             self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
         return self.ws
 
+    def _buffers(self, stream, device, shape, out, ws_bytes):
+        """``out`` (made if None) and a workspace of a call on ``stream``, made on that stream: torch's allocator gives
+        a freed tensor's memory to the next tensor of the stream that it was made on, so a workspace of another stream
+        than its kernels' would be somebody else's while they still write it."""
+        import torch
+
+        def make():
+            return (torch.empty(shape, dtype=torch.float32, device=device) if out is None else out,
+                    torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=self.arena.device))
+
+        if stream is None or not torch.cuda.is_available():
+            return make()
+        caller = torch.cuda.current_stream(self.arena.device)
+        if isinstance(stream, int):  # (0, the default stream, is not a handle to torch)
+            at = self.arena.device
+            stream = torch.cuda.ExternalStream(stream, device=at) if stream else torch.cuda.default_stream(at)
+        with torch.cuda.stream(stream):
+            made = make()
+        if out is None and made[0].is_cuda:  # (the caller may drop it with work of their own stream still to come)
+            made[0].record_stream(caller)
+        return made
+
     def decode(self, q, out=None, stream=None):
         import torch
         if out is None:
@@ -411,12 +433,10 @@ class KVCache:
         if q.dtype != torch.float16 or q.shape != shape or not q.is_contiguous():
             raise ValueError(f"q must be a contiguous float16 tensor of shape {shape}")
         n_q = int(q.shape[1])
-        if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=q.device)
-        elif out.dtype != torch.float32 or out.shape != shape or not out.is_contiguous():
+        if out is not None and (out.dtype != torch.float32 or out.shape != shape or not out.is_contiguous()):
             raise ValueError(f"out must be a contiguous float32 tensor of shape {shape}")
         need = kvq_window_workspace_bytes(self.handle, n_q, window, sinks)
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
+        out, ws = self._buffers(stream, q.device, shape, out, need)
         kvq_window_attention(self.handle, q, n_q, window, sinks, out, ws, stream=stream)
         return out
 
