@@ -361,7 +361,7 @@ class KVCache:
             kvq_cache_init(self.desc, 256, 0)
         self.arena = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         self.handle = kvq_cache_init(self.desc, self.arena)
-        self.ws = None
+        self.ws = self.ws_stream = None
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -382,6 +382,7 @@ class KVCache:
         need = kvq_workspace_bytes(self.handle)
         if self.ws is None or self.ws.numel() < need:
             self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
+            self.ws_stream = _stream(None)
         return self.ws
 
     def _buffers(self, stream, device, shape, out, ws_bytes):
@@ -406,23 +407,30 @@ class KVCache:
             made[0].record_stream(caller)
         return made
 
-    def decode(self, q, out=None, stream=None):
+    def _decode_buffers(self, stream, q, out):
+        """``out`` (made if None) and a workspace of a decode step: the cache's own on the stream that it was made on,
+        else one of the call's stream (two steps at once would write their records into the same one)."""
         import torch
+        shape, at = (self.batch, self.num_q_heads, self.head_dim), _stream(stream)
+        current = stream is None or at == _stream(None)
+        if current and self.ws is None:
+            self.workspace()
+        if not current or at != self.ws_stream:
+            return self._buffers(stream, q.device, shape, out, kvq_workspace_bytes(self.handle))
         if out is None:
-            out = torch.empty((self.batch, self.num_q_heads, self.head_dim), dtype=torch.float32,
-                              device=q.device)
-        kvq_decode_attention(self.handle, q, out, self.workspace(), stream=stream)
+            out = torch.empty(shape, dtype=torch.float32, device=q.device)
+        return out, self.workspace()
+
+    def decode(self, q, out=None, stream=None):
+        out, ws = self._decode_buffers(stream, q, out)
+        kvq_decode_attention(self.handle, q, out, ws, stream=stream)
         return out
 
     def chunk(self, q, out=None, stream=None):
         """Causal attention of the last q.shape[1] tokens of every sequence."""
-        import torch
         n_q = int(q.shape[1])
-        if out is None:
-            out = torch.empty((self.batch, n_q, self.num_q_heads, self.head_dim), dtype=torch.float32,
-                              device=q.device)
-        need = kvq_chunk_workspace_bytes(self.handle, n_q)
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.arena.device)
+        shape = (self.batch, n_q, self.num_q_heads, self.head_dim)
+        out, ws = self._buffers(stream, q.device, shape, out, kvq_chunk_workspace_bytes(self.handle, n_q))
         kvq_chunk_attention(self.handle, q, n_q, out, ws, stream=stream)
         return out
 
@@ -441,13 +449,10 @@ class KVCache:
         return out
 
     def append_decode(self, K, V, q, n_new=None, out=None, stream=None):
-        import torch
         if n_new is None:
             n_new = [int(K.shape[1])] * self.batch
-        if out is None:
-            out = torch.empty((self.batch, self.num_q_heads, self.head_dim), dtype=torch.float32,
-                              device=q.device)
-        kvq_append_decode(self.handle, K, V, n_new, q, out, self.workspace(), stream=stream)
+        out, ws = self._decode_buffers(stream, q, out)
+        kvq_append_decode(self.handle, K, V, n_new, q, out, ws, stream=stream)
         return out
 
     def seq_len(self, seq):

@@ -41,8 +41,10 @@ def log(monkeypatch):
     @contextlib.contextmanager
     def stream(s):
         x.scope.append(s)
-        yield
-        x.scope.pop()
+        try:
+            yield
+        finally:
+            x.scope.pop()
 
     def make(shape, **kw):
         t = empty(shape, **kw)
@@ -66,7 +68,7 @@ def log(monkeypatch):
 
 def cache():
     c = object.__new__(kvq.KVCache)
-    c.batch, c.num_q_heads, c.head_dim, c.handle, c.ws = 2, 8, 128, None, None
+    c.batch, c.num_q_heads, c.head_dim, c.handle, c.ws, c.ws_stream = 2, 8, 128, None, None, None
     c.arena = torch.zeros(1, dtype=torch.uint8)
     return c
 
@@ -87,3 +89,43 @@ def test_window_makes_its_tensors_on_the_stream_it_runs_on(log, given, runs_on):
     log.recorded.clear()
     cache().window(Q, 8, 2, out=torch.zeros(OUT), stream=given)
     assert log.made == [(runs_on, (5000,))] and log.recorded == []
+
+
+CALLS = {"chunk": (OUT, lambda c, **kw: c.chunk(Q, **kw)), "decode": (OUT[:1] + OUT[2:], lambda c, **kw: c.decode(Q[:, 0], **kw)),
+         "append_decode": (OUT[:1] + OUT[2:], lambda c, **kw: c.append_decode(Q, Q, Q[:, 0], **kw))}
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("given,runs_on", [(OTHER, OTHER), (32, OTHER), (0, DEFAULT), (None, CURRENT)], ids=str)
+def test_the_other_calls_do_too(log, call, given, runs_on):
+    shape, f = CALLS[call]
+    c = cache()
+    f(c, stream=given)
+    assert sorted(log.made, key=str) == sorted([(runs_on, shape), (runs_on, (5000,))], key=str)
+    assert log.recorded == ([(shape, CURRENT)] if given is not None else [])
+    assert log.calls == [given]
+
+
+@pytest.mark.parametrize("call", ["decode", "append_decode"])
+def test_the_caches_workspace_stays_with_its_stream(log, call):
+    shape, f = CALLS[call]
+    c = cache()
+    f(c)
+    assert log.made.count((CURRENT, (5000,))) == 1
+    for given in (None, CURRENT):  # kept
+        log.made.clear()
+        f(c, stream=given)
+        assert log.made == [(CURRENT, shape)]
+    log.made.clear()
+    f(c, stream=OTHER)
+    assert (OTHER, (5000,)) in log.made
+    with torch.cuda.stream(OTHER):  # the current stream is another one now
+        log.made.clear()
+        f(c)
+        assert (OTHER, (5000,)) in log.made
+        log.made.clear()  # the workspace's stream by name, not the current one: nothing of the current one's
+        f(c, stream=CURRENT)
+        assert {s for s, _ in log.made} == {CURRENT}
+    log.made.clear()
+    f(c)
+    assert log.made == [(CURRENT, shape)]

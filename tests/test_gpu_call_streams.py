@@ -23,7 +23,8 @@ def others(c):
     return s + [s[0].cuda_stream, s[1].cuda_stream]
 
 
-CALLS = {"window": lambda c, q, **kw: c.window(q, 200, 4, **kw)}
+CALLS = {"window": lambda c, q, **kw: c.window(q, 200, 4, **kw), "chunk": lambda c, q, **kw: c.chunk(q, **kw),
+         "decode": lambda c, q, **kw: c.decode(q, **kw)}
 
 
 @pytest.mark.parametrize("call", list(CALLS))
@@ -72,3 +73,21 @@ def test_workspace_is_not_the_next_tensors(monkeypatch):
         x = torch.empty((size,), dtype=torch.uint8, device="cuda")
         assert x.data_ptr() >= at + size or x.data_ptr() + size <= at
     torch.cuda.synchronize()
+
+
+def test_decode_steps_on_two_streams_at_once():
+    # one cache, two streams: each step has a workspace of its own
+    c = Setup((60000, 30000), 2, 2, R=40, seed=23)
+    qs = [torch.from_numpy(c.queries(1)[:, 0].copy()).cuda() for _ in range(2)]
+    want = [bits(c.cache.decode(q)) for q in qs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        outs = []
+        for q, s in zip(qs, streams):
+            with torch.cuda.stream(s):
+                outs.append(c.cache.decode(q))
+        outs += [c.cache.decode(qs[0], stream=streams[1]), c.cache.decode(qs[1])]
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want + want):
+            assert (bits(out) == w).all()
