@@ -952,6 +952,37 @@ int64_t window_splits(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   return std::min<int64_t>(kMaxSplits, (reach + per - 1) / per) + 1;
 }
 
+// Workgroups of a launch's row groups per sequence and split.
+int64_t window_units(const kvq_cache* c, const Rows& r) {
+  return (int64_t)c->d.num_kv_heads * (r.many ? (r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : r.nrg);
+}
+bool window_many_possible(const kvq_cache* c, int seq0, int nqry) {
+  return c->window[seq0] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyFrom;
+}
+
+// Workgroups that a class of n sequences is split into at most: 8 rounds of one per
+// compute unit, 16 for several sequences.  So many even out unequal lengths by
+// themselves, and the records of the splits, which the workspace has to hold at any
+// lengths, grow with them.  (Without a limit: 64 sequences of 100 to 9000 tokens, five
+// queries, 12 rounds 198 us, 8 rounds 212; 32 of 500 to 8000, 64 queries, 356 us and
+// 349, in a workspace of 2.2 GB and 0.28; one sequence takes 7 rounds at most.)
+int64_t window_workgroups(size_t n) { return (n > 1 ? 16 : 8) * target_workgroups(1); }
+
+// Most splits of all sequences of a windowed call together, at any lengths.
+int64_t window_records(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
+  const int64_t each = window_splits(c, nqry, window, sinks);
+  if (c->split_tokens > 0) return c->d.batch * each;
+  std::map<std::pair<int, int>, std::vector<int>> classes;
+  for (int i = 0; i < c->d.batch; ++i) classes[{c->bk[i], c->bv[i]}].push_back(i);
+  int64_t most = 0;
+  for (auto& cl : classes) {
+    int64_t units = window_units(c, window_rows(c, nqry, false));
+    if (window_many_possible(c, cl.second[0], nqry)) units = std::min(units, window_units(c, window_rows(c, nqry, true)));
+    most += std::min<int64_t>((int64_t)cl.second.size() * each, window_workgroups(cl.second.size()) / units);
+  }
+  return std::max<int64_t>(most, 1);
+}
+
 // Estimated time of a windowed launch of 16-row groups: workgroups, key blocks that a
 // wave of the longest takes, rows to merge.  A compute unit holds two workgroups,
 // but one already keeps its vector units near half busy, so each further one costs
@@ -993,7 +1024,7 @@ WindowSplit split_window(const kvq_cache* c, const std::vector<int>& seqs, int n
                          int64_t bound) {
   WindowSplit w;
   w.r = window_rows(c, nqry, many);
-  const int64_t units = (int64_t)c->d.num_kv_heads * (many ? (w.r.nrg + kvq::kPrefillWaves - 1) / kvq::kPrefillWaves : w.r.nrg);
+  const int64_t units = window_units(c, w.r);
   const int64_t least = many ? 1 : kMinGroupsPerSplit, rows = (int64_t)nqry * c->d.num_q_heads;
   const bool wide = c->bk[seqs[0]] + c->bv[seqs[0]] > 4;
   int64_t longest = 1;
@@ -1010,6 +1041,7 @@ WindowSplit split_window(const kvq_cache* c, const std::vector<int>& seqs, int n
       records += k > 1 ? k * rows : 0;
       merged += k > 1 ? rows : 0;
     }
+    if (ns > 1 && wgs > window_workgroups(seqs.size())) break;
     const double t = many ? window_many_us(wgs, n, wide, rows / c->d.num_kv_heads, records, merged)
                           : window_us(wgs, (n + least - 1) / least * (c->d.key_group / 32), merged);
     if (ns == 1 || t < w.us) w.us = t, w.per = n;
@@ -1042,7 +1074,7 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
   for (auto& cl : classes) {
     const std::vector<int>& seqs = cl.second;
     WindowSplit w = split_window(c, seqs, nqry, window, sinks, false, bound);
-    if (c->window[seqs[0]] && (int64_t)nqry * (c->d.num_q_heads / c->d.num_kv_heads) >= kWindowManyFrom) {
+    if (window_many_possible(c, seqs[0], nqry)) {
       WindowSplit other = split_window(c, seqs, nqry, window, sinks, true, bound);
       if (other.us < w.us) w = std::move(other);
     }
@@ -1064,14 +1096,14 @@ SplitPlan plan_window(const kvq_cache* c, int nqry, int32_t window, int32_t sink
     for (int i : seqs) {
       if (own_tails && p.nq[i] > 1 && c->L[i] > c->Lq[i]) ++p.ns[i];
       p.direct[i] = p.ns[i] == 1;
-      p.required += p.direct[i] && !w.r.many;  // (a workspace is asked for whether or not the lengths leave it unused)
+      if (p.direct[i] && !w.r.many) p.required = 1;  // (a workspace is asked for whether or not the lengths leave it unused)
     }
   }
   for (int i = 0; i < B; ++i) {
     p.base[i] = (int32_t)p.records;
     p.records += p.direct[i] ? 0 : p.ns[i];
   }
-  p.required += p.records;
+  p.required = std::max(p.required, p.records);
   return p;
 }
 
@@ -1220,8 +1252,7 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
 
 size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
-  const int64_t splits = window_splits(c, n_q, window, sinks);
-  return (size_t)c->d.batch * c->d.num_q_heads * n_q * (size_t)splits * kvq::kRecFloats * sizeof(float);
+  return (size_t)window_records(c, n_q, window, sinks) * c->d.num_q_heads * n_q * kvq::kRecFloats * sizeof(float);
 }
 
 kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, int32_t window, int32_t sinks,
