@@ -390,19 +390,16 @@ class KVCache:
         a freed tensor's memory to the next tensor of the stream that it was made on, so a workspace of another stream
         than its kernels' would be somebody else's while they still write it."""
         import torch
-
-        def make():
-            return (torch.empty(shape, dtype=torch.float32, device=device) if out is None else out,
-                    torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=self.arena.device))
-
+        at = self.arena.device
         if stream is None or not torch.cuda.is_available():
-            return make()
-        caller = torch.cuda.current_stream(self.arena.device)
+            if out is None:
+                out = torch.empty(shape, dtype=torch.float32, device=device)
+            return out, torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=at)
+        caller = torch.cuda.current_stream(at)
         if isinstance(stream, int):  # (0, the default stream, is not a handle to torch)
-            at = self.arena.device
             stream = torch.cuda.ExternalStream(stream, device=at) if stream else torch.cuda.default_stream(at)
         with torch.cuda.stream(stream):
-            made = make()
+            made = self._buffers(None, device, shape, out, ws_bytes)
         if out is None and made[0].is_cuda:  # (the caller may drop it with work of their own stream still to come)
             made[0].record_stream(caller)
         return made
