@@ -120,6 +120,7 @@ __device__ __forceinline__ Entries entries_of(const DistillArgs& a, int row, int
   const auto* z = reinterpret_cast<const typename T::raw*>(a.logits) + (size_t)row * a.row_stride;
   Entries e;
   float t[kMaxK / 64], top = -__builtin_inff();
+  bool some = false;
 #pragma unroll
   for (int i = 0; i < kMaxK / 64; ++i) {
     const int k = 64 * i + lane;
@@ -127,10 +128,13 @@ __device__ __forceinline__ Entries entries_of(const DistillArgs& a, int row, int
     t[i] = k < a.k ? a.teacher[(size_t)row * a.k + k] : -__builtin_inff();
     if ((uint32_t)e.index[i] >= (uint32_t)a.vocab || t[i] == -__builtin_inff()) e.index[i] = -1;
     e.z[i] = a.loss && e.index[i] >= 0 ? T::value(z[e.index[i]]) : 0.f;
-    if (e.index[i] >= 0) top = fmaxf(top, t[i]);
+    if (e.index[i] >= 0) {
+      top = fmaxf(top, t[i]);
+      some = true;
+    }
   }
   top = dec::wave_max(top);
-  e.any = top != -__builtin_inff();
+  e.any = __builtin_amdgcn_ballot_w64(some) != 0;  // (a NaN is an entry, which no maximum shows)
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < kMaxK / 64; ++i) {
@@ -151,7 +155,7 @@ __device__ __forceinline__ float loss_of(const DistillArgs& a, const Entries& e,
   double loss = 0.0;
 #pragma unroll
   for (int i = 0; i < kMaxK / 64; ++i)
-    if (e.index[i] >= 0 && e.q[i] > 0.f)
+    if (e.index[i] >= 0 && !(e.q[i] == 0.f))  // (NaN: a teacher logit of NaN or +inf)
       loss += (double)e.q[i] * ((double)e.x[i] - log_total - ((double)e.z[i] - (double)m) * c + log_sum);
   return (float)(wave_sum_d(loss) * 0.6931471805599453 * (double)a.temperature * (double)a.temperature);
 }

@@ -1,0 +1,41 @@
+"""Rows of the teacher loss that hold no finite number, on each of its paths: rows in
+registers (vocabularies to 32768), one launch per step, the loss alone, the gradient
+from a kept log-sum-exp.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_distill import TYPES, check_row, inputs, run  # noqa: E402
+
+VOCABS = [5, 20000, 40001]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("v", VOCABS)
+def test_teacher_logits_without_a_softmax(v, kind):
+    # q is the softmax of the row's entries: NaN with a NaN or +inf among them
+    n, k = 7, 5
+    z, t, i = inputs(n, v, k, seed=31, kind=kind)
+    t[1, 2] = math.nan
+    t[2] = math.nan
+    t[3, 0] = math.inf
+    t[4] = -math.inf
+    t[4, 3] = math.nan
+    t[5, 1] = math.nan                       # not an entry: its index is none
+    i[5, 1] = -1
+    bad = [1, 2, 3, 4]
+    for backward in (False, True):
+        loss, lse, grad = run(z, t, i, 2.0, backward=backward)
+        for r in range(n):
+            if r in bad:
+                assert math.isnan(loss[r]) and np.isfinite(lse[r]), r
+                listed = [x for x, y in zip(i[r], t[r]) if y != -math.inf]
+                assert np.isnan(grad[r][listed]).all() and np.isfinite(np.delete(grad[r], listed)).all(), r
+            else:
+                check_row(z[r], t[r], i[r], 2.0, kind, 1.0, loss[r], lse[r], torch.from_numpy(grad[r]), backward)
+    assert np.isnan(run(z, t, i, 2.0, want_grad=False)[0]).nonzero()[0].tolist() == bad
