@@ -176,8 +176,9 @@ size_t dgap_distill_workspace_bytes(int32_t rows, int32_t vocab);
  * An index outside [0, vocab) or a teacher logit of -inf stands for no entry
  * (rows of fewer entries); entries of one index add up; a row without entries
  * has loss and gradient 0; an entry's teacher logit of NaN or +inf makes the loss
- * NaN, and the gradient at the row's entries.  Logits are finite or -inf (p = 0: a loss of +inf
- * where the teacher has an entry there), one of a row finite at least.
+ * NaN, and the gradient at the row's entries.  Logits are finite or -inf (p = 0:
+ * a loss of +inf where the teacher has an entry there), of a row with entries one
+ * finite at least.
  * loss: device fp32 [rows].  lse: NULL or device fp32 [rows], log sum e^(z/T)
  * for dgap_distill_backward.  grad: NULL (the loss alone) or device rows of
  * the logits' type, grad_row_stride >= vocab elements apart; it may be the

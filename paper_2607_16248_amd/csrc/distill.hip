@@ -245,6 +245,9 @@ __device__ __forceinline__ typename T::raw grad_one(const DistillArgs& a, const 
   for (int j = 1; j < 8; ++j) r = j == (at & 7) ? o[j] : r;
   return r;
 }
+// That of a row without entries, whose gradient is 0 also where nothing in it is
+// finite: every logit, -inf too, gives 0 times a power of at most 1.
+constexpr Softmax kNoEntries = {3.402823466e38f, 0.f};
 // From the caller's log-sum-exp: m its place among the logits, as near as fp32
 // has it, and r what that leaves.
 __device__ __forceinline__ Softmax from_lse(const DistillArgs& a, int row) {
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a) {
 #pragma unroll
     for (int i = 0; i < kPer / 8; ++i) v[i] = load8<T>(z + from + min(8 * (i * kThreads + tid), bulk - 8));
   }
-  const Softmax p = OWN_SUM ? Softmax{a.row_sum[2 * row], a.row_sum[2 * row + 1]} : from_lse(a, row);
+  Softmax p = OWN_SUM ? Softmax{a.row_sum[2 * row], a.row_sum[2 * row + 1]} : from_lse(a, row);
   if (tid < 64) put_entries(s, entries_of<T>(a, row, tid), from, tid);
   clear_shares<kThreads>(s);
   __syncthreads();
@@ -303,6 +306,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a) {
   __syncthreads();
   sum_shares<kThreads>(s, a.k);
   __syncthreads();
+  if (!s.some) p = kNoEntries;
   const float f = s.some ? a.temperature * (a.grad_loss ? a.grad_loss[row] : 1.f) : 0.f;
   // (a run past the end was loaded as the last one, which its own thread may
   // have written by now: it is not used)
@@ -420,6 +424,7 @@ __global__ __launch_bounds__(kRowThreads) void distill_row_kernel(DistillArgs a)
         if (a.lse) a.lse[row] = (float)((log_sum + (double)p.m * (double)a.c) * 0.6931471805599453);
       }
     }
+    if (!s.some) p = kNoEntries;
     const float f = s.some ? a.temperature * (a.grad_loss ? a.grad_loss[row] : 1.f) : 0.f;
     auto* g = reinterpret_cast<typename T::raw*>(a.grad) + (size_t)row * a.grad_stride;
     const int next = min(row + (int)gridDim.x, a.rows - 1);  // (after the last row: that one again, unused)

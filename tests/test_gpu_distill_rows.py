@@ -39,3 +39,29 @@ def test_teacher_logits_without_a_softmax(v, kind):
             else:
                 check_row(z[r], t[r], i[r], 2.0, kind, 1.0, loss[r], lse[r], torch.from_numpy(grad[r]), backward)
     assert np.isnan(run(z, t, i, 2.0, want_grad=False)[0]).nonzero()[0].tolist() == bad
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("v", VOCABS)
+def test_masked_rows_without_entries(v, kind):
+    # loss and gradient 0, whatever the mask has left of the logits: padding must not reach the weights
+    n, k = 6, 3
+    z, t, i = inputs(n, v, k, seed=32, kind=kind)
+    low = torch.finfo(TYPES[kind]).min
+    z[1] = -math.inf
+    z[2] = low
+    z[3, :] = -math.inf
+    z[3, v // 2] = low
+    z[4] = torch.finfo(TYPES[kind]).max
+    i[1:5] = -1
+    t[2] = -math.inf
+    for T in (0.5, 2.0, 1e30):
+        for backward in (False, True):
+            scale = [1.0, 1.0, -2.0, 3.0, math.inf, 0.5]
+            loss, lse, grad = run(z, t, i, T, grad_loss=scale, backward=backward)
+            assert (loss[1:5] == 0).all() and (grad[1:5] == 0).all(), (T, backward)
+            assert lse[1] == -math.inf
+            for r in (0, 5) if T < 1e9 else ():
+                check_row(z[r], t[r], i[r], T, kind, scale[r], loss[r], lse[r], torch.from_numpy(grad[r]), backward)
+        loss, lse, _ = run(z, t, i, T, want_grad=False)
+        assert (loss[1:5] == 0).all() and lse[1] == -math.inf
