@@ -50,7 +50,7 @@ typedef enum {
   KVQ_OK = 0,
   KVQ_ERR_ARG = 1,          /* invalid argument or descriptor */
   KVQ_ERR_UNSUPPORTED = 2,  /* valid but not implemented (e.g. head_dim != 128) */
-  KVQ_ERR_CAPACITY = 3,     /* an append would exceed max_tokens; workspace too small */
+  KVQ_ERR_CAPACITY = 3,     /* an append would exceed max_tokens; workspace too small; no host memory */
   KVQ_ERR_RANGE = 4,        /* input outside the quantizer's domain (see kvq_check) */
   KVQ_ERR_STATE = 5,        /* call not valid in the cache's current state */
   KVQ_ERR_HIP = 6           /* a HIP runtime call failed */
@@ -265,7 +265,7 @@ size_t kvq_window_workspace_bytes(const kvq_cache* cache, int32_t n_q, int32_t w
  * reproducible for a fixed split setting.
  * Errors: KVQ_ERR_ARG (n_q, window or sinks out of range, a sequence shorter
  * than n_q > 1, null pointers, misaligned workspace), KVQ_ERR_CAPACITY
- * (workspace too small), KVQ_ERR_HIP. */
+ * (workspace too small, no host memory), KVQ_ERR_HIP. */
 kvq_status kvq_window_attention(const kvq_cache* cache, const void* q, int32_t n_q, int32_t window, int32_t sinks,
                                 float* out, void* ws, size_t ws_bytes, void* stream);
 

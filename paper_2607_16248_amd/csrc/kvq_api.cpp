@@ -12,6 +12,7 @@
 #include <cstdio>
 #include <cstring>
 #include <map>
+#include <new>
 #include <string>
 #include <utility>
 #include <vector>
@@ -78,9 +79,16 @@ kvq_status fail(kvq_status s, const char* fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_err = buf;
+  try {
+    g_err = buf;
+  } catch (const std::bad_alloc&) {
+    g_err.clear();
+  }
   return s;
 }
+// What a call of the C interface ends with when its plan finds no memory: no exception
+// may pass it.
+kvq_status no_memory() { return fail(KVQ_ERR_CAPACITY, "no host memory"); }
 
 kvq_status ok() {
   g_err.clear();
@@ -1135,7 +1143,7 @@ kvq_status run_window(const kvq_cache* c, const SplitPlan& p, const void* q, int
 extern "C" {
 
 kvq_status kvq_decode_attention(const kvq_cache* c, const void* q, float* out, void* ws, size_t ws_bytes,
-                                void* stream) {
+                                void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
   const SplitPlan p = plan_splits(c);
@@ -1144,9 +1152,11 @@ kvq_status kvq_decode_attention(const kvq_cache* c, const void* q, float* out, v
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;
   return ok();
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
-kvq_status kvq_decode_attention_noalloc(const kvq_cache* c, const void* q, float* out, void* stream) {
+kvq_status kvq_decode_attention_noalloc(const kvq_cache* c, const void* q, float* out, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
   const SplitPlan p = plan_splits(c);
@@ -1162,6 +1172,8 @@ kvq_status kvq_decode_attention_noalloc(const kvq_cache* c, const void* q, float
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;
   return ok();
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
 kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t n_max, const int32_t* n_new,
@@ -1217,16 +1229,20 @@ kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t
   return ok();
 }
 
-kvq_status kvq_decode_partials(const kvq_cache* c, const void* q, void* ws, size_t ws_bytes, void* stream) {
+kvq_status kvq_decode_partials(const kvq_cache* c, const void* q, void* ws, size_t ws_bytes, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   const kvq_status st = run_partials(c, plan_splits(c), q, ws, ws_bytes, stream);
   return st == KVQ_OK ? ok() : st;
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
-kvq_status kvq_decode_merge(const kvq_cache* c, const void* ws, float* out, void* stream) {
+kvq_status kvq_decode_merge(const kvq_cache* c, const void* ws, float* out, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   const kvq_status st = run_merge(c, plan_splits(c), ws, out, stream);
   return st == KVQ_OK ? ok() : st;
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
 size_t kvq_chunk_workspace_bytes(const kvq_cache* c, int32_t n_q) {
@@ -1235,7 +1251,7 @@ size_t kvq_chunk_workspace_bytes(const kvq_cache* c, int32_t n_q) {
 }
 
 kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, float* out, void* ws,
-                               size_t ws_bytes, void* stream) {
+                               size_t ws_bytes, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (n_q < 1 || n_q > KVQ_MAX_CHUNK) return fail(KVQ_ERR_ARG, "n_q = %d outside [1, %d]", n_q, KVQ_MAX_CHUNK);
   if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
@@ -1248,15 +1264,19 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;
   return ok();
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
-size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
+size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) try {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
   return (size_t)window_records(c, n_q, window, sinks) * c->d.num_q_heads * n_q * kvq::kRecFloats * sizeof(float);
+} catch (const std::bad_alloc&) {
+  return 0;
 }
 
 kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, int32_t window, int32_t sinks,
-                                float* out, void* ws, size_t ws_bytes, void* stream) {
+                                float* out, void* ws, size_t ws_bytes, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (n_q < 1 || n_q > KVQ_MAX_CHUNK) return fail(KVQ_ERR_ARG, "n_q = %d outside [1, %d]", n_q, KVQ_MAX_CHUNK);
   if (window < 1) return fail(KVQ_ERR_ARG, "window = %d must be at least 1", window);
@@ -1276,6 +1296,8 @@ kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, 
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;
   return ok();
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
 kvq_status kvq_dequant(const kvq_cache* c, int32_t seq, int32_t tok0, int32_t ntok, float* K_out, float* V_out,
