@@ -25,10 +25,8 @@
 // are exact: they depend neither on the order of the atomics nor on whether a
 // bin, the list or a search over the row summed an element.  Elements of the last
 // bin, 51 octaves down, count as 0 and are never chosen.  Where the bins that the
-// searches end in, with what lies between the filters' ones, hold more elements
-// than a list (thousands of equal logits; top-k of thousands beside a top-p that
-// ends far above it), each search goes over all the row's logits, a digit of the
-// keys at a time.
+// searches end in hold more elements than a list (thousands of equal logits), each
+// search goes over all the row's logits, a digit of the keys at a time.
 //
 // What bounds it: latency, along one workgroup's dependent steps: of one row's 23
 // us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then the ends 3.5,
@@ -42,6 +40,8 @@
 // every match of a load, run once from a cold instruction cache, cost more than a
 // loop.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "decode_common.h"
 #include "kvq_internal.h"
@@ -646,7 +646,7 @@ __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& 
   const double most = r.min_p > 0.f ? -log2((double)fminf(r.min_p, 1.f)) : 0.0;  // largest depth that min-p keeps
   const auto* z = row_logits<T>(a, row);
   const double step = 1.0 / (kPerOctave * r.inv);
-  bool listed = wanted <= (uint32_t)kSampleList;
+  const bool listed = wanted <= (uint32_t)kSampleList;
   const int index_bits = 32 - __builtin_clz((uint32_t)a.vocab);
   Held c[kListPer];
 #pragma unroll
@@ -665,57 +665,73 @@ __device__ __forceinline__ void select(const SampleArgs& a, int row, const Row& 
     const Range x = range_of(zmax, step, e.u0, e.u1), y = range_of(zmax, step, b0, b1);
     const float least = fminf(x.lo, y.lo);
     const int wv = tid >> 6, lane = tid & 63, bulk = a.vocab & ~7;
-    auto put = [&](float value, int i) {
-      const uint32_t slot = atomicAdd(&m.held, 1u);
-      if (slot < (uint32_t)kSampleList) m.list[slot] = make_uint2(__builtin_bit_cast(uint32_t, value), (uint32_t)i);
-    };
-    for (int g0 = 0; bulk > 0 && g0 < a.ngroup; g0 += kRowThreads) {
-      // groups g0 + 16 l + wv that reach the wanted bins
-      const int own = own_group(g0);
-      if (g0 > 0) first = groups[min(own, a.ngroup - 1)];
-      uint64_t left = __builtin_amdgcn_ballot_w64(own < a.ngroup && first >= least);
-      int group[kAhead];  // -1: none left
-      raw8_t<T> v[kAhead];
-      auto next = [&](int u) {
-        group[u] = left ? g0 + (kRowThreads / 64) * __builtin_ctzll(left) + wv : -1;
-        left &= left - 1;
-        v[u] = load_below<T>(z, kGroup * max(group[u], 0) + 8 * lane, bulk);
+    auto list = [&](auto sift_c) __attribute__((always_inline)) {
+      auto put = [&](float value, int i) {
+        if (decltype(sift_c)::value && !e.wanted(place_of(depth(zmax, value, r.inv)).bin)) return;
+        const uint32_t slot = atomicAdd(&m.held, 1u);
+        if (slot < (uint32_t)kSampleList) m.list[slot] = make_uint2(__builtin_bit_cast(uint32_t, value), (uint32_t)i);
       };
+      for (int g0 = 0; bulk > 0 && g0 < a.ngroup; g0 += kRowThreads) {
+        // groups g0 + 16 l + wv that reach the wanted bins
+        const int own = own_group(g0);
+        const float held = g0 > 0 ? groups[min(own, a.ngroup - 1)] : first;
+        uint64_t left = __builtin_amdgcn_ballot_w64(own < a.ngroup && held >= least);
+        int group[kAhead];  // -1: none left
+        raw8_t<T> v[kAhead];
+        auto next = [&](int u) {
+          group[u] = left ? g0 + (kRowThreads / 64) * __builtin_ctzll(left) + wv : -1;
+          left &= left - 1;
+          v[u] = load_below<T>(z, kGroup * max(group[u], 0) + 8 * lane, bulk);
+        };
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) next(u);
-      while (group[0] >= 0) {
+        for (int u = 0; u < kAhead; ++u) next(u);
+        while (group[0] >= 0) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (group[u] < 0) break;
-          const int at = kGroup * group[u] + 8 * lane;
-          uint32_t hits = 0;  // (no branch per logit)
+          for (int u = 0; u < kAhead; ++u) {
+            if (group[u] < 0) break;
+            const int at = kGroup * group[u] + 8 * lane;
+            uint32_t hits = 0;  // (no branch per logit)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float value = T::value(v[u][j]);
-            hits |= x.has(value) | y.has(value) ? 1u << j : 0u;
-          }
-          hits = at < bulk ? hits : 0u;
+            for (int j = 0; j < 8; ++j) {
+              const float value = T::value(v[u][j]);
+              hits |= x.has(value) | y.has(value) ? 1u << j : 0u;
+            }
+            hits = at < bulk ? hits : 0u;
 #pragma unroll 1
-          while (hits) {
-            const int j = __builtin_ctz(hits);
-            hits &= hits - 1;
-            float value = T::value(v[u][0]);
+            while (hits) {
+              const int j = __builtin_ctz(hits);
+              hits &= hits - 1;
+              float value = T::value(v[u][0]);
 #pragma unroll
-            for (int o = 1; o < 8; ++o) value = j == o ? T::value(v[u][o]) : value;
-            put(value, at + j);
+              for (int o = 1; o < 8; ++o) value = j == o ? T::value(v[u][o]) : value;
+              put(value, at + j);
+            }
+            next(u);
           }
-          next(u);
         }
       }
+      if (bulk + tid < a.vocab) {
+        const float value = T::value(z[bulk + tid]);
+        if (x.has(value) || y.has(value)) put(value, bulk + tid);
+      }
+    };
+    // Between the filters' bins others may lie (top-k's thousands below the end of
+    // top-p), and a range's end, rounded outwards to fp32, may be bins away: where
+    // that is more than the list takes, every hit's bin is looked at before it is put.
+    bool sift = b1 > b0 && s.count[b1 + 1] - s.count[b0] > (uint32_t)kSampleList;
+    if (!sift) {
+      list(std::false_type{});
+      __syncthreads();
+      sift = m.held > (uint32_t)kSampleList;
+      if (sift) {
+        __syncthreads();
+        if (tid == 0) m.held = 0;
+        __syncthreads();
+      }
     }
-    if (bulk + tid < a.vocab) {
-      const float value = T::value(z[bulk + tid]);
-      if (x.has(value) || y.has(value)) put(value, bulk + tid);
-    }
+    if (sift) list(std::true_type{});
     __syncthreads();
-    // a range of bins may hold others between the wanted ones: more than the list takes
-    listed = m.held <= (uint32_t)kSampleList;
-    const int n = (int)min(m.held, (uint32_t)kSampleList);
+    const int n = (int)m.held;
 #pragma unroll
     for (int j = 0; j < kListPer; ++j) {
       const int i = kRowThreads * j + tid;

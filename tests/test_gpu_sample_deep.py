@@ -103,3 +103,14 @@ def test_long_top_k_with_a_shorter_nucleus():
         for k, p in ((3000, 0.8), (5000, 0.95), (20000, 0.8), (20000, 0.95)):
             check(z, u, T=0.8, k=k, p=p)
             check(z, u, T=1.2, k=k, p=p, m=0.001)
+
+
+def test_thousands_an_fp32_step_below_the_leader():
+    # a temperature so low that the next fp32 number is many bins away: a range's end takes in what its bins do not hold
+    for vocab in (9000, 200000):
+        z = torch.full((vocab,), 3.0)
+        z[::2] = float(np.nextafter(np.float32(3.0), np.float32(0.0)))
+        z[1::2][5000 if vocab > 9000 else 900:] = -1.0
+        for T in (1e-6, 2e-8, 1e-30):
+            check(z, [0.0, 0.4, 0.999], T=T)
+            check(z, [0.0, 0.4, 0.999], T=T, k=vocab // 3, p=0.7)
