@@ -1,8 +1,9 @@
 /*
  * dgap — the logit-side runtime step of DGAP on AMD Instinct MI355X
  * (gfx950), the token drawn from the logits it leaves (dgap_sample), and the
- * loss that its corrector is trained with (dgap_distill).  Plain C ABI, in the
- * same library as kvq.h.
+ * Kullback-Leibler loss against a teacher's top logits, one term of what its
+ * corrector is trained with (dgap_distill).  Plain C ABI, in the same library as
+ * kvq.h.
  *
  * DGAP restores the local top-K candidate distribution of a decoder that
  * keeps a low-bit KV cache (Methodology, "DGAP Overview", online restoration

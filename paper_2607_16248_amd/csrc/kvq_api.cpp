@@ -295,8 +295,12 @@ kvq_status check_scratch(const void* ws, size_t ws_bytes, size_t need) {
 }
 
 // A workgroup per row takes all steps of a draw from so many rows on, and for
-// vocabularies up to kSampleSmall: 128 rows of 128256 fp32 58 us, with chunks of
-// rows 66 (64 rows 45 and 39); one row of 32768 16 us and 17.
+// vocabularies up to kSampleSmall: 128 rows of 128256 fp32 59 us, with chunks of
+// rows 66 (64 rows 45 and 38).  Below kSampleRows, fp32: rows of 16384, 1 of them 17.8
+// us and 19.9, 64 41 and 43; of 32768, 1 17.5 and 17.0, 16 20.4 and 21.0, 64 flat ones
+// 27 and 31; of 40960, 1 23.5 and 20.7, 16 24.2 and 22.9, 64 25.6 and 27.4; of 50257,
+// 1 21.0 and 16.6, 64 40.6 and 40.2; of 65536, 1 28 and 22, 64 43 and 41 (bf16 within
+// 10% of these).
 constexpr int kSampleRows = 128, kSampleSmall = 32768;
 
 // Workspace of one row of dgap_sample (see SampleArgs::ws).
@@ -308,8 +312,12 @@ uint64_t sample_row_bytes(int vocab) {
 
 // Whether loss and gradient of rows that fit a workgroup's registers come from one
 // pass over them, else from three launches that read them twice.  One pass for
-// short rows, whose three launches cost more than their work (rows of 32768: 64 fp32
-// 13.1 us and 19.9, 1024 57 and 69; bf16 256 16 and 19, 512 and 3000 alike), and for
+// short rows, whose three launches cost more than their work (16384: 64 fp32 11 us
+// and 16, bf16 512 20 and 18; 32768: 64 fp32 13 and 16, 256 19 and 24, 1024 57 and 68,
+// bf16 64 12 and 15, 256 14 and 17, 512 28 and 25; 40960: 64 fp32 17.5 and 16, 256 24
+// and 28, bf16 64 16 and 15.5, 256 19 and 19; 50257: 64 fp32 18 and 16, 256 26 and 32,
+// bf16 64 20 and 16, 256 23 and 22; 65536: 64 fp32 20 and 17, 256 30 and 38, bf16 64
+// 18 and 16, 512 35 and 40), and for
 // more logits than stay in the 256 MiB cache beside their gradient (128256 bf16: 3000
 // rows 335 us and 438, 1024 127 and 157, 512, which are 131 MB, 68 and 69, 128 23 and
 // 24 but 64 30 and 19; 152064 f16 with 256 entries: 512, 156 MB, 98 and 83, 1024 175

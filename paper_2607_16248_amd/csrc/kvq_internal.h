@@ -296,7 +296,7 @@ struct DistillArgs {
   float* lse;               // per row; with loss: null or written
   void* grad;               // logits' type; null: the loss alone
   float* ws;                // per (row, chunk): largest logit m, sum of 2^((z - m) c)
-  float* row_sum;           // per row: the same m, and the sum's log2
+  float* row_sum;           // per row: the largest of its m, and its sum's reciprocal
   int64_t row_stride, grad_stride;
   int32_t rows, vocab, nchunk, k;
   int32_t whole_rows;       // rows in a workgroup's registers (loss and grad not null), on so many

@@ -28,11 +28,12 @@
 // searches end in hold more elements than a list (thousands of equal logits), each
 // search goes over all the row's logits, a digit of the keys at a time.
 //
-// What bounds it: latency, along one workgroup's dependent steps: of one row's 23
-// us (128256 fp32, top-k 50 and top-p 0.95) max 3 and bins 5, then the ends 3.5,
+// What bounds it: latency, along one workgroup's dependent steps: of one row's 24
+// us (128256 fp32, top-k 50 and top-p 0.95, an input whose three searches all go by
+// digits; 19 to 20 over many inputs) max 3 and bins 5, then the ends 3.5,
 // listing 6 (the compares, at four waves per SIMD: with every load asked for at
 // once it takes as long) and the three searches 4, one step after the other.  Many
-// rows: 256 flat ones of 128256 fp16 61 us, of which 11 go to the first read (all
+// rows: 256 flat ones of 128256 fp16 60 us, of which 11 go to the first read (all
 // that comes from HBM, 13 at a copy's rate), 21 to the bins, about twenty
 // instructions a logit (without their atomics, with the chains of a load side by
 // side, or in fixed point, 20 to 21), and 27 to listing and searching.  Sorting the
