@@ -7,6 +7,8 @@ import math
 import numpy as np
 import pytest
 
+from paper_2607_16248_amd import kvq
+
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +67,20 @@ def test_masked_rows_without_entries(v, kind):
                 check_row(z[r], t[r], i[r], T, kind, scale[r], loss[r], lse[r], torch.from_numpy(grad[r]), backward)
         loss, lse, _ = run(z, t, i, T, want_grad=False)
         assert (loss[1:5] == 0).all() and lse[1] == -math.inf
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("v", [1, 7, 8, 13, 8193, 20000, 40001])
+def test_gradient_alone_in_the_logits_place(v, kind):
+    n, k = 3, min(v, 20)
+    z, t, i = inputs(n, v, k, seed=33, kind=kind)
+    loss, lse, want = run(z, t, i, 2.0, backward=True)
+    base = torch.full((n, v + 9), 3.0, dtype=TYPES[kind], device="cuda")
+    for off in (0, 1, 9):
+        x = base[:, off:off + v]
+        x.copy_(z)
+        kvq.dgap_distill_backward(x, torch.from_numpy(t).cuda(), torch.from_numpy(i).cuda(), 2.0, torch.from_numpy(lse).cuda(), x)
+        torch.cuda.synchronize()
+        assert (x.double().cpu().numpy() == want).all()
+        assert bool((base[:, :off] == 3.0).all()) and bool((base[:, off + v:] == 3.0).all())
+        base.fill_(3.0)
