@@ -240,8 +240,18 @@ def kvq_chunk_attention(cache: int, q, n_q: int, out, ws, ws_bytes: Optional[int
                                      _stream(stream)))
 
 
+_I32 = 1 << 31
+
+
+def _window_sizes(n_q, window, sinks):
+    """The sizes as the C interface takes them (ctypes would keep the lowest 32 bits of larger ones)."""
+    if not (-_I32 <= n_q < _I32 and -_I32 <= window < _I32 and -_I32 <= sinks < _I32):
+        raise ValueError(f"n_q = {n_q}, window = {window}, sinks = {sinks}: 32 bits each")
+    return int(n_q), int(window), int(sinks)
+
+
 def kvq_window_workspace_bytes(cache: int, n_q: int, window: int, sinks: int = 0) -> int:
-    return int(lib().kvq_window_workspace_bytes(cache, int(n_q), int(window), int(sinks)))
+    return int(lib().kvq_window_workspace_bytes(cache, *_window_sizes(n_q, window, sinks)))
 
 
 def _on_device(stream, call, *tensors) -> None:
@@ -273,8 +283,9 @@ def kvq_window_attention(cache: int, q, n_q: int, window: int, sinks: int, out, 
     ``sinks`` ones: q fp16 [batch][n_q][Hq][d], out fp32 [batch][n_q][Hq][d]."""
     if ws_bytes is None:
         ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    sizes = _window_sizes(n_q, window, sinks)
     _on_device(stream, lambda st: _check(lib().kvq_window_attention(
-        cache, _ptr(q), int(n_q), int(window), int(sinks), _ptr(out), _ptr(ws), int(ws_bytes), st)), q, out, ws)
+        cache, _ptr(q), *sizes, _ptr(out), _ptr(ws), int(ws_bytes), st)), q, out, ws)
 
 
 def kvq_append_decode(cache: int, K, V, n_new: Sequence[int], q, out, ws, ws_bytes: Optional[int] = None,
@@ -405,22 +416,23 @@ class KVCache:
         return made
 
     def _decode_buffers(self, stream, q, out):
-        """``out`` (made if None) and a workspace of a decode step: the cache's own on the stream that it was made on,
-        else one of the call's stream (two steps at once would write their records into the same one)."""
+        """``out`` (made if None), a workspace of a decode step and the call's stream: the cache's own workspace on the
+        stream that it was made on, else one of the call's stream (two steps at once would write their records into
+        the same one)."""
         import torch
         shape, at = (self.batch, self.num_q_heads, self.head_dim), _stream(stream)
         current = stream is None or at == _stream(None)
         if current and self.ws is None:
             self.workspace()
         if not current or at != self.ws_stream:
-            return self._buffers(stream, q.device, shape, out, kvq_workspace_bytes(self.handle))
+            return *self._buffers(stream, q.device, shape, out, kvq_workspace_bytes(self.handle)), at
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=q.device)
-        return out, self.workspace()
+        return out, self.workspace(), at
 
     def decode(self, q, out=None, stream=None):
-        out, ws = self._decode_buffers(stream, q, out)
-        kvq_decode_attention(self.handle, q, out, ws, stream=stream)
+        out, ws, at = self._decode_buffers(stream, q, out)
+        kvq_decode_attention(self.handle, q, out, ws, stream=at)
         return out
 
     def chunk(self, q, out=None, stream=None):
@@ -440,16 +452,21 @@ class KVCache:
         n_q = int(q.shape[1])
         if out is not None and (out.dtype != torch.float32 or out.shape != shape or not out.is_contiguous()):
             raise ValueError(f"out must be a contiguous float32 tensor of shape {shape}")
-        need = kvq_window_workspace_bytes(self.handle, n_q, window, sinks)
-        out, ws = self._buffers(stream, q.device, shape, out, need)
-        kvq_window_attention(self.handle, q, n_q, window, sinks, out, ws, stream=stream)
+        size = max(kvq_window_workspace_bytes(self.handle, n_q, window, sinks), 256)
+        if stream is not None:
+            out, ws = self._buffers(stream, q.device, shape, out, size)
+        else:
+            if out is None:
+                out = torch.empty(shape, dtype=torch.float32, device=q.device)
+            ws = torch.empty(size, dtype=torch.uint8, device=self.arena.device)
+        kvq_window_attention(self.handle, q, n_q, window, sinks, out, ws, size, stream=stream)
         return out
 
     def append_decode(self, K, V, q, n_new=None, out=None, stream=None):
         if n_new is None:
             n_new = [int(K.shape[1])] * self.batch
-        out, ws = self._decode_buffers(stream, q, out)
-        kvq_append_decode(self.handle, K, V, n_new, q, out, ws, stream=stream)
+        out, ws, at = self._decode_buffers(stream, q, out)
+        kvq_append_decode(self.handle, K, V, n_new, q, out, ws, stream=at)
         return out
 
     def seq_len(self, seq):
