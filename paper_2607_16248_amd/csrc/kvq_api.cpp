@@ -40,6 +40,7 @@ struct kvq_cache {
   std::vector<int32_t> L, Lq;
   std::vector<uint8_t> matrix;  // 1: the kernels of decode_mfma.hip (else decode_exact.hip)
   std::vector<uint8_t> window;  // 1: the many-row kernel serves its windowed queries
+  std::vector<std::pair<int, int>> classes;  // of equal key and value bits: the first sequence, how many there are
   std::vector<int> occupancy;    // resident decode workgroups per compute unit, per sequence's kernel
   int32_t split_tokens = 0;
   // paged layout: block table on the device (pm.table), page lists and the
@@ -440,6 +441,10 @@ kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena,
     const uint64_t head_bytes = c->paged ? packed_bytes : c->lay[i].stride;
     c->matrix.push_back(kvq::matrix_decode_supported(c->bk[i], c->bv[i], gq, d->key_group, d->value_group, head_bytes) ? 1 : 0);
     c->window.push_back(kvq::window_rows_supported(gq, d->key_group, d->value_group, head_bytes) ? 1 : 0);
+    auto same = [&](const std::pair<int, int>& cl) { return c->bk[cl.first] == c->bk[i] && c->bv[cl.first] == c->bv[i]; };
+    const auto cl = std::find_if(c->classes.begin(), c->classes.end(), same);
+    if (cl == c->classes.end()) c->classes.push_back({i, 1});
+    else ++cl->second;
   }
   // the split plan of a launch fills one round of its kernel's workgroups
   for (int i = 0; i < d->batch; ++i)
@@ -982,19 +987,17 @@ bool window_many_possible(const kvq_cache* c, int seq0, int nqry) {
 // lengths, grow with them.  (Without a limit: 64 sequences of 100 to 9000 tokens, five
 // queries, 12 rounds 198 us, 8 rounds 212; 32 of 500 to 8000, 64 queries, 356 us and
 // 349, in a workspace of 2.2 GB and 0.28; one sequence takes 7 rounds at most.)
-int64_t window_workgroups(size_t n) { return (n > 1 ? 16 : 8) * target_workgroups(1); }
+int64_t window_workgroups(int64_t n) { return (n > 1 ? 16 : 8) * target_workgroups(1); }
 
 // Most splits of all sequences of a windowed call together, at any lengths.
 int64_t window_records(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   const int64_t each = window_splits(c, nqry, window, sinks);
   if (c->split_tokens > 0) return c->d.batch * each;
-  std::map<std::pair<int, int>, std::vector<int>> classes;
-  for (int i = 0; i < c->d.batch; ++i) classes[{c->bk[i], c->bv[i]}].push_back(i);
   int64_t most = 0;
-  for (auto& cl : classes) {
+  for (const auto& cl : c->classes) {
     int64_t units = window_units(c, window_rows(c, nqry, false));
-    if (window_many_possible(c, cl.second[0], nqry)) units = std::min(units, window_units(c, window_rows(c, nqry, true)));
-    most += std::min<int64_t>((int64_t)cl.second.size() * each, window_workgroups(cl.second.size()) / units);
+    if (window_many_possible(c, cl.first, nqry)) units = std::min(units, window_units(c, window_rows(c, nqry, true)));
+    most += std::min<int64_t>(cl.second * each, window_workgroups(cl.second) / units);
   }
   return std::max<int64_t>(most, 1);
 }
@@ -1042,6 +1045,7 @@ WindowSplit split_window(const kvq_cache* c, const std::vector<int>& seqs, int n
   w.r = window_rows(c, nqry, many);
   const int64_t units = window_units(c, w.r);
   const int64_t least = many ? 1 : kMinGroupsPerSplit, rows = (int64_t)nqry * c->d.num_q_heads;
+  const int64_t most = window_workgroups((int64_t)seqs.size());
   const bool wide = c->bk[seqs[0]] + c->bv[seqs[0]] > 4;
   int64_t longest = 1;
   for (int i : seqs) {
@@ -1057,7 +1061,7 @@ WindowSplit split_window(const kvq_cache* c, const std::vector<int>& seqs, int n
       records += k > 1 ? k * rows : 0;
       merged += k > 1 ? rows : 0;
     }
-    if (ns > 1 && wgs > window_workgroups(seqs.size())) break;
+    if (ns > 1 && wgs > most) break;
     const double t = many ? window_many_us(wgs, n, wide, rows / c->d.num_kv_heads, records, merged)
                           : window_us(wgs, (n + least - 1) / least * (c->d.key_group / 32), merged);
     if (ns == 1 || t < w.us) w.us = t, w.per = n;
@@ -1276,11 +1280,9 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
   return no_memory();
 }
 
-size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) try {
+size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
   return (size_t)window_records(c, n_q, window, sinks) * c->d.num_q_heads * n_q * kvq::kRecFloats * sizeof(float);
-} catch (const std::bad_alloc&) {
-  return 0;
 }
 
 kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, int32_t window, int32_t sinks,
