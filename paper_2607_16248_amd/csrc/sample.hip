@@ -30,7 +30,7 @@
 //
 // What bounds it: latency, along one workgroup's dependent steps: of one row's 24
 // us (128256 fp32, top-k 50 and top-p 0.95, an input whose three searches all go by
-// digits; 19 to 20 over many inputs) max 3 and bins 5, then the ends 3.5,
+// digits; 19 to 21 over many inputs) max 3 and bins 5, then the ends 3.5,
 // listing 6 (the compares, at four waves per SIMD: with every load asked for at
 // once it takes as long) and the three searches 4, one step after the other.  Many
 // rows: 256 flat ones of 128256 fp16 60 us, of which 11 go to the first read (all
