@@ -1,6 +1,7 @@
 /*
  * dgap — the logit-side runtime step of DGAP on AMD Instinct MI355X
- * (gfx950), the token drawn from the logits it leaves (dgap_sample), and the
+ * (gfx950), penalties, biases and masks on logits (dgap_adjust), the token drawn
+ * from the logits they leave (dgap_sample), and the
  * Kullback-Leibler loss against a teacher's top logits, one term of what its
  * corrector is trained with (dgap_distill).  Plain C ABI, in the same library as
  * kvq.h.
@@ -144,6 +145,56 @@ size_t dgap_sample_workspace_bytes(int32_t batch, int32_t vocab);
  * KVQ_ERR_HIP.  Results are bitwise reproducible. */
 kvq_status dgap_sample(const dgap_sampling* p, int32_t* tokens, float* logprobs, void* ws, size_t ws_bytes,
                        void* stream);
+
+/* Rows of logits and what is changed in them before a token is drawn (device
+ * pointers; settings are arrays of `batch` values, one per row). */
+typedef struct {
+  const void* logits;       /* [batch] rows of `vocab` logits of `type`, row_stride elements apart */
+  int64_t row_stride;       /* >= vocab */
+  int32_t type;             /* dgap_type */
+  int32_t batch;            /* >= 1 */
+  int32_t vocab;            /* 1 .. 2^24 */
+  int32_t history;          /* entries of a row of `tokens`, 0 .. 2^24 */
+  const int32_t* tokens;    /* [batch][history] the row's tokens so far; NULL: none */
+  const int32_t* length;    /* how many of them there are (clipped to [0, history]); NULL: all */
+  const int32_t* prompt;    /* how many of those, the first ones, were given and not generated; NULL: 0 */
+  const float* repetition;  /* r > 0, finite; NULL: 1 */
+  const float* presence;    /* p, finite; NULL: 0 */
+  const float* frequency;   /* f, finite; NULL: 0 */
+  const int32_t* bias_token; /* [batch][biases] tokens; NULL: none */
+  const float* bias;        /* [batch][biases] */
+  const uint32_t* mask;     /* [mask_rows] rows of bits, mask_stride words apart: bit t % 32 of word t / 32 */
+  const int32_t* mask_row;  /* the row of `mask` that holds the row's bits; NULL: its own number */
+  int64_t mask_stride;      /* words, >= vocab / 32 rounded up; unused without mask */
+  int32_t biases;           /* 0 .. DGAP_MAX_BIASES */
+  int32_t mask_rows;        /* >= 1 with mask */
+} dgap_adjustment;
+
+/* Most biases per row. */
+#define DGAP_MAX_BIASES 65535
+
+/* Penalties for repeated tokens, biases and masks on rows of logits: what a decode
+ * step does between dgap_restore and dgap_sample ("DGAP Overview", online
+ * restoration framework: decoding proceeds from z~).  Of token t with logit z,
+ * seen anywhere in its row's history, and n times among the generated ones:
+ *   z1 = seen ? (z > 0 ? z / r : z r) : z      (repetition)
+ *   z2 = z1 - (f n + (n > 0 ? p : 0))          (frequency, presence)
+ *   z3 = z2 + bias of t                        (a bias of -inf gives -inf whatever z2 is)
+ *   out = its mask bit is 0 ? -inf : z3        (grammar)
+ * in fp32, rounded once to the logits' type (a token that nothing applies to keeps
+ * its bits).  Tokens outside [0, vocab) count for nothing, in the history and among
+ * the biases (rows of fewer); a token given several biases has the last of them.  A
+ * mask_row outside [0, mask_rows) leaves the row free.  A row whose mask leaves
+ * nothing is all -inf, for which dgap_sample gives token -1.  A row with a
+ * setting that is NaN or infinite, or with r <= 0, is written as NaN (-1 there,
+ * too).  Unlike dgap_restore's, these logits need not be finite.
+ * out: device rows of the logits' type, out_row_stride >= vocab elements apart;
+ * it may be the logits' own memory (row strides equal), but overlap them in no
+ * other way.  Results are bitwise reproducible; no workspace.
+ * Errors: KVQ_ERR_ARG (null pointers, shapes or type out of range, misaligned
+ * logits or out), KVQ_ERR_UNSUPPORTED (vocab above 2^24, 2^22 chunks of 8192 logits
+ * or more), KVQ_ERR_HIP. */
+kvq_status dgap_adjust(const dgap_adjustment* p, void* out, int64_t out_row_stride, void* stream);
 
 /* Most teacher entries per row. */
 #define DGAP_MAX_TEACHER 256

@@ -2,7 +2,9 @@
  * kvq — packed low-bit KV cache and attention over it for AMD Instinct
  * MI355X (gfx950): single-token decode, chunk queries (the last n_q tokens,
  * causal), windowed attention (a sliding window and first tokens that stay
- * visible) and a paged layout for serving.  Plain C ABI.
+ * visible), a paged layout for serving, appends that rotate queries and keys
+ * by their positions, and a second form of the cache with 8 bits an element and
+ * one scale for each block of tokens and head.  Plain C ABI.
  *
  * The computation is attention over a persistent low-bit KV cache.  The
  * paper evaluates KbVb caches, b-bit keys and b-bit values with
@@ -23,7 +25,8 @@
  *   - a token is quantized once it and its whole key group lie more than
  *     fp16_window tokens before the end of the sequence: the first
  *     Lq = key_group * floor(max(0, L - fp16_window) / key_group) tokens are
- *     packed, the remaining L - Lq (< fp16_window + key_group) stay fp16.
+ *     packed, the remaining L - Lq (< fp16_window + key_group) stay fp16
+ *     (after kvq_truncate, what was packed stays so).
  *
  * Conventions for every call:
  *   - Device pointers are HIP device pointers owned by the caller; the
@@ -110,6 +113,17 @@ int64_t kvq_seq_len(const kvq_cache* cache, int32_t seq);
  * slot can take a new sequence while the others keep decoding. */
 kvq_status kvq_seq_release(kvq_cache* cache, int32_t seq);
 
+/* Drop the newest tokens of every sequence (host bookkeeping only, no launch):
+ * sequence i keeps its first lens[i] ones, lens a host array [batch] with
+ * lens[i] between the tokens packed so far and its length.  What a program does
+ * after verifying drafted tokens (kvq_chunk_attention) with those that were
+ * rejected; an fp16_window of the longest draft keeps them out of the packed
+ * groups.  Packed groups stay: a sequence that later grows again packs the next
+ * group where it would have.  Errors, with nothing changed: KVQ_ERR_ARG (null
+ * pointers, a length below 0 or above the sequence's), KVQ_ERR_STATE (a length
+ * inside the packed tokens). */
+kvq_status kvq_truncate(kvq_cache* cache, const int32_t* lens);
+
 /* Free pages in the pool of a paged cache; -1 for a contiguous cache or
  * a NULL handle. */
 int64_t kvq_free_pages(const kvq_cache* cache);
@@ -131,6 +145,93 @@ int64_t kvq_free_pages(const kvq_cache* cache);
  * Prefill is an append with n_new = prompt length. */
 kvq_status kvq_append(kvq_cache* cache, const void* K, const void* V, int32_t n_max,
                       const int32_t* n_new, void* stream);
+
+/* Element types of the rows that kvq_append_rotary reads. */
+typedef enum { KVQ_F16 = 0, KVQ_BF16 = 1 } kvq_type;
+
+/* New tokens as a projection leaves them, and their rotation (device pointers). */
+typedef struct {
+  const void* q;            /* queries, [Hq][128] per token; NULL: keys and values alone */
+  const void* k;            /* keys, [Hkv][128] per token */
+  const void* v;            /* values, [Hkv][128] per token */
+  int64_t q_stride;         /* elements from one token's row to the next (row s * n_max + i is token */
+  int64_t k_stride;         /* i of sequence s), at least the row's own: rows of one buffer that */
+  int64_t v_stride;         /* holds q, k and v side by side have its width */
+  const float* cos_table;   /* [table_rows][rotary_dim / 2] */
+  const float* sin_table;
+  const int32_t* positions; /* [batch][n_max] rows of the tables; NULL: the token's place in its sequence */
+  int64_t table_rows;       /* >= 1 */
+  int32_t type;             /* kvq_type of q, k and v */
+  int32_t rotary_dim;       /* channels that turn, the first ones: a multiple of 16 up to 128 */
+  int32_t adjacent_pairs;   /* 0: channel c turns with c + rotary_dim / 2; 1: 2 c with 2 c + 1 */
+  int32_t pad;
+} kvq_rotary;
+
+/* kvq_append of rows that are rotated on the way, in the same launch: channels
+ * (a, b) of a pair j of token t become
+ *   a' = a cos[p][j] - b sin[p][j],   b' = a sin[p][j] + b cos[p][j],
+ * p the token's position, computed in 64 bits and rounded once to fp16; the other
+ * channels and the values are converted.  The cache then holds, byte for byte, what
+ * kvq_append of those fp16 rows leaves: any class, contiguous or paged, and
+ * block-scaled caches.  q_out: device fp16 [batch][n_max][Hq][128], 4-byte aligned, the
+ * rotated queries in the form that the attention calls take (rows past n_new[i]
+ * are left as they were); NULL where q is.  q_out may not overlap an input.
+ * n_max, n_new as in kvq_append.  Rows and tables need their elements' alignment.
+ * A given position outside the tables is taken as 0 and reported by kvq_check
+ * (KVQ_ERR_RANGE), as is what kvq_append reports.
+ * Errors, before anything is launched or changed: KVQ_ERR_ARG (null or misaligned
+ * pointers, strides, type, rotary_dim or table_rows out of range, places past the
+ * tables where positions is NULL), and kvq_append's. */
+kvq_status kvq_append_rotary(kvq_cache* cache, const kvq_rotary* r, int32_t n_max, const int32_t* n_new, void* q_out,
+                             void* stream);
+
+/* Element types of a block-scaled cache. */
+typedef enum {
+  KVQ_I8 = 0,   /* whole numbers -127 .. 127 */
+  KVQ_E4M3 = 1  /* 8-bit floating point, 4 exponent and 3 mantissa bits, largest 448, no infinity */
+} kvq_block_type;
+
+/* Shape and types of a block-scaled cache; fields as in kvq_cache_desc. */
+typedef struct {
+  int32_t batch;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;      /* 128 */
+  int32_t max_tokens;
+  int32_t block_tokens;  /* tokens that share a scale: 32, 64 or 128 */
+  int32_t fp16_window;
+  int32_t type_k;        /* kvq_block_type of the keys */
+  int32_t type_v;        /* of the values */
+  int32_t page_tokens;   /* 0, or a power of two >= block_tokens: paged */
+  int32_t num_pages;
+  int32_t pad;
+} kvq_block_desc;
+
+/* A cache that holds 8 bits an element and, for each block of block_tokens
+ * tokens and kv head, one fp32 scale of the keys and one of the values:
+ * s = max |x| over the block's tokens and channels / 127 (KVQ_I8) or / 448
+ * (KVQ_E4M3), rounded to fp32; the code is the number of the type that is nearest
+ * to x / s (ties to the even code; exactly), and stands for code * s.  Against an
+ * 8-bit class of kvq_cache_init it has 256 bytes and a quarter byte or less of
+ * scales per token and head (there 276 with groups of 32), and operands that need no zero-point;
+ * blocks in which one channel is far larger than the others keep fewer levels for
+ * those, e4m3 less so.  Blocks fill and leave the fp16 window as key groups do
+ * (key_group = block_tokens).  An element that is not finite makes its block's
+ * part zero and is reported by kvq_check (KVQ_ERR_RANGE).
+ * The handle goes to every call that takes a kvq_cache, with these differences:
+ * kvq_append_decode runs as kvq_append and kvq_decode_attention,
+ * kvq_decode_partials and kvq_decode_merge answer KVQ_ERR_UNSUPPORTED,
+ * kvq_dequant gives code * s rounded once to fp32, attention is within 1e-5
+ * (2-norm) of the exact one over these values, kvq_export's image is
+ *   key codes [Lq][128] | key scales [Lq/block_tokens] fp32 | value codes
+ *   [Lq][128] | value scales [Lq/block_tokens] fp32 | key tail [L-Lq][128] fp16 |
+ *   value tail [L-Lq][128] fp16
+ * (KVQ_I8 codes as two's complement bytes), and the workspaces of decode, chunk and
+ * window calls do not grow with the batch beyond what their splits write.
+ * Errors as kvq_cache_init's; kvq_block_cache_bytes gives 0 for an invalid
+ * descriptor. */
+size_t kvq_block_cache_bytes(const kvq_block_desc* desc);
+kvq_status kvq_block_cache_init(kvq_cache** out, const kvq_block_desc* desc, void* arena, size_t arena_bytes);
 
 /* Bytes of workspace kvq_decode_attention needs for any lengths up to
  * max_tokens under the current split setting. */

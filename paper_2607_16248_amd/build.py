@@ -1,7 +1,7 @@
 """Build the HIP library libkvq.so in-tree for gfx950.
 
 Every source is compiled by hipcc with packed fp32 ops disabled; the
-quantize-on-append source is also built with floating-point contraction
+quantize-on-append sources are also built with floating-point contraction
 off: the exact remainder that decides a 4- or 8-bit code takes its roundings
 one by one, fused only where it says so.  The decode sources are built assuming no NaN operands (queries are finite, cached
 values are finite by construction, and the only infinity, the -inf start of
@@ -42,6 +42,13 @@ SOURCES = [
     ("distill.hip", [], None),
     ("noalloc.hip", [], None),
     ("matrix_dispatch.cpp", [], None),
+    ("adjust.hip", [], None),
+    ("dgap_adjust.cpp", [], None),
+    ("kvq_rotary.cpp", [], None),
+    ("block_append.hip", ["-ffp-contract=off"], None),
+    ("block_tiles.hip", ["-fno-honor-nans"], None),
+    ("block_read.hip", [], None),
+    ("kvq_block.cpp", [], None),
     ("kvq_api.cpp", [], None),
 ] + [("decode_mfma.hip", ["-fno-honor-nans", f"-DKVQ_BK={bk}", f"-DKVQ_BV={bv}"], f"decode_mfma_k{bk}v{bv}.o")
      for bk, bv in MATRIX_CLASSES] + [
@@ -67,7 +74,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     workers = min(len(SOURCES), max(2, os.cpu_count() or 2))
     # the long compiles first, so that they start at once
-    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip", "window.hip"))
+    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip", "window.hip", "block_tiles.hip"))
     with cf.ThreadPoolExecutor(max_workers=workers) as ex:
         done = dict(zip(order, ex.map(lambda i: _compile(SOURCES[i][0], SOURCES[i][1], verbose, SOURCES[i][2]),
                                       order)))

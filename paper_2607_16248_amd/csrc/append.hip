@@ -33,6 +33,7 @@
 
 #include <type_traits>
 
+#include "append_common.h"
 #include "decode_common.h"
 #include "kvq_internal.h"
 #include "kvq_layout.h"
@@ -41,7 +42,6 @@ namespace kvq {
 namespace {
 
 typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ h2_t u2h(uint32_t v) { return __builtin_bit_cast(h2_t, v); }
 __device__ __forceinline__ uint32_t h2u(h2_t v) { return __builtin_bit_cast(uint32_t, v); }
@@ -204,35 +204,6 @@ __device__ __forceinline__ uint32_t quantize(float x, const Grid& g) {
   }
   return fi + (up ? 1u : 0u);
 }
-
-// 8 halves of a row at p: one 16-byte load, or halves (inputs that are not
-// 16-byte aligned).
-template <bool AL>
-__device__ __forceinline__ u4_t load8(const uint16_t* p) {
-  if constexpr (AL) return *reinterpret_cast<const u4_t*>(p);
-  u4_t v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
-  return v;
-}
-template <bool AL>
-__device__ __forceinline__ uint32_t load2(const uint16_t* p) {
-  if constexpr (AL) return *reinterpret_cast<const uint32_t*>(p);
-  return (uint32_t)p[0] | ((uint32_t)p[1] << 16);
-}
-
-// Row of token p: in the ring (appended by an earlier call) or in the input.
-struct Rows {
-  const uint16_t* in;    // input row of token L_old of this head
-  const uint16_t* ring;
-  size_t stride;         // halves from one input token to the next
-  int L_old, W;
-  bool fresh;            // none of the group's tokens sits in the ring (uniform)
-  __device__ __forceinline__ const uint16_t* at(int p) const {
-    if (!fresh && p < L_old) return ring + (size_t)(p % W) * kHeadDim;
-    return in + (size_t)(p - L_old) * stride;
-  }
-};
 
 // The lane's part of its key row dwords (kvq_layout.h: key_bit)
 // into the row at o: operand block kb, lane group g4.
@@ -471,16 +442,18 @@ __device__ __forceinline__ uint32_t quantize_values(const AppendArgs& a, int bv,
   }
 }
 
-template <int GK, bool AL>
-__device__ __forceinline__ void quantize_group(const AppendArgs& a, const AppendSeq& S, int h, int gi, int bk, int bv,
-                                               uint32_t* minmax, uint32_t* par) {
+// ROT: rows of a rotated append (rot), whose fresh keys turn as they are loaded.
+template <int GK, bool AL, bool ROT>
+__device__ __forceinline__ void quantize_group(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h, int gi,
+                                               int bk, int bv, uint32_t* minmax, uint32_t* par) {
   uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;  // the fp16 ring's region
   const int p0 = S.Lq_old + gi * GK;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cc = lane & 15, row = lane >> 4;
-  const size_t in0 = ((size_t)S.seq * a.n_max * a.hkv + h) * kHeadDim;
-  const Rows rk{a.K + in0, reinterpret_cast<const uint16_t*>(blk + region(a.tk)), (size_t)a.hkv * kHeadDim, S.L_old, a.W, p0 >= S.L_old};
-  const Rows rv{a.V + in0, reinterpret_cast<const uint16_t*>(blk + region(a.tv)), (size_t)a.hkv * kHeadDim, S.L_old, a.W, p0 >= S.L_old};
+  const size_t token0 = (size_t)S.seq * a.n_max, ks = ROT ? rot->k_stride : (size_t)a.hkv * kHeadDim,
+               vs = ROT ? rot->v_stride : (size_t)a.hkv * kHeadDim;
+  const Rows rk{a.K + token0 * ks + (size_t)h * kHeadDim, reinterpret_cast<const uint16_t*>(blk + region(a.tk)), ks, S.L_old, a.W, p0 >= S.L_old};
+  const Rows rv{a.V + token0 * vs + (size_t)h * kHeadDim, reinterpret_cast<const uint16_t*>(blk + region(a.tv)), vs, S.L_old, a.W, p0 >= S.L_old};
 
   u4_t kx[GK / 16];
 #pragma unroll
@@ -488,9 +461,26 @@ __device__ __forceinline__ void quantize_group(const AppendArgs& a, const Append
   uint32_t vx[8];
   auto load_v = [&](int b) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t) vx[t] = load2<AL>(rv.at(p0 + 32 * b + value_token(wv, t)) + 2 * lane);
+    for (int t = 0; t < 8; ++t) {
+      const int p = p0 + 32 * b + value_token(wv, t);
+      vx[t] = load2<AL>(rv.at(p) + 2 * lane);
+      if constexpr (ROT) {
+        if (p >= S.L_old) vx[t] = rotary::to_half2(vx[t], rot->bf16 != 0);
+      }
+    }
   };
   load_v(0);
+  if constexpr (ROT) {
+    const rotary::Turn turn(*rot, lane);
+#pragma unroll
+    for (int i = 0; i < GK / 16; ++i) {
+      const int p = p0 + 16 * i + 4 * wv + row;
+      if (p < S.L_old) continue;  // (the ring's keys have turned; 16 lanes share a token)
+      rotary::Angles g;
+      turn.load(*rot, rotary::table_row(*rot, a.arena, (int64_t)(token0 + (p - S.L_old)), p), g);
+      kx[i] = turn.apply(kx[i], g);
+    }
+  }
   uint32_t* bound = reinterpret_cast<uint32_t*>(blk + region(a.vb));
   const uint32_t seen = __hip_atomic_load(bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   // the packed segment (head region or page) of the group, and the group's
@@ -590,37 +580,8 @@ __device__ __forceinline__ void quantize_group(const AppendArgs& a, const Append
   }
 }
 
-// Copy part `part` (kCopyTokens tokens) of the new tokens that stay fp16 into
-// the ring of head h.
-template <bool AL>
-__device__ __forceinline__ void copy_ring(const AppendArgs& a, const AppendSeq& S, int h, int part) {
-  uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;
-  const int first = max(S.Lq_new, S.L_old) + part * kCopyTokens, end = min(S.L_new, first + kCopyTokens);
-  const size_t in0 = ((size_t)S.seq * a.n_max * a.hkv + h) * kHeadDim;
-  constexpr int kPer = kCopyTokens * (kHeadDim / 8) / kAppendThreads;  // 16-byte pieces per thread and tensor
-  u4_t x[2][kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int idx = i * kAppendThreads + threadIdx.x, p = first + (idx >> 4);
-    if (p < end) {
-      const size_t src = in0 + (size_t)(p - S.L_old) * a.hkv * kHeadDim + (idx & 15) * 8;
-      x[0][i] = load8<AL>(a.K + src);
-      x[1][i] = load8<AL>(a.V + src);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int idx = i * kAppendThreads + threadIdx.x, p = first + (idx >> 4);
-    if (p < end) {
-      const size_t dst = ((size_t)(p % a.W) * kHeadDim + (idx & 15) * 8) * 2;
-      *reinterpret_cast<u4_t*>(blk + region(a.tk) + dst) = x[0][i];
-      *reinterpret_cast<u4_t*>(blk + region(a.tv) + dst) = x[1][i];
-    }
-  }
-}
-
-template <int GK, bool AL>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int bk, int bv) {
+template <int GK, bool AL, bool ROT>
+__device__ __forceinline__ void append_group(const AppendArgs& a, const RotaryArgs* rot, int bk, int bv) {
   __shared__ __attribute__((aligned(16))) uint32_t minmax[4 * 128], par[192];
   const int wg = blockIdx.x;
   int si = 0;
@@ -630,10 +591,21 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
   const int local = wg - S.wg_begin, part = local / a.hkv, h = local - part * a.hkv;
   const int nquant = a.quantize ? S.n_quant : 0;
   if (part < nquant) {
-    quantize_group<GK, AL>(a, S, h, part, bk, bv, minmax, par);
-  } else {
-    copy_ring<AL>(a, S, h, part - nquant);
+    quantize_group<GK, AL, ROT>(a, rot, S, h, part, bk, bv, minmax, par);
+  } else if (!ROT || part < nquant + S.n_copy) {
+    copy_ring<AL, ROT>(a, rot, S, h, part - nquant);
+  } else if constexpr (ROT) {
+    rotary::turn_queries(a, *rot, S, h, part - nquant - S.n_copy);
   }
+}
+
+template <int GK, bool AL>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int bk, int bv) {
+  append_group<GK, AL, false>(a, nullptr, bk, bv);
+}
+template <int GK, bool AL>
+__global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(AppendArgs a, RotaryArgs rot, int bk, int bv) {
+  append_group<GK, AL, true>(a, &rot, bk, bv);
 }
 
 __global__ __launch_bounds__(256) void table_set_kernel(TableSet t) {
@@ -669,6 +641,30 @@ int launch_append(const AppendArgs& a, int bk, int bv, void* stream) {
     case 128:
       if (al) hipLaunchKernelGGL((append_kernel<128, true>), grid, block, 0, s, a, bk, bv);
       else hipLaunchKernelGGL((append_kernel<128, false>), grid, block, 0, s, a, bk, bv);
+      break;
+    default: return (int)hipErrorInvalidValue;
+  }
+  return (int)hipGetLastError();
+}
+
+int launch_append_rotary(const AppendArgs& a, const RotaryArgs* rot, int bk, int bv, void* stream) {
+  if (rot == nullptr) return launch_append(a, bk, bv, stream);
+  if (a.total_wg <= 0) return 0;
+  const bool al = rot->aligned != 0;
+  const dim3 grid(a.total_wg), block(kAppendThreads);
+  hipStream_t s = (hipStream_t)stream;
+  switch (a.gk) {
+    case 32:
+      if (al) hipLaunchKernelGGL((append_rotary_kernel<32, true>), grid, block, 0, s, a, *rot, bk, bv);
+      else hipLaunchKernelGGL((append_rotary_kernel<32, false>), grid, block, 0, s, a, *rot, bk, bv);
+      break;
+    case 64:
+      if (al) hipLaunchKernelGGL((append_rotary_kernel<64, true>), grid, block, 0, s, a, *rot, bk, bv);
+      else hipLaunchKernelGGL((append_rotary_kernel<64, false>), grid, block, 0, s, a, *rot, bk, bv);
+      break;
+    case 128:
+      if (al) hipLaunchKernelGGL((append_rotary_kernel<128, true>), grid, block, 0, s, a, *rot, bk, bv);
+      else hipLaunchKernelGGL((append_rotary_kernel<128, false>), grid, block, 0, s, a, *rot, bk, bv);
       break;
     default: return (int)hipErrorInvalidValue;
   }

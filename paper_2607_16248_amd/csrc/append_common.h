@@ -1,0 +1,85 @@
+// Pieces shared by the append kernels of the packed and the block-scaled caches:
+// row loads, and the copy of the tokens that stay fp16 into the ring.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "kvq_internal.h"
+#include "rotary.h"
+
+namespace kvq {
+namespace {
+
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+
+// 8 halves of a row at p: one 16-byte load, or halves (inputs that are not
+// 16-byte aligned).
+template <bool AL>
+__device__ __forceinline__ u4_t load8(const uint16_t* p) {
+  if constexpr (AL) return *reinterpret_cast<const u4_t*>(p);
+  u4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+  return v;
+}
+template <bool AL>
+__device__ __forceinline__ uint32_t load2(const uint16_t* p) {
+  if constexpr (AL) return *reinterpret_cast<const uint32_t*>(p);
+  return (uint32_t)p[0] | ((uint32_t)p[1] << 16);
+}
+
+// Row of token p: in the ring (appended by an earlier call) or in the input.
+struct Rows {
+  const uint16_t* in;    // input row of token L_old of this head
+  const uint16_t* ring;
+  size_t stride;         // halves from one input token to the next
+  int L_old, W;
+  bool fresh;            // none of the group's tokens sits in the ring (uniform)
+  __device__ __forceinline__ const uint16_t* at(int p) const {
+    if (!fresh && p < L_old) return ring + (size_t)(p % W) * kHeadDim;
+    return in + (size_t)(p - L_old) * stride;
+  }
+};
+
+// Copy part `part` (kCopyTokens tokens) of the new tokens that stay fp16 into
+// the ring of head h.
+template <bool AL, bool ROT>
+__device__ __forceinline__ void copy_ring(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h, int part) {
+  uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;
+  const int first = max(S.Lq_new, S.L_old) + part * kCopyTokens, end = min(S.L_new, first + kCopyTokens);
+  const size_t token0 = (size_t)S.seq * a.n_max, ks = ROT ? rot->k_stride : (size_t)a.hkv * kHeadDim,
+               vs = ROT ? rot->v_stride : (size_t)a.hkv * kHeadDim;
+  constexpr int kPer = kCopyTokens * (kHeadDim / 8) / kAppendThreads;  // 16-byte pieces per thread and tensor
+  u4_t x[2][kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int idx = i * kAppendThreads + threadIdx.x, p = first + (idx >> 4);
+    if (p < end) {
+      const size_t token = token0 + (p - S.L_old), at = (size_t)h * kHeadDim + (idx & 15) * 8;
+      x[0][i] = load8<AL>(a.K + token * ks + at);
+      x[1][i] = load8<AL>(a.V + token * vs + at);
+      if constexpr (ROT) {
+        const rotary::Turn turn(*rot, threadIdx.x & 63);
+        rotary::Angles g;
+        turn.load(*rot, rotary::table_row(*rot, a.arena, (int64_t)token, p), g);
+        x[0][i] = turn.apply(x[0][i], g);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) x[1][i][n] = rotary::to_half2(x[1][i][n], rot->bf16 != 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int idx = i * kAppendThreads + threadIdx.x, p = first + (idx >> 4);
+    if (p < end) {
+      const size_t dst = ((size_t)(p % a.W) * kHeadDim + (idx & 15) * 8) * 2;
+      *reinterpret_cast<u4_t*>(blk + region(a.tk) + dst) = x[0][i];
+      *reinterpret_cast<u4_t*>(blk + region(a.tv) + dst) = x[1][i];
+    }
+  }
+}
+
+}  // namespace
+}  // namespace kvq

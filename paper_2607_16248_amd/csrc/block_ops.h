@@ -1,0 +1,118 @@
+// Operand helpers of the block-scaled caches' attention: codes of 8 bits to exact
+// fp16 operands, queries lifted to full halves, the reference of the value scales.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "mfma_common.h"
+
+namespace kvq {
+namespace block_ops {
+
+using mfma_ops::f4_t;
+using mfma_ops::h2_t;
+using mfma_ops::h2u;
+using mfma_ops::h8_t;
+using mfma_ops::u2h;
+using mfma_ops::u4_t;
+
+// Eight codes (a byte each) as halves, exactly.  e4m3: the conversion instruction,
+// two elements each; whole numbers (held plus 128): the byte below the exponent of
+// 1024, less 1152, two instructions for two elements.
+template <bool E4M3>
+__device__ __forceinline__ h8_t operand(uint32_t lo, uint32_t hi) {
+  u4_t w;
+  if constexpr (E4M3) {
+    w[0] = h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
+    w[1] = h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
+    w[2] = h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
+    w[3] = h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
+  } else {
+    const h2_t c = {(_Float16)-1152.f, (_Float16)-1152.f};
+    w[0] = h2u(u2h(__builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) + c);
+    w[1] = h2u(u2h(__builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) + c);
+    w[2] = h2u(u2h(__builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) + c);
+    w[3] = h2u(u2h(__builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) + c);
+  }
+  return __builtin_bit_cast(h8_t, w);
+}
+
+// A row's query, times the power of two that puts its largest element at 2^14 or
+// above (elements 2^-28 of that and smaller would be subnormal halves, whose
+// products lose bits).  Returns the power's reciprocal.  The row's four lanes (16
+// apart) hold all of it.
+__device__ __forceinline__ float lift_query(u4_t (&q)[4]) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) top = max(top, max(q[kb][n] & 0x7FFFu, (q[kb][n] >> 16) & 0x7FFFu));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  if (top == 0u) return 1.f;
+  // exponent of the largest element: -24 .. 15
+  const int e = (int)(__builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)top)) >> 23) - 127;
+  const int up = 14 - e;  // -1 .. 38: in two steps of at most 2^15
+  if (up <= 0) return 1.f;
+  const int u0 = min(up, 15), u1 = min(up - u0, 15), u2 = up - u0 - u1;
+#pragma unroll
+  for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      h2_t x = u2h(q[kb][n]);
+      const _Float16 f0 = (_Float16)ldexpf(1.f, u0), f1 = (_Float16)ldexpf(1.f, u1), f2 = (_Float16)ldexpf(1.f, u2);
+      x = x * (h2_t){f0, f0};
+      x = x * (h2_t){f1, f1};
+      x = x * (h2_t){f2, f2};
+      q[kb][n] = h2u(x);
+    }
+  return ldexpf(1.f, -up);
+}
+
+// Two numbers as hi + lo halves (22 bits).  (A pair's hi halves are converted once:
+// left to itself, the compiler converts each a second time for the differences.)
+struct Halves {
+  uint32_t hi, lo;
+};
+__device__ __forceinline__ Halves split(float a, float b) {
+  Halves h;
+  h.hi = h2u((h2_t){(_Float16)a, (_Float16)b});
+  asm("" : "+v"(h.hi));
+  const h2_t x = u2h(h.hi);
+  h.lo = h2u((h2_t){(_Float16)fmaf((float)x.x, -1.f, a), (_Float16)fmaf((float)x.y, -1.f, b)});
+  return h;
+}
+
+// Accumulators are sums of weights times codes in units of a reference value
+// scale: a block's own scale enters its weights' exponent (up = log2 of scale over
+// reference, down = 2^-up for the sum of the weights).  A scale more than 4 times
+// off the reference becomes the reference; rescale() is then its change, else 1.
+struct ValueUnit {
+  float ref = 1.f, up = 0.f, down = 1.f;
+  bool set = false;
+  // the factor that the accumulators take
+  __device__ __forceinline__ float next(float scale) {
+    up = 0.f;
+    down = 1.f;
+    if (!(scale > 0.f)) return 1.f;  // (a block of zeros adds nothing in any unit)
+    if (!set) {
+      set = true;
+      ref = scale;
+      return 1.f;
+    }
+    const float ratio = scale * __builtin_amdgcn_rcpf(ref);
+    if (ratio <= 4.f && ratio >= 0.25f) {
+      up = __builtin_amdgcn_logf(ratio);
+      down = __builtin_amdgcn_exp2f(-up);
+      return 1.f;
+    }
+    const float f = ref / scale;
+    ref = scale;
+    return f;
+  }
+};
+
+}  // namespace block_ops
+}  // namespace kvq

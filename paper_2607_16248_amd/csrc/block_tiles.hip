@@ -1,0 +1,325 @@
+// Attention of few rows over a block-scaled cache (gfx950; include/kvq.h states
+// both): single-token decode, chunk queries and windows, up to 16 or 32 (query, head)
+// rows of a kv head.
+//
+//   S^T = K Q^T   (16 tokens x 16 rows; codes as exact halves, q as the fp16 it is)
+//   p = 2^(s_k c S + log2(s_v / ref) - m),   O^T += V^T P^T   (p in hi + lo halves)
+//
+// with s_k, s_v the block's scales: one number each for all 32 tokens that a wave
+// takes at a time, so they enter as factors of scores and weights, and codes stay
+// the integers (or e4m3 numbers) they are.  Products are transposed, so a lane's
+// weights are the next product's operand without a lane exchange.  A lane reads 16
+// consecutive bytes of a key row (any order of channels does, the query has the
+// same), and values lie in operand order (kvq_layout.h, block_value).
+//
+// A workgroup's four waves take 32-token blocks in turn; the next block's codes are
+// asked for before this one's are used.  One launch where a sequence has one split:
+// its workgroup adds the fp16 tail (tail_mfma.h) and writes the output.
+#include <hip/hip_runtime.h>
+
+#include "block_ops.h"
+#include "decode_common.h"
+#include "kvq_internal.h"
+#include "kvq_layout.h"
+#include "mfma_common.h"
+#include "tail_mfma.h"
+
+namespace kvq {
+namespace {
+
+using namespace dec;
+using block_ops::f4_t;
+using block_ops::h2_t;
+using block_ops::h8_t;
+using block_ops::u4_t;
+using mfma_ops::mfma;
+
+constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ratio up to 4
+constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
+constexpr float kNoScore = -1e30f;  // below any score
+constexpr int kPartRows = 8;        // rows of one pass of the cross-wave reduction
+
+// What a wave reads of a 32-token block.
+struct Codes {
+  u4_t k[4];  // token half, 64-channel half
+  u4_t v[4];  // pieces
+};
+
+// NT: tiles of 16 rows.
+template <bool K8, bool V8, int NT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 4))) void block_tiles_kernel(DecodeArgs a) {
+  __shared__ __attribute__((aligned(16))) Reduce<kPartRows> red;
+  const Work wk = find_work<true, true>(a);
+  const DecodeSeq& S = a.seq[wk.si];
+  const uint8_t* ring = a.arena + S.head0 + (uint64_t)wk.h * a.head_stride;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, blk = lane >> 4;
+  const int rows = a.qpr * a.gqh;  // of the group
+  const int inv = (65536 + a.gqh - 1) / a.gqh;
+  const size_t rec_rows = (size_t)a.hq * a.nqry;
+
+  const int seen0 = S.L - a.nqry + 1;
+  const int first_limit = seen0 + min(wk.rg * a.qpr, a.nqry - 1);
+  const int last_limit = seen0 + min(wk.rg * a.qpr + a.qpr - 1, a.nqry - 1);
+  const int gsh = __builtin_ctz(a.gk), bsh = gsh - 5;
+  const WindowGroups wg = window_groups(first_limit, last_limit, S.Lq, gsh, a.window, a.sinks);
+  // 32-token blocks of this split, every fourth one this wave's
+  const int gps = a.split_tokens >> gsh;
+  const int i0 = ((wk.sp * gps) << bsh) + wv, iend = min(wg.count, wk.sp * gps + gps) << bsh;
+  const int nblocks = i0 < iend ? (iend - i0 + kWaves - 1) / kWaves : 0;
+  auto token_of = [&](int i) {
+    i = i0 + kWaves * i;
+    const int j = i >> bsh;
+    return (i << 5) + (j < wg.sink ? 0 : (wg.first - wg.sink) << gsh);
+  };
+
+  // The page of block i's tokens; paged or not, one scalar load (of any word, times
+  // 0 bytes), asked for a block ahead of the loads that need it.
+  typedef const __attribute__((address_space(4))) int32_t scalar_t;
+  typedef const __attribute__((address_space(4))) float scalar_f;
+  const bool paged = a.pm.table != nullptr;
+  const uint8_t* head = a.arena + (paged ? a.pm.pool0 + (uint64_t)wk.h * a.pm.page_head_bytes : S.head0 + (uint64_t)wk.h * a.head_stride);
+  scalar_t* table = (scalar_t*)(paged ? a.pm.table + (size_t)S.seq * a.pm.max_pages : reinterpret_cast<const int32_t*>(ring + region(a.vb)));
+  const int page_shift = paged ? a.pm.page_shift : 31, in_page = paged ? a.pm.page_tokens - 1 : 0x7FFFFFFF;
+  const uint64_t page_bytes = paged ? a.pm.page_bytes : 0;
+  auto page_of = [&](int i) { return table[token_of(i) >> page_shift]; };
+  const uint32_t k_at = col * kHeadDim + 16 * blk, v_at = lane * 16;
+  auto load = [&](int i, int page, Codes& o, float& sk, float& sv) __attribute__((always_inline)) {
+    const int t = token_of(i) & in_page;
+    const uint8_t* seg = head + (uint64_t)(uint32_t)page * page_bytes;
+    const uint8_t* kr = seg + region(a.kc) + (size_t)t * kHeadDim;
+    const uint8_t* vr = seg + region(a.vc) + (size_t)t * kHeadDim;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o.k[n] = *reinterpret_cast<const u4_t*>(kr + (n >> 1) * 16 * kHeadDim + (n & 1) * 64 + k_at);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o.v[n] = *reinterpret_cast<const u4_t*>(vr + n * 1024 + v_at);
+    scalar_f* sc = (scalar_f*)(seg + region(a.km) + (size_t)(t >> gsh) * 8);
+    sk = sc[0];
+    sv = sc[1];
+  };
+  Codes cur;
+  float sk = 0.f, sv = 0.f;
+  int page = 0;
+  if (nblocks > 0) {  // under way before the queries are here
+    page = page_of(0);
+    load(0, page, cur, sk, sv);
+    page = page_of(min(1, nblocks - 1));
+  }
+
+  // rows 16 u + col of the group: query operands and limits (rows past whole
+  // queries, and queries past the last, repeat the last query)
+  u4_t q[NT][4];
+  int lim[NT];
+  float ksc[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    typedef u4_t u4_any __attribute__((aligned(4)));
+    const int g = 16 * u + col, x = (g * inv) >> 16, j = min(wk.rg * a.qpr + (x < a.qpr ? x : kSpareRow), a.nqry - 1);
+    lim[u] = seen0 + j;
+    const uint16_t* qr = a.q + (((size_t)S.seq * a.nqry + j) * a.hq + wk.h * a.gqh + (g - x * a.gqh)) * kHeadDim + 16 * blk;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) q[u][kb] = *reinterpret_cast<const u4_any*>(qr + 64 * (kb >> 1) + 8 * (kb & 1));
+    ksc[u] = a.qscale * block_ops::lift_query(q[u]);
+  }
+
+  float m[NT], most[NT], l[NT];
+  f4_t acc[NT][8];
+  block_ops::ValueUnit unit;
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    m[u] = most[u] = kNoScore;
+    l[u] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc[u][t] = (f4_t){0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto attend = [&](int i, const Codes& x, float s_k, float s_v) __attribute__((always_inline)) {
+    const float change = unit.next(s_v);
+    if (change != 1.f) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[u][t] *= change;
+    }
+    f4_t d[NT][2];
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) d[u][mb] = (f4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        const u4_t w = x.k[2 * mb + (kb >> 1)];
+        const h8_t k8 = block_ops::operand<K8>(w[2 * (kb & 1)], w[2 * (kb & 1) + 1]);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) d[u][mb] = mfma(k8, __builtin_bit_cast(h8_t, q[u][kb]), d[u][mb]);
+      }
+    }
+    const int tok = token_of(i);
+    if (tok + 32 > first_limit || (tok < last_limit - a.window && tok + 32 > a.sinks)) {
+      // token tok + 16mb + 4blk + r is visible below the limit, from the window's
+      // begin on or below the sinks' end
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        const int left = lim[u] - tok - 4 * blk, from = max(lim[u] - a.window, 0) - tok - 4 * blk, sunk = a.sinks - tok - 4 * blk;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int n = 16 * (e >> 2) + (e & 3);
+          float s = n < left && (n >= from || n < sunk) ? d[u][e >> 2][e & 3] : -__builtin_inff();
+          asm volatile("" : "+v"(s));  // (a branch: blocks within every window pass it by)
+          d[u][e >> 2][e & 3] = s;
+        }
+      }
+    }
+    h8_t ph[NT], pl[NT];
+    float top[NT], f[NT];
+    bool over = false;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      f[u] = ksc[u] * (s_k > 0.f ? s_k : 1.f);  // (a block of zeros has scores 0 at any scale; a hidden token's is -inf)
+      const f4_t y = d[u][0], z = d[u][1];
+      top[u] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
+      top[u] = fmaxf(top[u] * f[u], kNoScore);
+      most[u] = fmaxf(most[u], top[u]);
+      over |= top[u] - m[u] > kTop;
+    }
+    if (__builtin_amdgcn_ballot_w64(over)) {
+      // the rows' maxima over their four lanes; rows above the limit move their reference
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        float t = fmaxf(top[u], __shfl_xor(top[u], 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float mn = t - m[u] > kTop ? t + (kHeadroom - kTop) : m[u];
+        const float alpha = __builtin_amdgcn_exp2f(m[u] - mn);
+        m[u] = mn;
+        l[u] *= alpha;
+#pragma unroll
+        for (int t2 = 0; t2 < 8; ++t2) acc[u][t2] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const float bias = unit.up - m[u];
+      float sum = 0.f;
+      u4_t hw, lw;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float s0 = d[u][t >> 1][2 * (t & 1)], s1 = d[u][t >> 1][2 * (t & 1) + 1];
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s0, f[u], bias)), p1 = __builtin_amdgcn_exp2f(fmaf(s1, f[u], bias));
+        sum += p0 + p1;
+        const block_ops::Halves h = block_ops::split(p0, p1);
+        hw[t] = h.hi;
+        lw[t] = h.lo;
+      }
+      l[u] = fmaf(sum, unit.down, l[u]);
+      ph[u] = __builtin_bit_cast(h8_t, hw);
+      pl[u] = __builtin_bit_cast(h8_t, lw);
+    }
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      const u4_t w = x.v[mb >> 1];
+      const h8_t v8 = block_ops::operand<V8>(w[2 * (mb & 1)], w[2 * (mb & 1) + 1]);
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        acc[u][mb] = mfma(v8, ph[u], acc[u][mb]);
+        acc[u][mb] = mfma(v8, pl[u], acc[u][mb]);
+      }
+    }
+  };
+
+  for (int i = 0; i < nblocks; ++i) {
+    Codes next;
+    float nk, nv;
+    load(min(i + 1, nblocks - 1), page, next, nk, nv);  // (after the last block: that one again, unused)
+    page = page_of(min(i + 2, nblocks - 1));
+    attend(i, cur, sk, sv);
+    cur = next;
+    sk = nk;
+    sv = nv;
+  }
+
+  TailState<NT> st;
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    l[u] += __shfl_xor(l[u], 16);
+    l[u] += __shfl_xor(l[u], 32);
+    most[u] = fmaxf(most[u], __shfl_xor(most[u], 16));
+    most[u] = fmaxf(most[u], __shfl_xor(most[u], 32));
+    const float to_max = l[u] > 0.f ? __builtin_amdgcn_exp2f(m[u] - most[u]) : 0.f;  // records are relative to the maximum
+    st.m[u] = l[u] > 0.f ? most[u] : -__builtin_inff();
+    st.l[u] = l[u] * to_max;
+    const float f = unit.ref * to_max;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) st.acc[u][t] = acc[u][t] * f;
+  }
+  if (S.L > S.Lq && wk.sp == S.nsplit - 1) {  // the fp16 tail: the last split's, or all of it
+    TailState<NT> tail;
+    tail_split<NT, 16 * NT, true, 4, true>(a, S, wk.h, wk.rg, ring, tail, lane, wv);
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const float top = fmaxf(st.m[u], tail.m[u]);  // (-inf in a wave that read nothing)
+      const float f = st.l[u] > 0.f ? __builtin_amdgcn_exp2f(st.m[u] - top) : 0.f;
+      const float ft = tail.l[u] > 0.f ? __builtin_amdgcn_exp2f(tail.m[u] - top) : 0.f;
+      st.m[u] = top;
+      st.l[u] = st.l[u] * f + tail.l[u] * ft;
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st.acc[u][t][r] = st.acc[u][t][r] * f + tail.acc[u][t][r] * ft;
+    }
+  }
+
+  // the waves' results of rows r0 .. r0 + 7, merged into records (a sequence of one
+  // split: into the output; every row sees a token, l > 0)
+  auto write_rows = [&](int r0) {
+    for (int idx = threadIdx.x; idx < kPartRows * kHeadDim; idx += blockDim.x) {
+      const int r = idx / kHeadDim, c = idx % kHeadDim, g = r0 + r;
+      const int x = (g * inv) >> 16, j = wk.rg * a.qpr + x;
+      if (g >= rows || j >= a.nqry) continue;
+      float M = -__builtin_inff();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, red.m[w][r]);
+      float val = 0.f, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = red.m[w][r] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(red.m[w][r] - M);
+        val = fmaf(f, red.acc[w][idx], val);
+        sum = fmaf(f, red.l[w][r], sum);
+      }
+      const size_t row = (size_t)j * a.hq + wk.h * a.gqh + g - x * a.gqh;
+      if (S.nsplit == 1) {
+        a.out[((size_t)S.seq * rec_rows + row) * kHeadDim + c] = val / sum;
+      } else {
+        float* rec = a.ws + ((size_t)(S.ws_base + wk.sp) * rec_rows + row) * kRecFloats;
+        rec[4 + c] = val;
+        if (c == 0) { rec[0] = M; rec[1] = sum; }
+      }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < NT; ++u)
+    for (int r0 = 16 * u; r0 < min(rows, 16 * u + 16); r0 += kPartRows) {
+      __syncthreads();
+      stage_tail<kPartRows, NT>(st, u, r0, red, lane, wv);
+      __syncthreads();
+      write_rows(r0);
+    }
+}
+
+template <bool K8, bool V8>
+int launch_types(const DecodeArgs& a, int rows, void* stream) {
+  const dim3 grid(a.total_wg), block(64 * kWaves);
+  if (rows > 16) hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 2>), grid, block, 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 1>), grid, block, 0, (hipStream_t)stream, a);
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_block_tiles(const DecodeArgs& a, int type_k, int type_v, int rows, void* stream) {
+  if (a.total_wg <= 0) return 0;
+  if (type_k == kBlockE4M3)
+    return type_v == kBlockE4M3 ? launch_types<true, true>(a, rows, stream) : launch_types<true, false>(a, rows, stream);
+  return type_v == kBlockE4M3 ? launch_types<false, true>(a, rows, stream) : launch_types<false, false>(a, rows, stream);
+}
+
+}  // namespace kvq

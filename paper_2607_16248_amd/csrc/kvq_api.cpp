@@ -12,6 +12,7 @@
 #include <cstdio>
 #include <cstring>
 #include <map>
+#include <memory>
 #include <new>
 #include <string>
 #include <utility>
@@ -19,44 +20,31 @@
 
 #include "dgap.h"
 #include "kvq.h"
+#include "kvq_host.h"
 #include "kvq_internal.h"
 #include "kvq_layout.h"
 
 using kvq::HeadLayout;
+using kvq::check_rows;
+using kvq::fail;
+using kvq::hip_fail;
+using kvq::kMaxSplits;
+using kvq::log2_exact;
+using kvq::no_memory;
+using kvq::ok;
+using kvq::packed_len;
+using kvq::target_workgroups;
 
 static_assert(kvq::kScratchBytes == KVQ_NOALLOC_SCRATCH_BYTES, "scratch array size as the header states");
 static_assert(kvq::kDistillMaxK == DGAP_MAX_TEACHER, "teacher entries as the header states");
 static_assert(kvq::kSpareRow >= KVQ_MAX_CHUNK, "a spare row lies past every chunk query");
 
-struct kvq_cache {
-  kvq_cache_desc d{};
-  std::vector<uint8_t> bk, bv;
-  uint8_t* arena = nullptr;
-  size_t arena_bytes = 0;
-  int64_t cq = 0;   // most tokens ever packed per sequence
-  int32_t W = 0;    // ring slots per head
-  std::vector<uint64_t> head0;
-  std::vector<HeadLayout> lay;
-  std::vector<int32_t> L, Lq;
-  std::vector<uint8_t> matrix;  // 1: the kernels of decode_mfma.hip (else decode_exact.hip)
-  std::vector<uint8_t> window;  // 1: the many-row kernel serves its windowed queries
-  std::vector<std::pair<int, int>> classes;  // of equal key and value bits: the first sequence, how many there are
-  std::vector<int> occupancy;    // resident decode workgroups per compute unit, per sequence's kernel
-  int32_t split_tokens = 0;
-  // paged layout: block table on the device (pm.table), page lists and the
-  // free pool on the host
-  bool paged = false;
-  kvq::PageMap pm{};
-  std::vector<std::vector<int32_t>> pages;  // per sequence: pool page of each logical page
-  std::vector<int32_t> free_pages;           // taken from the back
-};
+namespace kvq {
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-constexpr int kMaxSplits = 512;          // packed splits per sequence and kv head
-constexpr int kMinGroupsPerSplit = 4;    // one key group per wave at least
 // Decode workgroups that fit the current device at once (one round of the
 // grid): compute units times the resident workgroups per unit (one 4-wave
 // workgroup per wave slot of a SIMD).
@@ -95,8 +83,29 @@ kvq_status ok() {
   g_err.clear();
   return KVQ_OK;
 }
+const char* last_error() { return g_err.c_str(); }
 
-bool valid_bits(int b) { return b == 1 || b == 2 || b == 4 || b == 8; }
+int64_t packed_capacity(const kvq_cache_desc* d) {
+  const int64_t past = (int64_t)d->max_tokens - d->fp16_window;
+  return past <= 0 ? 0 : past / d->key_group * d->key_group;
+}
+
+int32_t quantized_len(int64_t L, const kvq_cache_desc& d) {
+  const int64_t past = L - d.fp16_window;
+  return past <= 0 ? 0 : (int32_t)(past / d.key_group * d.key_group);
+}
+
+int log2_exact(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+
+kvq_status hip_fail(int e, const char* what) {
+  return fail(KVQ_ERR_HIP, "%s: %s", what, hipGetErrorString((hipError_t)e));
+}
+
+static bool valid_bits(int b) { return b == 1 || b == 2 || b == 4 || b == 8; }
 
 kvq_status check_desc(const kvq_cache_desc* d) {
   if (!d) return fail(KVQ_ERR_ARG, "descriptor is NULL");
@@ -136,19 +145,38 @@ kvq_status check_desc(const kvq_cache_desc* d) {
   return KVQ_OK;
 }
 
-int64_t packed_capacity(const kvq_cache_desc* d) {
-  const int64_t past = (int64_t)d->max_tokens - d->fp16_window;
-  return past <= 0 ? 0 : past / d->key_group * d->key_group;
+// Rows of logits that a call reads whole.
+kvq_status check_rows(const void* logits, int type, int64_t row_stride, int rows, int vocab, const char* what) {
+  if (!logits) return fail(KVQ_ERR_ARG, "logits is NULL");
+  if (type != DGAP_F32 && type != DGAP_F16 && type != DGAP_BF16) return fail(KVQ_ERR_ARG, "type %d is none of dgap_type", type);
+  if (rows < 1) return fail(KVQ_ERR_ARG, "%s must be >= 1 (got %d)", what, rows);
+  if (vocab < 1) return fail(KVQ_ERR_ARG, "vocab must be >= 1 (got %d)", vocab);
+  if (vocab > 1 << 24) return fail(KVQ_ERR_UNSUPPORTED, "vocab %d above 2^24", vocab);
+  if (row_stride < vocab) return fail(KVQ_ERR_ARG, "row_stride %lld smaller than vocab %d", (long long)row_stride, vocab);
+  // (a launch's threads, up to 1024 for 8192 logits, stay below 2^32)
+  if ((int64_t)rows * ((vocab + 8191) / 8192) >= (int64_t)1 << 22)
+    return fail(KVQ_ERR_UNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
+  const int size = type == DGAP_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % size != 0) return fail(KVQ_ERR_ARG, "logits must be aligned to their type");
+  return KVQ_OK;
 }
 
-int32_t quantized_len(int64_t L, const kvq_cache_desc& d) {
-  const int64_t past = L - d.fp16_window;
-  return past <= 0 ? 0 : (int32_t)(past / d.key_group * d.key_group);
-}
+}  // namespace kvq
 
-HeadLayout layout_of(const kvq_cache_desc* d, int bk, int bv) {
-  return kvq::head_layout(bk, bv, packed_capacity(d), d->key_group, d->value_group,
-                          (int64_t)d->fp16_window + d->key_group);
+namespace {
+
+using kvq::check_desc;
+using kvq::packed_capacity;
+using kvq::quantized_len;
+
+constexpr int kMinGroupsPerSplit = 4;    // one key group per wave at least
+// Layout of `tokens` packed tokens and `w` ring slots of a head.
+HeadLayout layout_for(const kvq_cache_desc* d, int bk, int bv, int64_t tokens, int64_t w, bool with_bound, bool block) {
+  return block ? kvq::block_layout(tokens, d->key_group, w, with_bound)
+               : kvq::head_layout(bk, bv, tokens, d->key_group, d->value_group, w, with_bound);
+}
+HeadLayout layout_of(const kvq_cache_desc* d, int bk, int bv, bool block) {
+  return layout_for(d, bk, bv, packed_capacity(d), (int64_t)d->fp16_window + d->key_group, true, block);
 }
 
 // Arena of a paged cache: header | fp16 rings [batch][Hkv] | block table
@@ -159,12 +187,12 @@ struct PagedArena {
   int32_t max_pages = 0, num_pages = 0;
 };
 
-PagedArena paged_arena(const kvq_cache_desc* d) {
+PagedArena paged_arena(const kvq_cache_desc* d, bool block) {
   PagedArena A;
   const int bk = d->bits_k[0], bv = d->bits_v[0], P = d->page_tokens;
   const int64_t W = (int64_t)d->fp16_window + d->key_group;
-  A.page = kvq::head_layout(bk, bv, P, d->key_group, d->value_group, 0, false);
-  A.ring = kvq::head_layout(bk, bv, 0, d->key_group, d->value_group, W);
+  A.page = layout_for(d, bk, bv, P, 0, false, block);
+  A.ring = layout_for(d, bk, bv, 0, W, true, block);
   A.seq_lay = A.page;
   A.seq_lay.tk = A.ring.tk;
   A.seq_lay.tv = A.ring.tv;
@@ -178,12 +206,6 @@ PagedArena paged_arena(const kvq_cache_desc* d) {
   A.page_bytes = (uint64_t)d->num_kv_heads * A.page.stride;
   A.total = A.pool0 + (uint64_t)A.num_pages * A.page_bytes;
   return A;
-}
-
-int log2_exact(int v) {
-  int s = 0;
-  while ((1 << s) < v) ++s;
-  return s;
 }
 
 // Split length of one launch's sequences (one bit class): the launch fills
@@ -252,10 +274,6 @@ int64_t splits_bound(const kvq_cache* c) {
   return nq + 1;
 }
 
-kvq_status hip_fail(int e, const char* what) {
-  return fail(KVQ_ERR_HIP, "%s: %s", what, hipGetErrorString((hipError_t)e));
-}
-
 // Sequences grouped by (key bits, value bits), each class in chunks that fit
 // one kernel-argument block.
 std::vector<std::pair<std::pair<int, int>, std::vector<int>>> bit_classes(const kvq_cache* c,
@@ -270,22 +288,6 @@ std::vector<std::pair<std::pair<int, int>, std::vector<int>>> bit_classes(const 
     }
   }
   return out;
-}
-
-// Rows of logits that a call reads whole.
-kvq_status check_rows(const void* logits, int type, int64_t row_stride, int rows, int vocab, const char* what) {
-  if (!logits) return fail(KVQ_ERR_ARG, "logits is NULL");
-  if (type != DGAP_F32 && type != DGAP_F16 && type != DGAP_BF16) return fail(KVQ_ERR_ARG, "type %d is none of dgap_type", type);
-  if (rows < 1) return fail(KVQ_ERR_ARG, "%s must be >= 1 (got %d)", what, rows);
-  if (vocab < 1) return fail(KVQ_ERR_ARG, "vocab must be >= 1 (got %d)", vocab);
-  if (vocab > 1 << 24) return fail(KVQ_ERR_UNSUPPORTED, "vocab %d above 2^24", vocab);
-  if (row_stride < vocab) return fail(KVQ_ERR_ARG, "row_stride %lld smaller than vocab %d", (long long)row_stride, vocab);
-  // (a launch's threads, up to 1024 for 8192 logits, stay below 2^32)
-  if ((int64_t)rows * ((vocab + 8191) / 8192) >= (int64_t)1 << 22)
-    return fail(KVQ_ERR_UNSUPPORTED, "%d rows of %d logits are too many for one call", rows, vocab);
-  const int size = type == DGAP_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(logits) % size != 0) return fail(KVQ_ERR_ARG, "logits must be aligned to their type");
-  return KVQ_OK;
 }
 
 kvq_status check_scratch(const void* ws, size_t ws_bytes, size_t need) {
@@ -375,40 +377,41 @@ bool matrix_decode_supported(int bk, int bv, int gq, int gk, int gv, uint64_t he
 }
 }  // namespace kvq
 
-extern "C" {
+namespace kvq {
 
-size_t kvq_cache_bytes(const kvq_cache_desc* d) {
+size_t arena_bytes(const kvq_cache_desc* d, bool block) {
   if (check_desc(d) != KVQ_OK) return 0;
-  if (d->page_tokens > 0) return (size_t)paged_arena(d).total;
+  if (d->page_tokens > 0) return (size_t)paged_arena(d, block).total;
   uint64_t total = kvq::kHeaderBytes;
-  for (int i = 0; i < d->batch; ++i) total += (uint64_t)d->num_kv_heads * layout_of(d, d->bits_k[i], d->bits_v[i]).stride;
+  for (int i = 0; i < d->batch; ++i) total += (uint64_t)d->num_kv_heads * layout_of(d, d->bits_k[i], d->bits_v[i], block).stride;
   return (size_t)total;
 }
 
-kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena, size_t arena_bytes) {
+kvq_status init_cache(kvq_cache** out, const kvq_cache_desc* d, void* arena, size_t bytes, bool block) {
   if (!out) return fail(KVQ_ERR_ARG, "out is NULL");
   *out = nullptr;
   const kvq_status st = check_desc(d);
   if (st != KVQ_OK) return st;
   if (!arena) return fail(KVQ_ERR_ARG, "arena is NULL");
   if (reinterpret_cast<uintptr_t>(arena) % kvq::kAlign != 0) return fail(KVQ_ERR_ARG, "arena must be 256-byte aligned");
-  const size_t need = kvq_cache_bytes(d);
-  if (arena_bytes < need)
-    return fail(KVQ_ERR_CAPACITY, "arena holds %zu bytes, the cache needs %zu", arena_bytes, need);
-  kvq_cache* c = new kvq_cache();
+  const size_t need = arena_bytes(d, block);
+  if (bytes < need)
+    return fail(KVQ_ERR_CAPACITY, "arena holds %zu bytes, the cache needs %zu", bytes, need);
+  std::unique_ptr<kvq_cache> owner(new kvq_cache());
+  kvq_cache* c = owner.get();
   c->d = *d;
   c->bk.assign(d->bits_k, d->bits_k + d->batch);
   c->bv.assign(d->bits_v, d->bits_v + d->batch);
   c->d.bits_k = c->bk.data();
   c->d.bits_v = c->bv.data();
   c->arena = static_cast<uint8_t*>(arena);
-  c->arena_bytes = arena_bytes;
+  c->arena_bytes = bytes;
   c->cq = packed_capacity(d);
   c->W = d->fp16_window + d->key_group;
   uint64_t off = kvq::kHeaderBytes;
   uint64_t packed_bytes = 0;  // what the matrix kernel's 32-bit offsets must reach (one buffer resource)
   if (d->page_tokens > 0) {
-    const PagedArena A = paged_arena(d);
+    const PagedArena A = paged_arena(d, block);
     c->paged = true;
     c->pm.table = reinterpret_cast<const int32_t*>(c->arena + A.table_off);
     c->pm.pool0 = A.pool0;
@@ -429,7 +432,7 @@ kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena,
     packed_bytes = A.page.stride;  // one page's region of one kv head, whatever the pool size
   } else {
     for (int i = 0; i < d->batch; ++i) {
-      c->lay.push_back(layout_of(d, c->bk[i], c->bv[i]));
+      c->lay.push_back(layout_of(d, c->bk[i], c->bv[i], block));
       c->head0.push_back(off);
       off += (uint64_t)d->num_kv_heads * c->lay.back().stride;
     }
@@ -451,8 +454,20 @@ kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena,
     c->occupancy.push_back(c->matrix[i] ? kvq::matrix_decode_occupancy(c->bk[i], c->bv[i], d->key_group,
                                                                        d->num_q_heads / d->num_kv_heads)
                                         : 2);
-  *out = c;
+  *out = owner.release();
   return ok();
+}
+
+}  // namespace kvq
+
+extern "C" {
+
+size_t kvq_cache_bytes(const kvq_cache_desc* d) { return kvq::arena_bytes(d, false); }
+
+kvq_status kvq_cache_init(kvq_cache** out, const kvq_cache_desc* d, void* arena, size_t arena_bytes) try {
+  return kvq::init_cache(out, d, arena, arena_bytes, false);
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
 void kvq_cache_destroy(kvq_cache* c) { delete c; }
@@ -494,8 +509,25 @@ int64_t kvq_free_pages(const kvq_cache* c) {
   return (int64_t)c->free_pages.size();
 }
 
-kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max, const int32_t* n_new,
-                      void* stream) {
+kvq_status kvq_truncate(kvq_cache* c, const int32_t* lens) {
+  if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
+  if (!lens) return fail(KVQ_ERR_ARG, "lens is NULL");
+  for (int i = 0; i < c->d.batch; ++i) {
+    if (lens[i] < 0 || lens[i] > c->L[i])
+      return fail(KVQ_ERR_ARG, "sequence %d: length %d outside [0, %d]", i, lens[i], c->L[i]);
+    if (lens[i] < c->Lq[i])
+      return fail(KVQ_ERR_STATE, "sequence %d: length %d is below its %d packed tokens", i, lens[i], c->Lq[i]);
+  }
+  std::copy(lens, lens + c->d.batch, c->L.begin());
+  return ok();
+}
+
+}  // extern "C"
+
+namespace kvq {
+
+kvq_status append_tokens(kvq_cache* c, const void* K, const void* V, int32_t n_max, const int32_t* n_new,
+                         const RotaryArgs* rot, AppendLaunch launch, void* stream) {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!n_new) return fail(KVQ_ERR_ARG, "n_new is NULL");
   if (n_max < 0) return fail(KVQ_ERR_ARG, "n_max must be >= 0");
@@ -518,7 +550,7 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max,
   int64_t pages_needed = 0;
   for (int i = 0; i < d.batch; ++i) {
     L_new[i] = c->L[i] + n_new[i];
-    Lq_new[i] = quantized_len(L_new[i], d);
+    Lq_new[i] = packed_len(c, i, L_new[i]);
     if (n_new[i] > 0) seqs.push_back(i);
     // a launch that both packs and fills the ring must not overwrite a slot
     // it still reads: safe when the tokens span at most the ring, or when
@@ -530,6 +562,8 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max,
   if (c->paged && pages_needed > (int64_t)c->free_pages.size())
     return fail(KVQ_ERR_CAPACITY, "the append needs %lld more pages, the pool has %zu free", (long long)pages_needed,
                 c->free_pages.size());
+  const auto classes = bit_classes(c, seqs);  // (no memory is asked for once anything has changed)
+  for (int i = 0; c->paged && i < d.batch; ++i) c->pages[i].reserve((Lq_new[i] + d.page_tokens - 1) / d.page_tokens);
   {
     // a sequence's first packed group starts a fresh bound on its value
     // scales (after kvq_seq_release or kvq_cache_reset the old one is stale)
@@ -578,7 +612,7 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max,
   const int phases = fused ? 1 : 2;
   for (int ph = 0; ph < phases; ++ph) {
     const bool quant = fused || ph == 0, copy = fused || ph == 1;
-    for (auto& cls : bit_classes(c, seqs)) {
+    for (auto& cls : classes) {
       kvq::AppendArgs a{};
       const HeadLayout& lay = c->lay[cls.second[0]];
       a.arena = c->arena;
@@ -599,12 +633,13 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max,
         s.n_quant = (Lq_new[i] - c->Lq[i]) / d.key_group;
         const int32_t stay = L_new[i] - std::max(Lq_new[i], c->L[i]);
         s.n_copy = copy ? (stay + kvq::kCopyTokens - 1) / kvq::kCopyTokens : 0;
+        s.n_query = rot && rot->q && ph == 0 ? (n_new[i] + kvq::kQueryTokens - 1) / kvq::kQueryTokens : 0;
         s.wg_begin = wg;
-        wg += ((quant ? s.n_quant : 0) + s.n_copy) * d.num_kv_heads;
+        wg += ((quant ? s.n_quant : 0) + s.n_copy + s.n_query) * d.num_kv_heads;
       }
       a.nseq = n;
       a.total_wg = wg;
-      const int e = kvq::launch_append(a, cls.first.first, cls.first.second, stream);
+      const int e = launch(a, rot, cls.first.first, cls.first.second, stream);
       if (e) return hip_fail(e, "append launch");
     }
   }
@@ -615,8 +650,23 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max,
   return ok();
 }
 
+}  // namespace kvq
+
+extern "C" {
+
+kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int32_t n_max, const int32_t* n_new,
+                      void* stream) try {
+  const auto packed = [](const kvq::AppendArgs& a, const kvq::RotaryArgs*, int bk, int bv, void* s) {
+    return kvq::launch_append(a, bk, bv, s);
+  };
+  return kvq::append_tokens(c, K, V, n_max, n_new, nullptr, c && c->block ? c->block->append : packed, stream);
+} catch (const std::bad_alloc&) {
+  return no_memory();
+}
+
 size_t kvq_workspace_bytes(const kvq_cache* c) {
   if (!c) return 0;
+  if (c->block) return c->block->bound(c, 1, -1, 0);
   return (size_t)c->d.batch * c->d.num_q_heads * (size_t)splits_bound(c) * kvq::kRecFloats * sizeof(float);
 }
 
@@ -1158,6 +1208,7 @@ kvq_status kvq_decode_attention(const kvq_cache* c, const void* q, float* out, v
                                 void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
+  if (c->block) return c->block->attend(c, q, 1, -1, 0, out, ws, ws_bytes, stream);
   const SplitPlan p = plan_splits(c);
   kvq_status st = run_partials(c, p, q, ws, ws_bytes, stream);
   if (st != KVQ_OK) return st;
@@ -1171,14 +1222,16 @@ kvq_status kvq_decode_attention(const kvq_cache* c, const void* q, float* out, v
 kvq_status kvq_decode_attention_noalloc(const kvq_cache* c, const void* q, float* out, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!q || !out) return fail(KVQ_ERR_ARG, "q and out must be device pointers");
-  const SplitPlan p = plan_splits(c);
-  const size_t need = (size_t)p.records * c->d.num_q_heads * kvq::kRecFloats * sizeof(float);
+  const SplitPlan p = c->block ? SplitPlan{} : plan_splits(c);
+  const size_t need = c->block ? c->block->need(c, 1, -1, 0)
+                               : (size_t)p.records * c->d.num_q_heads * kvq::kRecFloats * sizeof(float);
   if (need > kvq::kScratchBytes)
     return fail(KVQ_ERR_CAPACITY, "this decode needs %zu bytes of workspace, more than the %zu bytes of the "
                 "library's scratch array; use kvq_decode_attention with a caller workspace", need, kvq::kScratchBytes);
   void* ws = nullptr;
   const int e = kvq::scratch_workspace(&ws);
   if (e) return hip_fail(e, "scratch array address");
+  if (c->block) return c->block->attend(c, q, 1, -1, 0, out, ws, kvq::kScratchBytes, stream);
   kvq_status st = run_partials(c, p, q, ws, kvq::kScratchBytes, stream);
   if (st != KVQ_OK) return st;
   st = run_merge(c, p, ws, out, stream);
@@ -1189,7 +1242,7 @@ kvq_status kvq_decode_attention_noalloc(const kvq_cache* c, const void* q, float
 }
 
 kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t n_max, const int32_t* n_new,
-                             const void* q, float* out, void* ws, size_t ws_bytes, void* stream) {
+                             const void* q, float* out, void* ws, size_t ws_bytes, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
   if (!n_new) return fail(KVQ_ERR_ARG, "n_new is NULL");
   if (n_max < 0) return fail(KVQ_ERR_ARG, "n_max must be >= 0");
@@ -1203,7 +1256,7 @@ kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t
       return fail(KVQ_ERR_CAPACITY, "sequence %d: %d + %d tokens exceed max_tokens = %d", i, c->L[i], n_new[i],
                   d.max_tokens);
     any |= n_new[i] > 0;
-    flush |= quantized_len(c->L[i] + n_new[i], d) != c->Lq[i];
+    flush |= packed_len(c, i, (int64_t)c->L[i] + n_new[i]) != c->Lq[i];
   }
   if (any && (!K || !V)) return fail(KVQ_ERR_ARG, "K and V must be device pointers");
   if (any && (reinterpret_cast<uintptr_t>(K) % 4 != 0 || reinterpret_cast<uintptr_t>(V) % 4 != 0))
@@ -1214,15 +1267,24 @@ kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t
   const std::vector<int32_t> L_old = c->L, Lq_old = c->Lq;
   for (int i = 0; i < d.batch; ++i) {
     c->L[i] = L_old[i] + n_new[i];
-    c->Lq[i] = quantized_len(c->L[i], d);
+    c->Lq[i] = packed_len(c, i, c->L[i]);
   }
-  const SplitPlan p = plan_splits(c);
-  const size_t need = (size_t)p.records * d.num_q_heads * kvq::kRecFloats * sizeof(float);
+  SplitPlan p;
+  size_t need = 0;
+  try {
+    p = c->block ? SplitPlan{} : plan_splits(c);
+    need = c->block ? c->block->need(c, 1, -1, 0) : (size_t)p.records * d.num_q_heads * kvq::kRecFloats * sizeof(float);
+  } catch (const std::bad_alloc&) {
+    c->L = L_old;
+    c->Lq = Lq_old;
+    throw;
+  }
   const char* bad = nullptr;
   kvq_status bad_st = KVQ_ERR_ARG;
   if (need > 0 && !ws) bad = "workspace is NULL";
   else if (ws_bytes < need) bad = "workspace too small for the lengths after the append", bad_st = KVQ_ERR_CAPACITY;
   else if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) bad = "workspace must be 16-byte aligned";
+  flush |= c->block != nullptr;  // (they have no fused step)
   if (bad || flush) {
     c->L = L_old;
     c->Lq = Lq_old;
@@ -1239,10 +1301,13 @@ kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t
   st = run_merge(c, p, ws, out, stream);
   if (st != KVQ_OK) return st;
   return ok();
+} catch (const std::bad_alloc&) {
+  return no_memory();
 }
 
 kvq_status kvq_decode_partials(const kvq_cache* c, const void* q, void* ws, size_t ws_bytes, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
+  if (c->block) return fail(KVQ_ERR_UNSUPPORTED, "a block-scaled cache has no split records");
   const kvq_status st = run_partials(c, plan_splits(c), q, ws, ws_bytes, stream);
   return st == KVQ_OK ? ok() : st;
 } catch (const std::bad_alloc&) {
@@ -1251,6 +1316,7 @@ kvq_status kvq_decode_partials(const kvq_cache* c, const void* q, void* ws, size
 
 kvq_status kvq_decode_merge(const kvq_cache* c, const void* ws, float* out, void* stream) try {
   if (!c) return fail(KVQ_ERR_ARG, "cache is NULL");
+  if (c->block) return fail(KVQ_ERR_UNSUPPORTED, "a block-scaled cache has no split records");
   const kvq_status st = run_merge(c, plan_splits(c), ws, out, stream);
   return st == KVQ_OK ? ok() : st;
 } catch (const std::bad_alloc&) {
@@ -1259,6 +1325,7 @@ kvq_status kvq_decode_merge(const kvq_cache* c, const void* ws, float* out, void
 
 size_t kvq_chunk_workspace_bytes(const kvq_cache* c, int32_t n_q) {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK) return 0;
+  if (c->block) return c->block->bound(c, n_q, -1, 0);
   return kvq_workspace_bytes(c) * (size_t)n_q;
 }
 
@@ -1270,6 +1337,7 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
   for (int i = 0; i < c->d.batch; ++i)
     if (c->L[i] < n_q)
       return fail(KVQ_ERR_ARG, "sequence %d holds %d tokens, fewer than the %d chunk queries", i, c->L[i], n_q);
+  if (c->block) return c->block->attend(c, q, n_q, -1, 0, out, ws, ws_bytes, stream);
   const SplitPlan p = plan_splits(c, n_q, ws_bytes);
   kvq_status st = run_partials(c, p, q, ws, ws_bytes, stream, nullptr, out);
   if (st != KVQ_OK) return st;
@@ -1282,6 +1350,7 @@ kvq_status kvq_chunk_attention(const kvq_cache* c, const void* q, int32_t n_q, f
 
 size_t kvq_window_workspace_bytes(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   if (!c || n_q < 1 || n_q > KVQ_MAX_CHUNK || window < 1 || sinks < 0) return 0;
+  if (c->block) return c->block->bound(c, n_q, window, sinks);
   return (size_t)window_records(c, n_q, window, sinks) * c->d.num_q_heads * n_q * kvq::kRecFloats * sizeof(float);
 }
 
@@ -1300,6 +1369,7 @@ kvq_status kvq_window_attention(const kvq_cache* c, const void* q, int32_t n_q, 
   }
   window = std::min(window, longest);
   sinks = std::min(sinks, longest);
+  if (c->block) return c->block->attend(c, q, n_q, window, sinks, out, ws, ws_bytes, stream);
   const SplitPlan p = plan_window(c, n_q, window, sinks);
   kvq_status st = run_window(c, p, q, window, sinks, out, ws, ws_bytes, stream);
   if (st != KVQ_OK) return st;
@@ -1329,8 +1399,8 @@ kvq_status kvq_dequant(const kvq_cache* c, int32_t seq, int32_t tok0, int32_t nt
   a.kc = kvq::region_units(lay.kc); a.km = kvq::region_units(lay.km); a.vc = kvq::region_units(lay.vc);
   a.vm = kvq::region_units(lay.vm); a.tk = kvq::region_units(lay.tk); a.tv = kvq::region_units(lay.tv);
   a.hkv = c->d.num_kv_heads; a.gk = c->d.key_group; a.gv = c->d.value_group; a.W = c->W;
-  a.bk = c->bk[seq]; a.bv = c->bv[seq]; a.Lq = c->Lq[seq]; a.tok0 = tok0; a.ntok = ntok;
-  const int e = kvq::launch_dequant(a, stream);
+  a.bk = c->block ? c->type_k : c->bk[seq]; a.bv = c->block ? c->type_v : c->bv[seq]; a.Lq = c->Lq[seq]; a.tok0 = tok0; a.ntok = ntok;
+  const int e = c->block ? c->block->dequant(a, stream) : kvq::launch_dequant(a, stream);
   if (e) return hip_fail(e, "dequant launch");
   return ok();
 }
@@ -1338,6 +1408,7 @@ kvq_status kvq_dequant(const kvq_cache* c, int32_t seq, int32_t tok0, int32_t nt
 size_t kvq_export_bytes(const kvq_cache* c, int32_t seq, int32_t h) {
   if (!c || seq < 0 || seq >= c->d.batch || h < 0 || h >= c->d.num_kv_heads) return 0;
   const size_t Lq = c->Lq[seq], tail = c->L[seq] - c->Lq[seq], D = kvq::kHeadDim;
+  if (c->block) return Lq * 2 * D + Lq / c->d.key_group * 2 * sizeof(float) + tail * D * 2 * 2;
   return Lq * 16 * c->bk[seq] + Lq / c->d.key_group * 2 * D * 2 + Lq * 16 * c->bv[seq] +
          Lq * (D / c->d.value_group) * 4 + tail * D * 2 * 2;
 }
@@ -1361,13 +1432,21 @@ kvq_status kvq_export(const kvq_cache* c, int32_t seq, int32_t h, void* dst, siz
   x.vc_out = x.km_out + Lq / c->d.key_group * 2 * D * 2;
   x.vm_out = x.vc_out + Lq * 16 * c->bv[seq];
   x.tk_out = x.vm_out + Lq * (D / c->d.value_group) * 4;
+  if (c->block) {  // key codes, scales, value codes, scales, then the tails
+    x.vc_out = x.km_out + Lq / c->d.key_group * sizeof(float);
+    x.vm_out = x.vc_out + Lq * D;
+    x.tk_out = x.vm_out + Lq / c->d.key_group * sizeof(float);
+    x.bk = c->type_k;
+    x.bv = c->type_v;
+  }
   x.tv_out = x.tk_out + tail * D * 2;
   x.kc = kvq::region_units(lay.kc); x.km = kvq::region_units(lay.km); x.vc = kvq::region_units(lay.vc);
   x.vm = kvq::region_units(lay.vm); x.tk = kvq::region_units(lay.tk); x.tv = kvq::region_units(lay.tv);
-  x.bk = c->bk[seq]; x.bv = c->bv[seq]; x.gk = c->d.key_group; x.gv = c->d.value_group; x.W = c->W;
+  if (!c->block) x.bk = c->bk[seq], x.bv = c->bv[seq];
+  x.gk = c->d.key_group; x.gv = c->d.value_group; x.W = c->W;
   x.Lq = (int32_t)Lq; x.ntail = (int32_t)tail; x.seq = seq; x.h = h;
   x.pm = c->pm;
-  const int e = kvq::launch_export(x, stream);
+  const int e = c->block ? c->block->export_image(x, stream) : kvq::launch_export(x, stream);
   if (e) return hip_fail(e, "export launch");
   return ok();
 }
@@ -1524,7 +1603,7 @@ kvq_status dgap_distill_backward(const dgap_distillation* p, const float* lse, c
   return ok();
 }
 
-const char* kvq_last_error(void) { return g_err.c_str(); }
+const char* kvq_last_error(void) { return kvq::last_error(); }
 
 kvq_status kvq_read_probe(const void* src, size_t bytes, uint32_t* sink, void* stream) {
   if (!src || !sink) return fail(KVQ_ERR_ARG, "src and sink must be device pointers");

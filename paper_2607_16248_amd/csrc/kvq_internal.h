@@ -62,6 +62,27 @@ inline HeadLayout head_layout(int bk, int bv, int64_t cq, int gk, int gv, int64_
   return L;
 }
 
+// Block-scaled caches: 8 bits an element and one fp32 scale of the keys and one
+// of the values for each key group (block) of tokens and head, with
+//   kc  key codes    [Cq][128]       token rows
+//   km  scales       [Cq/Gk][2]      keys', values' (fp32)
+//   vc  value codes  [Cq/32][4096]   blocks of 32 tokens, kvq_layout.h
+// (whole numbers are held plus 128, e4m3 as it is), the rings as above, and
+// nothing at vm and vb.
+inline HeadLayout block_layout(int64_t cq, int gk, int64_t w, bool with_bound) {
+  HeadLayout L{};
+  uint64_t o = 0;
+  L.kc = o; o = align_up(o + (uint64_t)cq * kHeadDim, kAlign);
+  L.km = o; o = align_up(o + (uint64_t)(cq / gk) * 8, kAlign);
+  L.vc = o; o = align_up(o + (uint64_t)cq * kHeadDim, kAlign);
+  L.vm = o;
+  L.tk = o; o = align_up(o + (uint64_t)w * kHeadDim * 2, kAlign);
+  L.tv = o; o = align_up(o + (uint64_t)w * kHeadDim * 2, kAlign);
+  L.vb = o; o = with_bound ? align_up(o + 4, kAlign) : o;
+  L.stride = o;
+  return L;
+}
+
 // ---------------------------------------------------------------- paging
 //
 // Paged caches keep the packed codes and scales of page_tokens consecutive
@@ -113,6 +134,7 @@ struct TableSet {
 
 constexpr int kAppendThreads = 256;
 constexpr int kCopyTokens = 32;  // ring tokens one copy workgroup of a head writes
+constexpr int kQueryTokens = 16;  // tokens whose queries of one kv head a workgroup rotates
 
 struct AppendSeq {
   uint64_t head0;     // arena offset of (seq, head 0)
@@ -121,6 +143,7 @@ struct AppendSeq {
   int32_t wg_begin;   // first workgroup of this sequence
   int32_t n_quant;    // key groups to pack per head
   int32_t n_copy;     // copy workgroups per head in this launch (ring slots written: kCopyTokens each)
+  int32_t n_query;    // query workgroups per head (rotated appends)
 };
 
 struct AppendArgs {
@@ -133,6 +156,22 @@ struct AppendArgs {
   int32_t quantize;   // 1: pack groups in this launch
   PageMap pm;
   AppendSeq seq[kMaxSeqPerLaunch];
+};
+
+// Rotated appends: the rows that AppendArgs' K and V stand for, and the angles.
+// A row is a token's heads, contiguous; rows are `stride` elements apart over
+// [batch][n_max].
+struct RotaryArgs {
+  const uint16_t* q;      // or null
+  uint16_t* q_out;        // fp16 [batch][n_max][Hq][128]
+  const float* cos_;      // [rows][rot / 2]
+  const float* sin_;
+  const int32_t* position;  // [batch][n_max] rows of the tables; null: the token's place in its sequence
+  int64_t q_stride, k_stride, v_stride;
+  int64_t rows;
+  int32_t rot, pairs;     // channels rotated; 1: neighbours, 0: c and c + rot / 2
+  int32_t bf16, gqh;      // inputs' type; query heads per kv head
+  int32_t aligned, pad;   // rows can be read 16 bytes at a time
 };
 
 // ---------------------------------------------------------------- decode
@@ -281,6 +320,30 @@ struct SampleArgs {
   int32_t unit;              // masses are in units of 2^-unit of the largest weight
 };
 
+// ---------------------------------------------------------------- adjusted logits
+
+constexpr int kAdjustChunk = 4096;  // logits per workgroup
+
+struct AdjustArgs {
+  const void* logits;
+  void* out;
+  int64_t row_stride, out_stride;  // elements
+  const int32_t* tokens;
+  const int32_t* length;
+  const int32_t* prompt;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_token;
+  const float* bias;
+  const uint32_t* mask;
+  const int32_t* mask_row;
+  int64_t mask_stride;             // words
+  int32_t batch, vocab, history, biases, mask_rows;
+  int32_t nchunk;                  // chunks of a row
+  int32_t runs;                    // 1: runs of 8 logits lie alike in memory, in and out (16-byte accesses)
+};
+
 // ---------------------------------------------------------------- teacher loss
 
 constexpr int kDistillChunk = 8192;  // logits per workgroup
@@ -340,6 +403,15 @@ struct ExportArgs {
 
 // Launchers (defined next to their kernels).  Return a hipError_t as int.
 int launch_append(const AppendArgs& a, int bk, int bv, void* stream);
+// The same with rotated keys and queries.
+int launch_append_rotary(const AppendArgs& a, const RotaryArgs* rot, int bk, int bv, void* stream);
+// The same for block-scaled caches, by element types; their reads; their attention
+// (tiles of up to 16 or 32 rows; many rows).
+constexpr int kBlockE4M3 = 1;  // KVQ_E4M3
+int launch_append_block(const AppendArgs& a, const RotaryArgs* rot, int type_k, int type_v, void* stream);
+int launch_dequant_block(const struct DequantArgs& a, void* stream);
+int launch_export_block(const struct ExportArgs& a, void* stream);
+int launch_block_tiles(const DecodeArgs& a, int type_k, int type_v, int rows, void* stream);
 int launch_table_set(const TableSet& t, void* stream);
 // Zero the given 32-bit words of the arena (byte offsets), up to kTableSetMax per launch.
 struct WordReset {
@@ -386,6 +458,7 @@ int launch_export(const ExportArgs& a, void* stream);
 int launch_merge(const MergeArgs& a, void* stream);
 int launch_dgap(const struct DgapArgs& a, int batch, void* stream);
 int launch_sample(const SampleArgs& a, int type, void* stream);
+int launch_adjust(const AdjustArgs& a, int type, void* stream);
 int launch_distill(const DistillArgs& a, int type, void* stream);
 int launch_dequant(const DequantArgs& a, void* stream);
 int launch_fill_zero(void* dst, size_t words, void* stream);

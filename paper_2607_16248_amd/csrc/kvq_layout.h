@@ -161,4 +161,13 @@ KVQ_HD inline int value_meta_pos(int r) { return 8 * ((r & 15) >> 2) + 4 * (r >>
 KVQ_HD inline int value_meta_s(int g, int r) { return (g * 32 + value_meta_pos(r)) * 2; }
 KVQ_HD inline int value_meta_z(int g, int r, int ng) { return (ng * 32 + g * 32 + value_meta_pos(r)) * 2; }
 
+// Block-scaled caches: byte of block token r (0..31), channel c in a 4096-byte
+// block of value codes.  Lane c % 16 + 16 kg of an operand holds 16 bytes of each
+// of four pieces, piece i the operands mb = 2 i and 2 i + 1, so that a wave reads a
+// piece in one go.
+KVQ_HD inline int block_value(int r, int c) {
+  const int kg = (r & 15) >> 2, e = (r & 3) + 4 * (r >> 4), mb = c >> 4;
+  return (mb >> 1) * 1024 + ((c & 15) + 16 * kg) * 16 + 8 * (mb & 1) + e;
+}
+
 }  // namespace kvq

@@ -19,7 +19,8 @@ STATUS_NAMES = ["KVQ_OK", "KVQ_ERR_ARG", "KVQ_ERR_UNSUPPORTED", "KVQ_ERR_CAPACIT
                 "KVQ_ERR_RANGE", "KVQ_ERR_STATE", "KVQ_ERR_HIP"]
 
 EXPORTED = ["kvq_cache_bytes", "kvq_cache_init", "kvq_cache_destroy", "kvq_cache_reset",
-            "kvq_seq_len", "kvq_seq_release", "kvq_free_pages",
+            "kvq_seq_len", "kvq_seq_release", "kvq_truncate", "kvq_free_pages",
+            "kvq_block_cache_bytes", "kvq_block_cache_init", "kvq_append_rotary",
             "kvq_append", "kvq_workspace_bytes", "kvq_decode_attention", "kvq_decode_attention_noalloc",
             "kvq_append_decode",
             "kvq_decode_partials", "kvq_decode_merge", "kvq_chunk_workspace_bytes", "kvq_chunk_attention",
@@ -28,7 +29,7 @@ EXPORTED = ["kvq_cache_bytes", "kvq_cache_init", "kvq_cache_destroy", "kvq_cache
             "kvq_set_split_tokens", "kvq_last_error", "kvq_version",
             "kvq_read_probe", "kvq_read_probe_sink_bytes",
             "dgap_workspace_bytes", "dgap_info_floats", "dgap_restore",
-            "dgap_sample_workspace_bytes", "dgap_sample",
+            "dgap_sample_workspace_bytes", "dgap_sample", "dgap_adjust",
             "dgap_distill_workspace_bytes", "dgap_distill", "dgap_distill_backward"]
 
 
@@ -46,6 +47,33 @@ class CacheDesc(ctypes.Structure):
                 ("value_group", ctypes.c_int32), ("fp16_window", ctypes.c_int32),
                 ("bits_k", ctypes.POINTER(ctypes.c_uint8)), ("bits_v", ctypes.POINTER(ctypes.c_uint8)),
                 ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class BlockDesc(ctypes.Structure):
+    """kvq_block_desc of include/kvq.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("batch", "num_q_heads", "num_kv_heads", "head_dim", "max_tokens", "block_tokens", "fp16_window",
+                 "type_k", "type_v", "page_tokens", "num_pages", "pad")]
+
+
+class Rotary(ctypes.Structure):
+    """kvq_rotary of include/kvq.h (device pointers)."""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int64), ("type", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("adjacent_pairs", ctypes.c_int32), ("pad", ctypes.c_int32)]
+
+
+class DgapAdjustment(ctypes.Structure):
+    """dgap_adjustment of include/dgap.h (device pointers)."""
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("vocab", ctypes.c_int32), ("history", ctypes.c_int32),
+                ("tokens", ctypes.c_void_p), ("length", ctypes.c_void_p), ("prompt", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("bias_token", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_row", ctypes.c_void_p), ("mask_stride", ctypes.c_int64), ("biases", ctypes.c_int32),
+                ("mask_rows", ctypes.c_int32)]
 
 
 class DgapParams(ctypes.Structure):
@@ -95,6 +123,10 @@ def lib():
         "kvq_seq_len": ([P, I32], I64),
         "kvq_seq_release": ([P, I32], ctypes.c_int),
         "kvq_free_pages": ([P], I64),
+        "kvq_truncate": ([P, ctypes.POINTER(I32)], ctypes.c_int),
+        "kvq_block_cache_bytes": ([ctypes.POINTER(BlockDesc)], S),
+        "kvq_block_cache_init": ([ctypes.POINTER(P), ctypes.POINTER(BlockDesc), P, S], ctypes.c_int),
+        "kvq_append_rotary": ([P, ctypes.POINTER(Rotary), I32, ctypes.POINTER(I32), P, P], ctypes.c_int),
         "kvq_append": ([P, P, P, I32, ctypes.POINTER(I32), P], ctypes.c_int),
         "kvq_workspace_bytes": ([P], S),
         "kvq_decode_attention": ([P, P, P, P, S, P], ctypes.c_int),
@@ -122,6 +154,7 @@ def lib():
         "dgap_distill_workspace_bytes": ([I32, I32], S),
         "dgap_distill": ([ctypes.POINTER(DgapDistillation), P, P, P, I64, P, P, S, P], ctypes.c_int),
         "dgap_distill_backward": ([ctypes.POINTER(DgapDistillation), P, P, P, I64, P], ctypes.c_int),
+        "dgap_adjust": ([ctypes.POINTER(DgapAdjustment), P, I64, P], ctypes.c_int),
         "dgap_sample": ([ctypes.POINTER(DgapSampling), P, P, P, S, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
@@ -199,6 +232,13 @@ def kvq_seq_release(cache: int, seq: int) -> None:
     _check(lib().kvq_seq_release(cache, seq))
 
 
+def kvq_truncate(cache: int, lens: Sequence[int]) -> None:
+    """Every sequence keeps its first lens[i] tokens (one length per sequence)."""
+    if not all(0 <= n < _I32 for n in lens):
+        raise ValueError("lengths are numbers of 32 bits, 0 and above")
+    _check(lib().kvq_truncate(cache, (ctypes.c_int32 * max(1, len(lens)))(*lens)))
+
+
 def kvq_free_pages(cache: int) -> int:
     return int(lib().kvq_free_pages(cache))
 
@@ -209,6 +249,78 @@ def kvq_append(cache: int, K, V, n_new: Sequence[int], n_max: Optional[int] = No
     if n_max is None:
         n_max = int(K.shape[1]) if K is not None and not isinstance(K, int) else max(n_new, default=0)
     _check(lib().kvq_append(cache, _ptr(K), _ptr(V), int(n_max), n, _stream(stream)))
+
+
+_KVQ_TYPES = {"torch.float16": 0, "torch.bfloat16": 1}
+
+
+def _token_rows(name, x, shape, dtype):
+    """The row stride of a [batch][n][heads][128] tensor whose rows ([heads][128]) are contiguous and evenly apart."""
+    if x.dtype != dtype or tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}")
+    b, n, h, d = x.shape
+    row = x.stride(1) if n > 1 else x.stride(0) if b > 1 else h * d
+    if (d > 1 and x.stride(3) != 1) or (h > 1 and x.stride(2) != d) or (n > 1 and b > 1 and x.stride(0) != n * row) \
+            or row < h * d:
+        raise ValueError(f"{name} must have contiguous rows of {h * d} elements, evenly apart")
+    return int(row)
+
+
+def kvq_append_rotary(cache: int, q, K, V, cos, sin, n_new: Sequence[int], q_out, batch: int, num_q_heads: int,
+                      num_kv_heads: int, positions=None, pairs: bool = False, stream=None) -> None:
+    """Append K, V ([batch][n_max][Hkv][128], fp16 or bf16, rows evenly apart) with the keys rotated by ``cos`` and
+    ``sin`` (fp32 [rows][rotary_dim / 2]); ``q`` ([batch][n_max][Hq][128]) or None is rotated into ``q_out`` (fp16).
+
+    ``positions`` int32 [batch][n_max]: rows of the tables (None: the tokens' places); ``pairs``: neighbouring channels
+    turn together, else those rotary_dim / 2 apart."""
+    if len(n_new) != batch or not all(-_I32 <= n < _I32 for n in n_new):
+        raise ValueError(f"n_new must hold {batch} numbers of 32 bits")
+    n_max, d = int(K.shape[1]) if K.dim() == 4 else -1, 128
+    if str(K.dtype) not in _KVQ_TYPES:
+        raise TypeError(f"rows of {K.dtype}: float16 or bfloat16 are supported")
+    ks = _token_rows("K", K, (batch, n_max, num_kv_heads, d), K.dtype)
+    vs = _token_rows("V", V, (batch, n_max, num_kv_heads, d), K.dtype)
+    qs = 0 if q is None else _token_rows("q", q, (batch, n_max, num_q_heads, d), K.dtype)
+    if q is not None:
+        shape = (batch, n_max, num_q_heads, d)
+        if q_out is None or str(q_out.dtype) != "torch.float16" or tuple(q_out.shape) != shape or not q_out.is_contiguous():
+            raise ValueError(f"q_out must be a contiguous float16 tensor of shape {shape}")
+    for name, x in (("cos", cos), ("sin", sin)):
+        if str(x.dtype) != "torch.float32" or x.dim() != 2 or not x.is_contiguous() or x.shape != cos.shape:
+            raise ValueError(f"{name} must be a contiguous float32 tensor [rows][rotary_dim / 2], like the other table")
+    p = Rotary(_ptr(q), _ptr(K), _ptr(V), qs, ks, vs, _ptr(cos), _ptr(sin),
+               _per_row("positions", positions, batch * n_max, "torch.int32"), int(cos.shape[0]),
+               _KVQ_TYPES[str(K.dtype)], 2 * int(cos.shape[1]), int(bool(pairs)), 0)
+    n = (ctypes.c_int32 * max(1, batch))(*n_new)
+    _on_device(stream, lambda st: _check(lib().kvq_append_rotary(
+        cache, ctypes.byref(p), n_max, n, _ptr(q_out) if q is not None else None, st)),
+        q, K, V, cos, sin, positions, q_out)
+
+
+BLOCK_TYPES = {"i8": 0, "e4m3": 1}
+
+
+def make_block_desc(batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int, max_tokens: int, block_tokens: int,
+                    fp16_window: int, type_k: str, type_v: str, page_tokens: int = 0, num_pages: int = 0) -> BlockDesc:
+    """The descriptor of a block-scaled cache; types "i8" or "e4m3"."""
+    for t in (type_k, type_v):
+        if t not in BLOCK_TYPES:
+            raise ValueError(f"type {t!r}: 'i8' or 'e4m3'")
+    return BlockDesc(batch, num_q_heads, num_kv_heads, head_dim, max_tokens, block_tokens, fp16_window,
+                     BLOCK_TYPES[type_k], BLOCK_TYPES[type_v], page_tokens, num_pages, 0)
+
+
+def kvq_block_cache_bytes(desc: BlockDesc) -> int:
+    return int(lib().kvq_block_cache_bytes(ctypes.byref(desc)))
+
+
+def kvq_block_cache_init(desc: BlockDesc, arena, arena_bytes: Optional[int] = None) -> int:
+    """Handle (an int) of a block-scaled cache over ``arena`` (a device tensor or address)."""
+    if arena_bytes is None:
+        arena_bytes = arena.numel() * arena.element_size()
+    h = ctypes.c_void_p()
+    _check(lib().kvq_block_cache_init(ctypes.byref(h), ctypes.byref(desc), _ptr(arena), int(arena_bytes)))
+    return h.value
 
 
 def kvq_workspace_bytes(cache: int) -> int:
@@ -469,6 +581,29 @@ class KVCache:
         kvq_append_decode(self.handle, K, V, n_new, q, out, ws, stream=at)
         return out
 
+    def append_rotary(self, q, K, V, cos, sin, n_new=None, positions=None, pairs=False, q_out=None, stream=None):
+        """Append with rotated keys; returns the rotated queries (fp16), or None without ``q``."""
+        if n_new is None:
+            n_new = [int(K.shape[1])] * self.batch
+        if q is not None and q_out is None:
+            import torch
+            at = stream if stream is not None and q.is_cuda else None
+            if at is not None and isinstance(at, int):
+                at = torch.cuda.ExternalStream(at, device=q.device) if at else torch.cuda.default_stream(q.device)
+            with torch.cuda.stream(at):  # (rows past a sequence's new tokens are nobody's)
+                q_out = torch.zeros(q.shape, dtype=torch.float16, device=q.device)
+            if at is not None:  # (the caller may drop it with work of their own stream still to come)
+                q_out.record_stream(torch.cuda.current_stream(q.device))
+        kvq_append_rotary(self.handle, q, K, V, cos, sin, n_new, q_out, self.batch, self.num_q_heads,
+                          self.num_kv_heads, positions=positions, pairs=pairs, stream=stream)
+        return q_out if q is not None else None
+
+    def truncate(self, lens):
+        """Keep the first lens[i] tokens of every sequence (those after them are dropped)."""
+        if len(lens) != self.batch:
+            raise ValueError(f"{self.batch} lengths are needed")
+        kvq_truncate(self.handle, lens)
+
     def seq_len(self, seq):
         return kvq_seq_len(self.handle, seq)
 
@@ -499,6 +634,29 @@ class KVCache:
 
     def reset(self):
         kvq_cache_reset(self.handle)
+
+
+class BlockCache(KVCache):
+    """A block-scaled cache (8 bits an element, a scale for each block of tokens and head) over a torch-allocated,
+    zero-filled device arena; its calls are KVCache's.  Types "i8" or "e4m3"; ``type_v`` None: the keys'."""
+
+    def __init__(self, batch, num_q_heads, num_kv_heads, max_tokens, type_k="e4m3", type_v=None, block_tokens=64,
+                 fp16_window=0, head_dim=128, device="cuda", page_tokens=0, num_pages=0):
+        import torch
+        type_v = type_k if type_v is None else type_v
+        self.desc = make_block_desc(batch, num_q_heads, num_kv_heads, head_dim, max_tokens, block_tokens, fp16_window,
+                                    type_k, type_v, page_tokens, num_pages)
+        self.page_tokens, self.num_pages = page_tokens, num_pages
+        self.batch, self.num_q_heads, self.num_kv_heads = batch, num_q_heads, num_kv_heads
+        self.head_dim, self.key_group, self.block_tokens = head_dim, block_tokens, block_tokens
+        self.fp16_window, self.type_k, self.type_v, self.max_tokens = fp16_window, type_k, type_v, max_tokens
+        nbytes = kvq_block_cache_bytes(self.desc)
+        if nbytes == 0:
+            # surface the descriptor error through init
+            kvq_block_cache_init(self.desc, 256, 0)
+        self.arena = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.handle = kvq_block_cache_init(self.desc, self.arena)
+        self.ws = self.ws_stream = None
 
 
 # ------------------------------------------------------------------ DGAP
@@ -575,6 +733,51 @@ def dgap_sample(logits, uniform, tokens, ws, temperature=None, top_k=None, top_p
     out = _per_row("tokens", tokens, n, i32), _per_row("logprobs", logprobs, n, f32)
     _on_device(stream, lambda st: _check(lib().dgap_sample(ctypes.byref(p), *out, _ptr(ws), int(ws_bytes), st)),
                logits, uniform, tokens, ws, temperature, top_k, top_p, min_p, logprobs)
+
+
+def dgap_adjust(logits, out=None, tokens=None, length=None, prompt=None, repetition=None, presence=None, frequency=None,
+                bias_token=None, bias=None, mask=None, mask_row=None, stream=None) -> None:
+    """Penalties for repeated tokens, biases and masks on rows of ``logits`` ([rows][vocab], fp32, fp16 or bf16), into
+    ``out`` (like ``logits``; None: in place).
+
+    ``tokens`` int32 [rows][history], the rows' tokens so far, of which the first ``length`` count and the first
+    ``prompt`` of those were given; ``repetition``, ``presence``, ``frequency`` fp32 [rows]; ``bias_token`` int32 and
+    ``bias`` fp32 [rows][biases]; ``mask`` int32 [states][words], bit t % 32 of word t / 32 for token t, and ``mask_row``
+    int32 [rows], the row's state (-1: none; None: its own number).
+    """
+    kind, stride = _rows(logits)
+    n, v, f32, i32 = int(logits.shape[0]), int(logits.shape[1]), "torch.float32", "torch.int32"
+    if out is None:
+        out = logits
+    if out.dtype != logits.dtype or out.shape != logits.shape:
+        raise ValueError("out must have the logits' type and shape")
+    out_stride = _rows(out)[1]
+
+    def table(name, x, dtype):
+        if x is None:
+            return 0
+        if x.dim() != 2 or x.shape[0] != n:
+            raise ValueError(f"{name} must be [rows][...]")
+        _per_row(name, x, x.numel(), dtype)
+        return int(x.shape[1])
+
+    history, biases = table("tokens", tokens, i32), table("bias_token", bias_token, i32)
+    if (bias is None) != (bias_token is None) or table("bias", bias, f32) != biases:
+        raise ValueError("bias_token and bias go together, [rows][biases]")
+    if mask is not None and (mask.dim() != 2 or str(mask.dtype) != i32 or (mask.shape[1] > 1 and mask.stride(1) != 1)
+                             or 32 * mask.shape[1] < v):
+        raise ValueError(f"mask must be an int32 tensor [states][words] with contiguous rows of {(v + 31) // 32} words")
+    states = 0 if mask is None else int(mask.shape[0])
+    if mask is not None and mask_row is None and states < n:
+        raise ValueError("without mask_row, mask must have a row for every row of logits")
+    words = 0 if mask is None else int(mask.stride(0)) if states > 1 else int(mask.shape[1])
+    p = DgapAdjustment(_ptr(logits), stride, kind, n, v, history, _ptr(tokens), _per_row("length", length, n, i32),
+                       _per_row("prompt", prompt, n, i32), _per_row("repetition", repetition, n, f32),
+                       _per_row("presence", presence, n, f32), _per_row("frequency", frequency, n, f32),
+                       _ptr(bias_token), _ptr(bias), _ptr(mask), _per_row("mask_row", mask_row, n, i32), words, biases,
+                       states)
+    _on_device(stream, lambda st: _check(lib().dgap_adjust(ctypes.byref(p), _ptr(out), out_stride, st)),
+               logits, out, tokens, length, prompt, repetition, presence, frequency, bias_token, bias, mask, mask_row)
 
 
 def dgap_distill_workspace_bytes(rows: int, vocab: int) -> int:
