@@ -44,31 +44,29 @@ __device__ __forceinline__ h8_t operand(uint32_t lo, uint32_t hi) {
 // products lose bits).  Returns the power's reciprocal.  The row's four lanes (16
 // apart) hold all of it.
 __device__ __forceinline__ float lift_query(u4_t (&q)[4]) {
-  uint32_t top = 0u;
+  typedef uint16_t us2_t __attribute__((ext_vector_type(2)));
+  us2_t m = {0, 0};
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-    for (int n = 0; n < 4; ++n) top = max(top, max(q[kb][n] & 0x7FFFu, (q[kb][n] >> 16) & 0x7FFFu));
+    for (int n = 0; n < 4; ++n) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2_t, q[kb][n] & 0x7FFF7FFFu));
+  uint32_t top = max((uint32_t)m.x, (uint32_t)m.y);
   top = max(top, (uint32_t)__shfl_xor((int)top, 16));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-  if (top == 0u) return 1.f;
   // exponent of the largest element: -24 .. 15
   const int e = (int)(__builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)top)) >> 23) - 127;
-  const int up = 14 - e;  // -1 .. 38: in two steps of at most 2^15
-  if (up <= 0) return 1.f;
-  const int u0 = min(up, 15), u1 = min(up - u0, 15), u2 = up - u0 - u1;
+  int up = top == 0u ? 0 : max(14 - e, 0);  // 0 .. 38, at most 15 at a time
+  const float back = ldexpf(1.f, -up);
+  do {
+    const int step = min(up, 15);
+    const _Float16 f = __builtin_bit_cast(_Float16, (uint16_t)((step + 15) << 10));
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb)
+    for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      h2_t x = u2h(q[kb][n]);
-      const _Float16 f0 = (_Float16)ldexpf(1.f, u0), f1 = (_Float16)ldexpf(1.f, u1), f2 = (_Float16)ldexpf(1.f, u2);
-      x = x * (h2_t){f0, f0};
-      x = x * (h2_t){f1, f1};
-      x = x * (h2_t){f2, f2};
-      q[kb][n] = h2u(x);
-    }
-  return ldexpf(1.f, -up);
+      for (int n = 0; n < 4; ++n) q[kb][n] = h2u(u2h(q[kb][n]) * (h2_t){f, f});
+    up -= step;
+  } while (__builtin_amdgcn_ballot_w64(up > 0) != 0);
+  return back;
 }
 
 // Two numbers as hi + lo halves (22 bits).  (A pair's hi halves are converted once:

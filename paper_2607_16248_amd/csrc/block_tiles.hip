@@ -13,8 +13,12 @@
 // same), and values lie in operand order (kvq_layout.h, block_value).
 //
 // A workgroup's four waves take 32-token blocks in turn; the next block's codes are
-// asked for before this one's are used.  One launch where a sequence has one split:
-// its workgroup adds the fp16 tail (tail_mfma.h) and writes the output.
+// asked for before this one's are used.  Work is split by its amount: the key groups
+// of all sequences and kv heads are one list, of which every workgroup takes the same
+// number, whatever heads they belong to (sequences of different lengths would
+// otherwise leave compute units idle).  The part that holds a head's end adds the
+// fp16 tail (tail_mfma.h); a sequence whose heads are whole in their workgroups is
+// written to the output, else its parts are joined by the merge launch.
 #include <hip/hip_runtime.h>
 
 #include "block_ops.h"
@@ -37,7 +41,10 @@ using mfma_ops::mfma;
 constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ratio up to 4
 constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
 constexpr float kNoScore = -1e30f;  // below any score
-constexpr int kPartRows = 8;        // rows of one pass of the cross-wave reduction
+
+__device__ __forceinline__ float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
 
 // What a wave reads of a 32-token block.
 struct Codes {
@@ -45,11 +52,41 @@ struct Codes {
   u4_t v[4];  // pieces
 };
 
+// The waves' results of a part, joined through LDS.
+template <int NT>
+struct Joined {
+  float m[kWaves][16 * NT], l[kWaves][16 * NT];
+  float acc[kWaves][16 * NT][kHeadDim + 4];  // (rows begin in distinct banks)
+};
+
+// The sequence that holds unit u (DecodeSeq::wg_begin: its first unit): the last one
+// that begins at u or before.
+__device__ __forceinline__ int sequence_of(const DecodeArgs& a, int u) {
+  static_assert(kMaxSeqPerLaunch <= 64, "one lane per sequence");
+  if (a.nseq == 1) return 0;
+  const int lane = threadIdx.x & 63;
+  const auto* args = (const DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();  // (indexed by lane, `a` would be copied)
+  const int begin = args->seq[min(lane, kMaxSeqPerLaunch - 1)].wg_begin;
+  return __popcll(__builtin_amdgcn_ballot_w64(lane < a.nseq && begin <= u)) - 1;
+}
+
+// Eight lanes' loads of codes that one workgroup reads once (ONCE: past the caches,
+// 188 us to 168 at 32 sequences of 9000 to 16384 tokens) or several row groups read.
+template <bool ONCE>
+__device__ __forceinline__ u4_t load_codes(const uint8_t* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u4_t*>(p));
+  return *reinterpret_cast<const u4_t*>(p);
+}
+
+// The part [u0, u1) of the units of one (sequence, kv head, row group): its key groups
+// below n_groups, the fp16 tail with the last unit.
+struct Part {
+  int si, h, rg, u0, u1, split;
+};
+
 // NT: tiles of 16 rows.
-template <bool K8, bool V8, int NT>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 4))) void block_tiles_kernel(DecodeArgs a) {
-  __shared__ __attribute__((aligned(16))) Reduce<kPartRows> red;
-  const Work wk = find_work<true, true>(a);
+template <bool K8, bool V8, int NT, bool ONCE>
+__device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk, Joined<NT>& red) {
   const DecodeSeq& S = a.seq[wk.si];
   const uint8_t* ring = a.arena + S.head0 + (uint64_t)wk.h * a.head_stride;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -63,9 +100,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int last_limit = seen0 + min(wk.rg * a.qpr + a.qpr - 1, a.nqry - 1);
   const int gsh = __builtin_ctz(a.gk), bsh = gsh - 5;
   const WindowGroups wg = window_groups(first_limit, last_limit, S.Lq, gsh, a.window, a.sinks);
-  // 32-token blocks of this split, every fourth one this wave's
-  const int gps = a.split_tokens >> gsh;
-  const int i0 = ((wk.sp * gps) << bsh) + wv, iend = min(wg.count, wk.sp * gps + gps) << bsh;
+  // 32-token blocks of this part, every fourth one this wave's
+  const int i0 = (wk.u0 << bsh) + wv, iend = min(wg.count, wk.u1) << bsh;
   const int nblocks = i0 < iend ? (iend - i0 + kWaves - 1) / kWaves : 0;
   auto token_of = [&](int i) {
     i = i0 + kWaves * i;
@@ -73,44 +109,23 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     return (i << 5) + (j < wg.sink ? 0 : (wg.first - wg.sink) << gsh);
   };
 
-  // The page of block i's tokens; paged or not, one scalar load (of any word, times
-  // 0 bytes), asked for a block ahead of the loads that need it.
-  typedef const __attribute__((address_space(4))) int32_t scalar_t;
-  typedef const __attribute__((address_space(4))) float scalar_f;
+  // The page of a block's tokens and its scales come by vector loads, whose results
+  // arrive in the order asked for: pages two blocks ahead, scales ahead of the keys.
+  // (As scalar loads, which are waited for all at once, each block stood still for
+  // them: 268 MB, n = 1, 46 us.)
   const bool paged = a.pm.table != nullptr;
   const uint8_t* head = a.arena + (paged ? a.pm.pool0 + (uint64_t)wk.h * a.pm.page_head_bytes : S.head0 + (uint64_t)wk.h * a.head_stride);
-  scalar_t* table = (scalar_t*)(paged ? a.pm.table + (size_t)S.seq * a.pm.max_pages : reinterpret_cast<const int32_t*>(ring + region(a.vb)));
+  const int32_t* table = a.pm.table + (size_t)S.seq * a.pm.max_pages;
   const int page_shift = paged ? a.pm.page_shift : 31, in_page = paged ? a.pm.page_tokens - 1 : 0x7FFFFFFF;
   const uint64_t page_bytes = paged ? a.pm.page_bytes : 0;
-  auto page_of = [&](int i) { return table[token_of(i) >> page_shift]; };
+  int zero = 0;
+  asm("" : "+v"(zero));  // (keeps the loads' addresses in vector registers)
+  auto page_of = [&](int i) { return paged ? table[(token_of(i) >> page_shift) + zero] : 0; };
   const uint32_t k_at = col * kHeadDim + 16 * blk, v_at = lane * 16;
-  auto load = [&](int i, int page, Codes& o, float& sk, float& sv) __attribute__((always_inline)) {
-    const int t = token_of(i) & in_page;
-    const uint8_t* seg = head + (uint64_t)(uint32_t)page * page_bytes;
-    const uint8_t* kr = seg + region(a.kc) + (size_t)t * kHeadDim;
-    const uint8_t* vr = seg + region(a.vc) + (size_t)t * kHeadDim;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) o.k[n] = *reinterpret_cast<const u4_t*>(kr + (n >> 1) * 16 * kHeadDim + (n & 1) * 64 + k_at);
-#pragma unroll
-    for (int n = 0; n < 4; ++n) o.v[n] = *reinterpret_cast<const u4_t*>(vr + n * 1024 + v_at);
-    scalar_f* sc = (scalar_f*)(seg + region(a.km) + (size_t)(t >> gsh) * 8);
-    sk = sc[0];
-    sv = sc[1];
-  };
-  Codes cur;
-  float sk = 0.f, sv = 0.f;
-  int page = 0;
-  if (nblocks > 0) {  // under way before the queries are here
-    page = page_of(0);
-    load(0, page, cur, sk, sv);
-    page = page_of(min(1, nblocks - 1));
-  }
-
   // rows 16 u + col of the group: query operands and limits (rows past whole
   // queries, and queries past the last, repeat the last query)
   u4_t q[NT][4];
   int lim[NT];
-  float ksc[NT];
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     typedef u4_t u4_any __attribute__((aligned(4)));
@@ -119,9 +134,45 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const uint16_t* qr = a.q + (((size_t)S.seq * a.nqry + j) * a.hq + wk.h * a.gqh + (g - x * a.gqh)) * kHeadDim + 16 * blk;
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) q[u][kb] = *reinterpret_cast<const u4_any*>(qr + 64 * (kb >> 1) + 8 * (kb & 1));
-    ksc[u] = a.qscale * block_ops::lift_query(q[u]);
+  }
+  Codes code;
+  auto segment = [&](int i, int page, int& t) {
+    t = token_of(i) & in_page;
+    return head + (uint64_t)(uint32_t)page * page_bytes;
+  };
+  auto load_keys = [&](int i, int page) __attribute__((always_inline)) {
+    int t;
+    const uint8_t* seg = segment(i, page, t);
+    const uint8_t* kr = seg + region(a.kc) + (size_t)t * kHeadDim;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) code.k[n] = load_codes<ONCE>(kr + (n >> 1) * 16 * kHeadDim + (n & 1) * 64 + k_at);
+  };
+  auto load_values = [&](int i, int page) __attribute__((always_inline)) {
+    int t;
+    const uint8_t* seg = segment(i, page, t);
+    const uint8_t* vr = seg + region(a.vc) + (size_t)t * kHeadDim;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) code.v[n] = load_codes<ONCE>(vr + n * 1024 + v_at);
+  };
+  float2 scale = make_float2(0.f, 0.f);
+  auto load_scales = [&](int i, int page) __attribute__((always_inline)) {
+    int t;
+    const uint8_t* seg = segment(i, page, t);
+    scale = *reinterpret_cast<const float2*>(seg + region(a.km) + (size_t)((t >> gsh) + zero) * 8);
+  };
+  const int last = nblocks - 1;
+  int page = 0;
+  if (nblocks > 0) {  // under way while the queries are waited for
+    const int first = __builtin_amdgcn_readfirstlane(page_of(0));
+    page = page_of(min(1, last));
+    load_scales(0, first);
+    load_keys(0, first);
+    load_values(0, first);
   }
 
+  float ksc[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) ksc[u] = a.qscale * block_ops::lift_query(q[u]);
   float m[NT], most[NT], l[NT];
   f4_t acc[NT][8];
   block_ops::ValueUnit unit;
@@ -133,7 +184,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int t = 0; t < 8; ++t) acc[u][t] = (f4_t){0.f, 0.f, 0.f, 0.f};
   }
 
-  auto attend = [&](int i, const Codes& x, float s_k, float s_v) __attribute__((always_inline)) {
+  // block i; the next one's keys are asked for when this one has its scores, its
+  // values and scales when this one is done
+  auto attend = [&](int i) __attribute__((always_inline)) {
+    const int next = min(i + 1, last);  // (after the last block: that one again, unused)
+    const float s_k = uniform(scale.x), s_v = uniform(scale.y);
     const float change = unit.next(s_v);
     if (change != 1.f) {
 #pragma unroll
@@ -148,12 +203,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       for (int u = 0; u < NT; ++u) d[u][mb] = (f4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
-        const u4_t w = x.k[2 * mb + (kb >> 1)];
+        const u4_t w = code.k[2 * mb + (kb >> 1)];
         const h8_t k8 = block_ops::operand<K8>(w[2 * (kb & 1)], w[2 * (kb & 1) + 1]);
 #pragma unroll
         for (int u = 0; u < NT; ++u) d[u][mb] = mfma(k8, __builtin_bit_cast(h8_t, q[u][kb]), d[u][mb]);
       }
     }
+    const int at = __builtin_amdgcn_readfirstlane(page);
+    page = page_of(min(i + 2, last));
+    load_scales(next, at);
+    load_keys(next, at);
     const int tok = token_of(i);
     if (tok + 32 > first_limit || (tok < last_limit - a.window && tok + 32 > a.sinks)) {
       // token tok + 16mb + 4blk + r is visible below the limit, from the window's
@@ -216,7 +275,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) {
-      const u4_t w = x.v[mb >> 1];
+      const u4_t w = code.v[mb >> 1];
       const h8_t v8 = block_ops::operand<V8>(w[2 * (mb & 1)], w[2 * (mb & 1) + 1]);
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
@@ -224,18 +283,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         acc[u][mb] = mfma(v8, pl[u], acc[u][mb]);
       }
     }
+    load_values(next, at);
   };
 
-  for (int i = 0; i < nblocks; ++i) {
-    Codes next;
-    float nk, nv;
-    load(min(i + 1, nblocks - 1), page, next, nk, nv);  // (after the last block: that one again, unused)
-    page = page_of(min(i + 2, nblocks - 1));
-    attend(i, cur, sk, sv);
-    cur = next;
-    sk = nk;
-    sv = nv;
-  }
+  for (int i = 0; i < nblocks; ++i) attend(i);
 
   TailState<NT> st;
 #pragma unroll
@@ -251,7 +302,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int t = 0; t < 8; ++t) st.acc[u][t] = acc[u][t] * f;
   }
-  if (S.L > S.Lq && wk.sp == S.nsplit - 1) {  // the fp16 tail: the last split's, or all of it
+  if (S.L > S.Lq && wk.u1 == S.nq) {  // the fp16 tail
     TailState<NT> tail;
     tail_split<NT, 16 * NT, true, 4, true>(a, S, wk.h, wk.rg, ring, tail, lane, wv);
 #pragma unroll
@@ -268,48 +319,90 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
   }
 
-  // the waves' results of rows r0 .. r0 + 7, merged into records (a sequence of one
-  // split: into the output; every row sees a token, l > 0)
-  auto write_rows = [&](int r0) {
-    for (int idx = threadIdx.x; idx < kPartRows * kHeadDim; idx += blockDim.x) {
-      const int r = idx / kHeadDim, c = idx % kHeadDim, g = r0 + r;
-      const int x = (g * inv) >> 16, j = wk.rg * a.qpr + x;
-      if (g >= rows || j >= a.nqry) continue;
-      float M = -__builtin_inff();
+  __syncthreads();  // (the part before is read)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, red.m[w][r]);
-      float val = 0.f, sum = 0.f;
+  for (int u = 0; u < NT; ++u) {
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = red.m[w][r] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(red.m[w][r] - M);
-        val = fmaf(f, red.acc[w][idx], val);
-        sum = fmaf(f, red.l[w][r], sum);
-      }
-      const size_t row = (size_t)j * a.hq + wk.h * a.gqh + g - x * a.gqh;
-      if (S.nsplit == 1) {
-        a.out[((size_t)S.seq * rec_rows + row) * kHeadDim + c] = val / sum;
-      } else {
-        float* rec = a.ws + ((size_t)(S.ws_base + wk.sp) * rec_rows + row) * kRecFloats;
-        rec[4 + c] = val;
-        if (c == 0) { rec[0] = M; rec[1] = sum; }
-      }
+    for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_t*>(&red.acc[wv][16 * u + col][16 * t + 4 * blk]) = st.acc[u][t];
+    if (blk == 0) {
+      red.m[wv][16 * u + col] = st.m[u];
+      red.l[wv][16 * u + col] = st.l[u];
     }
-  };
+  }
+  __syncthreads();
+  // a thread joins four channels of a row: into the output of a sequence of one part
+  // (every row sees a token in it), else into a record
+  for (int idx = threadIdx.x; idx < rows * (kHeadDim / 4); idx += blockDim.x) {
+    const int g = idx / (kHeadDim / 4), c = 4 * (idx % (kHeadDim / 4)), x = (g * inv) >> 16, j = wk.rg * a.qpr + x;
+    if (j >= a.nqry) continue;
+    float M = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-  for (int u = 0; u < NT; ++u)
-    for (int r0 = 16 * u; r0 < min(rows, 16 * u + 16); r0 += kPartRows) {
-      __syncthreads();
-      stage_tail<kPartRows, NT>(st, u, r0, red, lane, wv);
-      __syncthreads();
-      write_rows(r0);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, red.m[w][g]);
+    f4_t val = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = red.m[w][g] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(red.m[w][g] - M);
+      const f4_t v = *reinterpret_cast<const f4_t*>(&red.acc[w][g][c]);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) val[n] = fmaf(f, v[n], val[n]);
+      sum = fmaf(f, red.l[w][g], sum);
     }
+    const size_t row = (size_t)j * a.hq + wk.h * a.gqh + g - x * a.gqh;
+    if (S.nsplit == 1) {
+      typedef f4_t f4_any __attribute__((aligned(4)));
+      *reinterpret_cast<f4_any*>(a.out + ((size_t)S.seq * rec_rows + row) * kHeadDim + c) = val / (f4_t){sum, sum, sum, sum};
+    } else {
+      float* rec = a.ws + ((size_t)(S.ws_base + wk.split) * rec_rows + row) * kRecFloats;
+      *reinterpret_cast<f4_t*>(rec + 4 + c) = val;
+      if (c == 0) { rec[0] = M; rec[1] = sum; }
+    }
+  }
+  // row groups of one sequence have one number of records: those of fewer parts end
+  // with empty ones
+  if (wk.u1 == S.nq) {
+    for (int split = wk.split + 1; split < S.nsplit; ++split)
+      for (int idx = threadIdx.x; idx < rows * kRecFloats; idx += blockDim.x) {
+        const int g = idx / kRecFloats, c = idx - g * kRecFloats, x = (g * inv) >> 16, j = wk.rg * a.qpr + x;
+        if (j >= a.nqry) continue;
+        const size_t row = (size_t)j * a.hq + wk.h * a.gqh + g - x * a.gqh;
+        a.ws[((size_t)(S.ws_base + split) * rec_rows + row) * kRecFloats + c] = c == 0 ? -__builtin_inff() : 0.f;
+      }
+  }
+}
+
+// The units of a launch (a key group each, and those that stand for a tail) lie one
+// (sequence, kv head, row group) after the other; a workgroup takes
+// a.split_tokens of them (a count here), whatever they belong to.
+template <bool K8, bool V8, int NT, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void block_tiles_kernel(DecodeArgs a) {
+  __shared__ __attribute__((aligned(16))) Joined<NT> red;
+  const int per = a.split_tokens, end = min((int)(blockIdx.x + 1) * per, a.total_wg);
+  for (int u = blockIdx.x * per; u < end;) {
+    Part p;
+    p.si = sequence_of(a, u);
+    const DecodeSeq& S = a.seq[p.si];
+    const int at = u - S.wg_begin, seg = at / S.nq, begin = S.wg_begin + seg * S.nq;
+    p.h = seg / a.nrg;
+    p.rg = seg - p.h * a.nrg;
+    p.u0 = u - begin;
+    p.u1 = min(S.nq, end - begin);
+    p.split = (int)blockIdx.x - begin / per;
+    attend_part<K8, V8, NT, ONCE>(a, p, red);
+    u = begin + p.u1;
+  }
 }
 
 template <bool K8, bool V8>
 int launch_types(const DecodeArgs& a, int rows, void* stream) {
-  const dim3 grid(a.total_wg), block(64 * kWaves);
-  if (rows > 16) hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 2>), grid, block, 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 1>), grid, block, 0, (hipStream_t)stream, a);
+  const dim3 grid((unsigned)((a.total_wg + a.split_tokens - 1) / a.split_tokens)), block(64 * kWaves);
+  hipStream_t s = (hipStream_t)stream;
+  if (a.nrg > 1) {
+    if (rows > 16) hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 2, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 1, false>), grid, block, 0, s, a);
+  } else {
+    if (rows > 16) hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 2, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 1, true>), grid, block, 0, s, a);
+  }
   return (int)hipGetLastError();
 }
 

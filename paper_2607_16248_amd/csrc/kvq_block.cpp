@@ -3,7 +3,7 @@
 // caches' (kvq_api.cpp).
 #include <algorithm>
 #include <cmath>
-#include <cstring>
+#include <cstdint>
 #include <new>
 #include <vector>
 
@@ -25,21 +25,18 @@ Rows rows_for(const kvq_cache* c, int nqry) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
   Rows r;
   r.nqry = nqry;
+  r.rows = nqry * gqh > 16 ? 32 : 16;
   r.qpr = std::min(nqry, r.rows / gqh);
   r.nrg = (nqry + r.qpr - 1) / r.qpr;
   return r;
 }
 
-// Workgroups per sequence and split.
+// Row groups per sequence.
 int64_t units_of(const kvq_cache* c, const Rows& r) { return (int64_t)c->d.num_kv_heads * r.nrg; }
-
-// Workgroups that a call is split into at most (its records, which the workspace
-// holds at any lengths, grow with them).
-int64_t most_workgroups() { return 8 * kvq::target_workgroups(1); }
 
 int32_t group_shift(const kvq_cache* c) { return kvq::log2_exact(c->d.key_group); }
 
-// Most blocks (key groups) that a workgroup of sequence i reads.
+// Most blocks (key groups) that a row group of sequence i reads.
 int32_t reach_of(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks) {
   const int32_t seen0 = c->L[i] - r.nqry + 1, gsh = group_shift(c);
   int32_t most = 0;
@@ -50,87 +47,85 @@ int32_t reach_of(const kvq_cache* c, int i, const Rows& r, int32_t window, int32
   return most;
 }
 
-constexpr int kMinPerSplit = 4;  // 32-token blocks per split at least: one per wave
+// Workgroups of a launch, where there is work for so many: two per compute unit are
+// resident.
+int64_t workgroups() { return 2 * kvq::target_workgroups(1); }
+constexpr int kMinBlocks = 4;  // 32-token blocks per workgroup at least: one per wave
 
-int64_t splits_bound(const kvq_cache* c) {
-  const int64_t groups = c->cq / c->d.key_group;
-  const int64_t per = c->split_tokens > 0 ? c->split_tokens / c->d.key_group : 1;
-  return std::min<int64_t>(kvq::kMaxSplits, (groups + per - 1) / per) + 1;
+// Units that stand for a row group's beginning and end (queries, joined waves, records) and
+// its fp16 tail, in the time of a key group each: kPartTokens tokens, the tail's and 64
+// more.  64 sequences of 100 to 12000 tokens, tails of 128 to 191: 184 us without them,
+// 150 with 256 tokens, 140 with 384 and with 768.  Where a workgroup's share is small,
+// every one has a beginning and an end, and they count for a quarter of it at most.
+constexpr int kPartTokens = 384;
+int32_t extra_units(int32_t tail, int32_t G, int64_t share) {
+  const int64_t tokens = std::min<int64_t>((tail > 0 ? tail + 64 : 0) + kPartTokens, share * G / 4);
+  return std::max<int32_t>((int32_t)((tokens + G - 1) / G), tail > 0 ? 1 : 0);
 }
 
-// Estimated time of a launch, us: workgroups, 32-token blocks that a wave of the
-// longest takes, bytes read, rows to merge.
-double estimate_us(int64_t wgs, int64_t blocks, double bytes, int64_t merged_rows) {
-  const int64_t slots = 2 * kvq::target_workgroups(1), rounds = (wgs + slots - 1) / slots;
-  const double work = std::max((double)rounds * (2.0 + 0.7 * (double)blocks), bytes / 5.0e6);
-  return 3.0 + work + (merged_rows > 0 ? 4.0 + 2e-3 * (double)merged_rows : 0.0);
-}
-
+// What a call's launches are given: the list of work units of a launch's sequences
+// (the key groups that a row group reads, and units that stand for its tail), of
+// which every workgroup takes `per`.
 struct Plan {
   Rows r;
-  int32_t per = 1;                       // key groups per split
-  std::vector<int32_t> nq, ns, base;     // per sequence: packed splits, all splits, first record
+  std::vector<int32_t> units, begin, ns, base;  // per sequence: units of a row group, first unit, records, first record
+  std::vector<int> first;                       // per launch: its first sequence
+  std::vector<int32_t> per, total;              // per launch
   int64_t records = 0;
+  bool fits = true;
 };
 
 Plan plan_for(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   Plan p;
   p.r = rows_for(c, nqry);
-  const int B = c->d.batch;
-  p.nq.assign(B, 0);
+  const int B = c->d.batch, G = c->d.key_group;
+  p.units.assign(B, 0);
+  p.begin.assign(B, 0);
   p.ns.assign(B, 0);
   p.base.assign(B, 0);
-  std::vector<int32_t> reach(B, 0);
-  int64_t longest = 1;
-  const int64_t units = units_of(c, p.r), rows = (int64_t)nqry * c->d.num_q_heads;
-  double bytes = 0.0;
-  for (int i = 0; i < B; ++i) {
-    if (c->L[i] == 0) continue;
-    reach[i] = reach_of(c, i, p.r, window, sinks);
-    longest = std::max<int64_t>(longest, reach[i]);
-    bytes += (double)reach[i] * c->d.key_group * 256.0 * c->d.num_kv_heads;
-  }
-  const int bpg = c->d.key_group / 32;
-  int64_t per = longest;
-  if (c->split_tokens > 0) {
-    per = std::max<int64_t>(c->split_tokens / c->d.key_group, (longest + kvq::kMaxSplits - 1) / kvq::kMaxSplits);
-  } else {
-    double best = 0.0;
-    int64_t tried = 0;
-    for (int64_t ns = 1; ns <= std::min<int64_t>(kvq::kMaxSplits, longest); ++ns) {
-      const int64_t n = (longest + ns - 1) / ns;
-      if (n == tried) continue;
-      tried = n;
-      if (ns > 1 && n * bpg < kMinPerSplit) break;
-      int64_t wgs = 0, merged = 0;
-      for (int i = 0; i < B; ++i) {
-        if (c->L[i] == 0) continue;
-        const int64_t k = std::max<int64_t>(1, (reach[i] + n - 1) / n);
-        wgs += units * k;
-        merged += k > 1 ? rows : 0;
+  const int64_t groups = units_of(c, p.r);
+  int i = 0;
+  while (i < B) {
+    p.first.push_back(i);
+    int64_t total = 0;
+    const int from0 = i;
+    int upto = i;
+    for (int n = 0; upto < B && n < kvq::kMaxSeqPerLaunch; ++upto) {
+      if (c->L[upto] == 0) continue;
+      ++n;
+      p.units[upto] = reach_of(c, upto, p.r, window, sinks);
+      total += groups * p.units[upto];
+    }
+    const int64_t share = (total + workgroups() - 1) / workgroups();
+    total = 0;
+    for (int n = 0; i < B && n < kvq::kMaxSeqPerLaunch; ++i) {
+      if (c->L[i] == 0) continue;
+      ++n;
+      p.units[i] += extra_units(c->L[i] - c->Lq[i], G, share);
+      p.begin[i] = (int32_t)std::min<int64_t>(total, INT32_MAX);
+      total += groups * p.units[i];
+    }
+    int64_t per = (total + workgroups() - 1) / workgroups();
+    per = std::max<int64_t>({per, (kMinBlocks * 32 + G - 1) / G, 1});
+    if (c->split_tokens > 0) per = c->split_tokens / G;
+    p.fits &= total + per < INT32_MAX && (total + per - 1) / per < (int64_t)1 << 22;
+    p.per.push_back((int32_t)per);
+    p.total.push_back((int32_t)std::min<int64_t>(total, INT32_MAX));
+    for (int from = from0; from < i; ++from) {
+      if (c->L[from] == 0) continue;
+      // parts of the row group with the most of them
+      int64_t ns = 1;
+      for (int64_t s = 0; s < groups; ++s) {
+        const int64_t b = p.begin[from] + s * p.units[from];
+        ns = std::max(ns, (b + p.units[from] - 1) / per - b / per + 1);
+        if (ns >= (p.units[from] + per - 2) / per + 1) break;  // (no more than that)
       }
-      if (ns > 1 && wgs > most_workgroups()) break;
-      const double t = estimate_us(wgs, (n * bpg + 3) / 4, bytes, merged);
-      if (ns == 1 || t < best) best = t, per = n;
+      p.ns[from] = (int32_t)ns;
+      p.base[from] = (int32_t)std::min<int64_t>(p.records, INT32_MAX);
+      p.records += ns > 1 ? ns : 0;
     }
   }
-  p.per = (int32_t)per;
-  int64_t wgs = 0, tails = 0;
-  for (int i = 0; i < B; ++i) {
-    if (c->L[i] == 0) continue;
-    p.nq[i] = (int32_t)((reach[i] + per - 1) / per);
-    p.ns[i] = std::max(1, p.nq[i]);
-    wgs += units * p.ns[i];
-    if (p.nq[i] > 1 && c->L[i] > c->Lq[i]) tails += units;
-  }
-  // the fp16 tail takes a workgroup of its own where there is room and the splits
-  // are merged anyway
-  const bool own_tails = wgs + tails <= kvq::target_workgroups(1);
-  for (int i = 0; i < B; ++i) {
-    if (own_tails && p.nq[i] > 1 && c->L[i] > c->Lq[i]) ++p.ns[i];
-    p.base[i] = (int32_t)p.records;
-    p.records += p.ns[i] > 1 ? p.ns[i] : 0;
-  }
+  p.fits &= p.records < INT32_MAX;
   return p;
 }
 
@@ -145,14 +140,23 @@ void full(const kvq_cache* c, int32_t& window, int32_t& sinks) {
   sinks = std::min(sinks, longest);
 }
 
+// A list of n units of `groups` row groups in parts of `per` has n / per + 2 of them in
+// a sequence at most.  Lists of no more than `workgroups()` parts: a sequence has so
+// many of them, and no more records than its parts and row groups divided, and one.
 size_t bound(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   (void)window;
   (void)sinks;
-  const int64_t each = splits_bound(c), all = c->d.batch * each;
-  if (c->split_tokens > 0) return (size_t)all * record_bytes(c, n_q);
-  // a plan of more than one split has most_workgroups() of them at most, and the tails'
-  const int64_t most = most_workgroups() / units_of(c, rows_for(c, n_q)) + c->d.batch;
-  return (size_t)std::max<int64_t>(1, std::min(all, most)) * record_bytes(c, n_q);
+  const int64_t G = c->d.key_group, B = c->d.batch, groups = units_of(c, rows_for(c, n_q));
+  const int64_t units = c->cq / G + extra_units((int32_t)std::min<int64_t>((int64_t)c->d.fp16_window + G, 1 << 30), (int32_t)G, INT32_MAX);
+  const int64_t least = c->split_tokens > 0 ? c->split_tokens / G : std::max<int64_t>(1, (kMinBlocks * 32 + G - 1) / G);
+  int64_t records = B * ((units + least - 2) / least + 1);
+  if (c->split_tokens == 0) {
+    // per >= total / workgroups(): the parts of a row group, (units - 1) / per + 2 at most, are
+    // no more than workgroups() / groups of all sequences of a launch together, and 2 each
+    const int64_t launches = (B + kvq::kMaxSeqPerLaunch - 1) / kvq::kMaxSeqPerLaunch;
+    records = std::min(records, launches * (workgroups() / groups + 1) + 2 * B);
+  }
+  return (size_t)std::max<int64_t>(1, records) * record_bytes(c, n_q);
 }
 
 size_t need(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
@@ -165,12 +169,12 @@ kvq_status attend(const kvq_cache* c, const void* q, int32_t n_q, int32_t window
   const kvq_cache_desc& d = c->d;
   full(c, window, sinks);
   const Plan p = plan_for(c, n_q, window, sinks);
+  if (!p.fits) return fail(KVQ_ERR_UNSUPPORTED, "too much work for one call");
   const size_t bytes = (size_t)p.records * record_bytes(c, n_q);
   if (bytes > 0 && !ws) return fail(KVQ_ERR_ARG, "workspace is NULL");
   if (ws_bytes < bytes) return fail(KVQ_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, bytes);
   if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return fail(KVQ_ERR_ARG, "workspace must be 16-byte aligned");
-  int i = 0;
-  while (i < d.batch) {
+  for (size_t k = 0; k < p.first.size(); ++k) {
     kvq::DecodeArgs a{};
     const kvq::HeadLayout& lay = c->lay[0];
     a.arena = c->arena;
@@ -181,23 +185,21 @@ kvq_status attend(const kvq_cache* c, const void* q, int32_t n_q, int32_t window
     a.kc = kvq::region_units(lay.kc); a.km = kvq::region_units(lay.km); a.vc = kvq::region_units(lay.vc);
     a.vm = kvq::region_units(lay.vm); a.tk = kvq::region_units(lay.tk); a.tv = kvq::region_units(lay.tv); a.vb = kvq::region_units(lay.vb);
     a.hq = d.num_q_heads; a.hkv = d.num_kv_heads; a.gk = d.key_group; a.gv = d.value_group; a.W = c->W;
-    a.split_tokens = p.per * d.key_group;
+    a.split_tokens = p.per[k];  // units per workgroup
     a.qscale = (float)(1.4426950408889634 / std::sqrt((double)d.head_dim));
     a.nqry = p.r.nqry; a.qpr = p.r.qpr; a.nrg = p.r.nrg; a.gqh = d.num_q_heads / d.num_kv_heads;
     a.pm = c->pm;
     a.window = window;
     a.sinks = sinks;
-    int64_t wg = 0;
-    for (; i < d.batch && a.nseq < kvq::kMaxSeqPerLaunch; ++i) {
+    for (int i = p.first[k]; i < d.batch && a.nseq < kvq::kMaxSeqPerLaunch; ++i) {
       if (c->L[i] == 0) continue;
       kvq::DecodeSeq& s = a.seq[a.nseq++];
       s.head0 = c->head0[i];
       s.seq = i; s.L = s.L_old = c->L[i]; s.Lq = c->Lq[i];
-      s.nq = p.nq[i]; s.nsplit = p.ns[i]; s.ws_base = p.base[i];
-      s.wg_begin = (int32_t)wg;
-      wg += p.ns[i] * units_of(c, p.r);
+      s.nq = p.units[i]; s.nsplit = p.ns[i]; s.ws_base = p.base[i];
+      s.wg_begin = p.begin[i];
     }
-    a.total_wg = (int32_t)wg;
+    a.total_wg = p.total[k];  // units
     const int e = kvq::launch_block_tiles(a, c->type_k, c->type_v, p.r.rows, stream);
     if (e) return kvq::hip_fail(e, "block-scaled attention launch");
   }
