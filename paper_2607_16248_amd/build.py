@@ -47,6 +47,7 @@ SOURCES = [
     ("kvq_rotary.cpp", [], None),
     ("block_append.hip", ["-ffp-contract=off"], None),
     ("block_tiles.hip", ["-fno-honor-nans"], None),
+    ("block_rows.hip", ["-fno-honor-nans"], None),
     ("block_read.hip", [], None),
     ("kvq_block.cpp", [], None),
     ("kvq_api.cpp", [], None),
@@ -74,7 +75,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     workers = min(len(SOURCES), max(2, os.cpu_count() or 2))
     # the long compiles first, so that they start at once
-    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip", "window.hip", "block_tiles.hip"))
+    order = sorted(range(len(SOURCES)), key=lambda i: SOURCES[i][0] not in ("decode_mfma.hip", "decode_exact.hip", "chunk_mfma.hip", "prefill_mfma.hip", "window.hip", "block_tiles.hip", "block_rows.hip"))
     with cf.ThreadPoolExecutor(max_workers=workers) as ex:
         done = dict(zip(order, ex.map(lambda i: _compile(SOURCES[i][0], SOURCES[i][1], verbose, SOURCES[i][2]),
                                       order)))

@@ -6,6 +6,7 @@
 
 #include <stdint.h>
 
+#include "kvq_internal.h"
 #include "mfma_common.h"
 
 namespace kvq {
@@ -111,6 +112,21 @@ struct ValueUnit {
     return f;
   }
 };
+
+// The sequence that holds unit u (DecodeSeq::wg_begin: its first unit): the last one
+// that begins at u or before.
+__device__ __forceinline__ int sequence_of(const DecodeArgs& a, int u) {
+  static_assert(kMaxSeqPerLaunch <= 64, "one lane per sequence");
+  if (a.nseq == 1) return 0;
+  const int lane = threadIdx.x & 63;
+  const auto* args = (const DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();  // (indexed by lane, `a` would be copied)
+  const int begin = args->seq[min(lane, kMaxSeqPerLaunch - 1)].wg_begin;
+  return __popcll(__builtin_amdgcn_ballot_w64(lane < a.nseq && begin <= u)) - 1;
+}
+
+__device__ __forceinline__ float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
 
 }  // namespace block_ops
 }  // namespace kvq

@@ -42,10 +42,6 @@ constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ra
 constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
 constexpr float kNoScore = -1e30f;  // below any score
 
-__device__ __forceinline__ float uniform(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
-}
-
 // What a wave reads of a 32-token block.
 struct Codes {
   u4_t k[4];  // token half, 64-channel half
@@ -59,19 +55,8 @@ struct Joined {
   float acc[kWaves][16 * NT][kHeadDim + 4];  // (rows begin in distinct banks)
 };
 
-// The sequence that holds unit u (DecodeSeq::wg_begin: its first unit): the last one
-// that begins at u or before.
-__device__ __forceinline__ int sequence_of(const DecodeArgs& a, int u) {
-  static_assert(kMaxSeqPerLaunch <= 64, "one lane per sequence");
-  if (a.nseq == 1) return 0;
-  const int lane = threadIdx.x & 63;
-  const auto* args = (const DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();  // (indexed by lane, `a` would be copied)
-  const int begin = args->seq[min(lane, kMaxSeqPerLaunch - 1)].wg_begin;
-  return __popcll(__builtin_amdgcn_ballot_w64(lane < a.nseq && begin <= u)) - 1;
-}
-
-// Eight lanes' loads of codes that one workgroup reads once (ONCE: past the caches,
-// 188 us to 168 at 32 sequences of 9000 to 16384 tokens) or several row groups read.
+// Codes that one workgroup reads once (ONCE: past the caches, 188 us to 168 at 32
+// sequences of 9000 to 16384 tokens), or several row groups.
 template <bool ONCE>
 __device__ __forceinline__ u4_t load_codes(const uint8_t* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u4_t*>(p));
@@ -79,7 +64,7 @@ __device__ __forceinline__ u4_t load_codes(const uint8_t* p) {
 }
 
 // The part [u0, u1) of the units of one (sequence, kv head, row group): its key groups
-// below n_groups, the fp16 tail with the last unit.
+// and, as the last unit that stands for work, the fp16 tail.
 struct Part {
   int si, h, rg, u0, u1, split;
 };
@@ -188,7 +173,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
   // values and scales when this one is done
   auto attend = [&](int i) __attribute__((always_inline)) {
     const int next = min(i + 1, last);  // (after the last block: that one again, unused)
-    const float s_k = uniform(scale.x), s_v = uniform(scale.y);
+    const float s_k = block_ops::uniform(scale.x), s_v = block_ops::uniform(scale.y);
     const float change = unit.next(s_v);
     if (change != 1.f) {
 #pragma unroll
@@ -302,7 +287,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
 #pragma unroll
     for (int t = 0; t < 8; ++t) st.acc[u][t] = acc[u][t] * f;
   }
-  if (S.L > S.Lq && wk.u1 == S.nq) {  // the fp16 tail
+  if (S.L > S.Lq && wk.u1 == S.L_old) {  // the fp16 tail
     TailState<NT> tail;
     tail_split<NT, 16 * NT, true, 4, true>(a, S, wk.h, wk.rg, ring, tail, lane, wv);
 #pragma unroll
@@ -359,7 +344,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
   }
   // row groups of one sequence have one number of records: those of fewer parts end
   // with empty ones
-  if (wk.u1 == S.nq) {
+  if (wk.u1 == S.L_old) {
     for (int split = wk.split + 1; split < S.nsplit; ++split)
       for (int idx = threadIdx.x; idx < rows * kRecFloats; idx += blockDim.x) {
         const int g = idx / kRecFloats, c = idx - g * kRecFloats, x = (g * inv) >> 16, j = wk.rg * a.qpr + x;
@@ -372,29 +357,29 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
 
 // The units of a launch (a key group each, and those that stand for a tail) lie one
 // (sequence, kv head, row group) after the other; a workgroup takes
-// a.split_tokens of them (a count here), whatever they belong to.
+// a.units_per_wg of them, whatever they belong to.
 template <bool K8, bool V8, int NT, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void block_tiles_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) Joined<NT> red;
-  const int per = a.split_tokens, end = min((int)(blockIdx.x + 1) * per, a.total_wg);
+  const int per = a.units_per_wg, end = min((int)(blockIdx.x + 1) * per, a.total_wg);
   for (int u = blockIdx.x * per; u < end;) {
     Part p;
-    p.si = sequence_of(a, u);
+    p.si = block_ops::sequence_of(a, u);
     const DecodeSeq& S = a.seq[p.si];
     const int at = u - S.wg_begin, seg = at / S.nq, begin = S.wg_begin + seg * S.nq;
     p.h = seg / a.nrg;
     p.rg = seg - p.h * a.nrg;
     p.u0 = u - begin;
-    p.u1 = min(S.nq, end - begin);
+    p.u1 = min(S.L_old, end - begin);
     p.split = (int)blockIdx.x - begin / per;
-    attend_part<K8, V8, NT, ONCE>(a, p, red);
-    u = begin + p.u1;
+    if (p.u0 < p.u1) attend_part<K8, V8, NT, ONCE>(a, p, red);
+    u = begin + S.nq;
   }
 }
 
 template <bool K8, bool V8>
 int launch_types(const DecodeArgs& a, int rows, void* stream) {
-  const dim3 grid((unsigned)((a.total_wg + a.split_tokens - 1) / a.split_tokens)), block(64 * kWaves);
+  const dim3 grid((unsigned)((a.total_wg + a.units_per_wg - 1) / a.units_per_wg)), block(64 * kWaves);
   hipStream_t s = (hipStream_t)stream;
   if (a.nrg > 1) {
     if (rows > 16) hipLaunchKernelGGL((block_tiles_kernel<K8, V8, 2, false>), grid, block, 0, s, a);

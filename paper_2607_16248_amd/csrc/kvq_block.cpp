@@ -16,10 +16,16 @@ using kvq::fail;
 namespace {
 
 // Rows of an attention launch: nqry queries per sequence in row groups of qpr
-// queries (DecodeArgs).
+// queries (DecodeArgs): tiles of up to 16 or 32 rows, or workgroups of `waves` row
+// groups of 32 (block_rows.hip).
 struct Rows {
   int nqry = 1, qpr = 1, nrg = 1, rows = 16;
+  int waves = 0;   // many rows: row groups per workgroup, else 0
+  int groups = 1;  // that take parts of their own: row groups, or workgroups' sets of them
 };
+
+// Many rows from so many (query, head) rows of a kv head on.
+constexpr int kManyRows = 64;
 
 Rows rows_for(const kvq_cache* c, int nqry) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
@@ -27,50 +33,56 @@ Rows rows_for(const kvq_cache* c, int nqry) {
   r.nqry = nqry;
   r.rows = nqry * gqh > 16 ? 32 : 16;
   r.qpr = std::min(nqry, r.rows / gqh);
-  r.nrg = (nqry + r.qpr - 1) / r.qpr;
+  r.nrg = r.groups = (nqry + r.qpr - 1) / r.qpr;
+  if (nqry * gqh >= kManyRows) {
+    r.waves = r.nrg > 4 ? 8 : 4;
+    r.groups = (r.nrg + r.waves - 1) / r.waves;
+  }
   return r;
 }
 
-// Row groups per sequence.
-int64_t units_of(const kvq_cache* c, const Rows& r) { return (int64_t)c->d.num_kv_heads * r.nrg; }
-
 int32_t group_shift(const kvq_cache* c) { return kvq::log2_exact(c->d.key_group); }
 
-// Most blocks (key groups) that a row group of sequence i reads.
-int32_t reach_of(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks) {
+// Units of work of the groups of a sequence: key groups (tiles, the most of any
+// row group, and one for the tail) or 32-token blocks.
+int32_t tile_units(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks) {
   const int32_t seen0 = c->L[i] - r.nqry + 1, gsh = group_shift(c);
   int32_t most = 0;
   for (int first = 0; first < r.nqry; first += r.qpr) {
     const int32_t seen_first = seen0 + first, seen_last = seen0 + std::min(first + r.qpr, r.nqry) - 1;
     most = std::max(most, kvq::window_groups(seen_first, seen_last, c->Lq[i], gsh, window, sinks).count);
   }
-  return most;
+  return most + (c->L[i] > c->Lq[i] ? 1 : 0);
+}
+int32_t row_units(const kvq_cache* c, int i, const Rows& r, int32_t window, int32_t sinks, int group) {
+  return kvq::row_blocks(r.nqry, r.qpr * r.waves, c->L[i], c->Lq[i], group_shift(c), window, sinks, group).total;
 }
 
-// Workgroups of a launch, where there is work for so many: two per compute unit are
-// resident.
-int64_t workgroups() { return 2 * kvq::target_workgroups(1); }
-constexpr int kMinBlocks = 4;  // 32-token blocks per workgroup at least: one per wave
+// Workgroups of a launch, where there is work for so many: as many as are resident.
+int64_t workgroups(const Rows& r) { return (r.waves == 8 ? 1 : 2) * kvq::target_workgroups(1); }
+constexpr int kMinBlocks = 4;  // 32-token blocks per workgroup at least (tiles: one per wave)
 
-// Units that stand for a row group's beginning and end (queries, joined waves, records) and
-// its fp16 tail, in the time of a key group each: kPartTokens tokens, the tail's and 64
-// more.  64 sequences of 100 to 12000 tokens, tails of 128 to 191: 184 us without them,
-// 150 with 256 tokens, 140 with 384 and with 768.  Where a workgroup's share is small,
-// every one has a beginning and an end, and they count for a quarter of it at most.
+// Tiles: units that stand for a row group's beginning and end (queries, joined waves,
+// records) and its fp16 tail, in the time of a key group each: kPartTokens tokens, the
+// tail's and 64 more.  64 sequences of 100 to 12000 tokens, tails of 128 to 191: 184 us
+// without them, 150 with 256 tokens, 140 with 384 and with 768.  Where a workgroup's
+// share is small, every one has a beginning and an end, and they count for a quarter
+// of it at most.
 constexpr int kPartTokens = 384;
-int32_t extra_units(int32_t tail, int32_t G, int64_t share) {
-  const int64_t tokens = std::min<int64_t>((tail > 0 ? tail + 64 : 0) + kPartTokens, share * G / 4);
-  return std::max<int32_t>((int32_t)((tokens + G - 1) / G), tail > 0 ? 1 : 0);
+int32_t tile_extra(int32_t tail, int32_t G, int64_t share) {
+  const int64_t tokens = std::min<int64_t>((tail > 0 ? tail + 64 - G : 0) + kPartTokens, share * G / 4);
+  return std::max(0, (int32_t)((tokens + G - 1) / G));
 }
+// Many rows: the same, in blocks.
+constexpr int kRowExtra = 8;
 
-// What a call's launches are given: the list of work units of a launch's sequences
-// (the key groups that a row group reads, and units that stand for its tail), of
+// What a call's launches are given: the list of work units of a launch's sequences, of
 // which every workgroup takes `per`.
 struct Plan {
   Rows r;
-  std::vector<int32_t> units, begin, ns, base;  // per sequence: units of a row group, first unit, records, first record
-  std::vector<int> first;                       // per launch: its first sequence
-  std::vector<int32_t> per, total;              // per launch
+  std::vector<int32_t> real, units, begin, ns, base;  // per sequence: DecodeSeq's L_old, nq, wg_begin, nsplit, ws_base
+  std::vector<int> first;                             // per launch: its first sequence
+  std::vector<int32_t> per, total, extra;             // per launch
   int64_t records = 0;
   bool fits = true;
 };
@@ -78,50 +90,52 @@ struct Plan {
 Plan plan_for(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
   Plan p;
   p.r = rows_for(c, nqry);
-  const int B = c->d.batch, G = c->d.key_group;
-  p.units.assign(B, 0);
-  p.begin.assign(B, 0);
-  p.ns.assign(B, 0);
-  p.base.assign(B, 0);
-  const int64_t groups = units_of(c, p.r);
-  int i = 0;
-  while (i < B) {
+  const Rows& r = p.r;
+  const int B = c->d.batch, G = c->d.key_group, hkv = c->d.num_kv_heads;
+  for (auto* v : {&p.real, &p.units, &p.begin, &p.ns, &p.base}) v->assign(B, 0);
+  for (int i = 0; i < B;) {
+    const int from = i;
     p.first.push_back(i);
     int64_t total = 0;
-    const int from0 = i;
-    int upto = i;
-    for (int n = 0; upto < B && n < kvq::kMaxSeqPerLaunch; ++upto) {
-      if (c->L[upto] == 0) continue;
-      ++n;
-      p.units[upto] = reach_of(c, upto, p.r, window, sinks);
-      total += groups * p.units[upto];
-    }
-    const int64_t share = (total + workgroups() - 1) / workgroups();
-    total = 0;
     for (int n = 0; i < B && n < kvq::kMaxSeqPerLaunch; ++i) {
       if (c->L[i] == 0) continue;
       ++n;
-      p.units[i] += extra_units(c->L[i] - c->Lq[i], G, share);
-      p.begin[i] = (int32_t)std::min<int64_t>(total, INT32_MAX);
-      total += groups * p.units[i];
+      if (r.waves) {
+        for (int g = 0; g < r.groups; ++g) p.real[i] += row_units(c, i, r, window, sinks, g);
+        total += (int64_t)hkv * p.real[i];
+      } else {
+        p.real[i] = tile_units(c, i, r, window, sinks);
+        total += (int64_t)hkv * r.groups * p.real[i];
+      }
     }
-    int64_t per = (total + workgroups() - 1) / workgroups();
-    per = std::max<int64_t>({per, (kMinBlocks * 32 + G - 1) / G, 1});
-    if (c->split_tokens > 0) per = c->split_tokens / G;
+    const int64_t share = (total + workgroups(r) - 1) / workgroups(r);
+    const int32_t extra = (int32_t)std::min<int64_t>(kRowExtra, share / 4);
+    total = 0;
+    for (int k = from; k < i; ++k) {
+      if (c->L[k] == 0) continue;
+      p.units[k] = p.real[k] + (r.waves ? r.groups * extra : tile_extra(c->L[k] - c->Lq[k], G, share));
+      p.begin[k] = (int32_t)std::min<int64_t>(total, INT32_MAX);
+      total += (int64_t)hkv * (r.waves ? 1 : r.groups) * p.units[k];
+    }
+    const int64_t least = r.waves ? kMinBlocks : (kMinBlocks * 32 + G - 1) / G;
+    int64_t per = std::max<int64_t>({(total + workgroups(r) - 1) / workgroups(r), least, 1});
+    if (c->split_tokens > 0) per = c->split_tokens / (r.waves ? 32 : G);
     p.fits &= total + per < INT32_MAX && (total + per - 1) / per < (int64_t)1 << 22;
     p.per.push_back((int32_t)per);
+    p.extra.push_back(extra);
     p.total.push_back((int32_t)std::min<int64_t>(total, INT32_MAX));
-    for (int from = from0; from < i; ++from) {
-      if (c->L[from] == 0) continue;
-      // parts of the row group with the most of them
-      int64_t ns = 1;
-      for (int64_t s = 0; s < groups; ++s) {
-        const int64_t b = p.begin[from] + s * p.units[from];
-        ns = std::max(ns, (b + p.units[from] - 1) / per - b / per + 1);
-        if (ns >= (p.units[from] + per - 2) / per + 1) break;  // (no more than that)
-      }
-      p.ns[from] = (int32_t)ns;
-      p.base[from] = (int32_t)std::min<int64_t>(p.records, INT32_MAX);
+    for (int k = from; k < i && p.fits; ++k) {
+      if (c->L[k] == 0) continue;
+      // parts of the group with the most of them
+      int64_t ns = 1, b = p.begin[k];
+      for (int h = 0; h < hkv; ++h)
+        for (int g = 0; g < r.groups; ++g) {
+          const int64_t n = r.waves ? row_units(c, k, r, window, sinks, g) : p.real[k];
+          ns = std::max(ns, (b + n - 1) / per - b / per + 1);
+          b += r.waves ? n + extra : p.units[k];
+        }
+      p.ns[k] = (int32_t)ns;
+      p.base[k] = (int32_t)std::min<int64_t>(p.records, INT32_MAX);
       p.records += ns > 1 ? ns : 0;
     }
   }
@@ -140,21 +154,24 @@ void full(const kvq_cache* c, int32_t& window, int32_t& sinks) {
   sinks = std::min(sinks, longest);
 }
 
-// A list of n units of `groups` row groups in parts of `per` has n / per + 2 of them in
-// a sequence at most.  Lists of no more than `workgroups()` parts: a sequence has so
-// many of them, and no more records than its parts and row groups divided, and one.
+// A group of n units in parts of `per` has (n + per - 2) / per + 1 of them at most.
 size_t bound(const kvq_cache* c, int32_t n_q, int32_t window, int32_t sinks) {
   (void)window;
   (void)sinks;
-  const int64_t G = c->d.key_group, B = c->d.batch, groups = units_of(c, rows_for(c, n_q));
-  const int64_t units = c->cq / G + extra_units((int32_t)std::min<int64_t>((int64_t)c->d.fp16_window + G, 1 << 30), (int32_t)G, INT32_MAX);
-  const int64_t least = c->split_tokens > 0 ? c->split_tokens / G : std::max<int64_t>(1, (kMinBlocks * 32 + G - 1) / G);
+  const Rows r = rows_for(c, n_q);
+  const int64_t G = c->d.key_group, B = c->d.batch, unit = r.waves ? 32 : G;
+  const int64_t units = ((int64_t)c->d.max_tokens + unit - 1) / unit + 2;  // of a group, without those that stand for no work
+  const int64_t least = c->split_tokens > 0 ? c->split_tokens / unit
+                                            : std::max<int64_t>(1, r.waves ? kMinBlocks : (kMinBlocks * 32 + G - 1) / G);
   int64_t records = B * ((units + least - 2) / least + 1);
   if (c->split_tokens == 0) {
-    // per >= total / workgroups(): the parts of a row group, (units - 1) / per + 2 at most, are
-    // no more than workgroups() / groups of all sequences of a launch together, and 2 each
+    // per >= total / workgroups: of the sequences of a launch, the sum of units / per over all
+    // groups is workgroups() at most, and a group has no more parts than that and 2.
+    // Many rows: the group with the most blocks counts; half of them are the average at least
+    // (causal groups grow evenly), and the kv heads have them all
     const int64_t launches = (B + kvq::kMaxSeqPerLaunch - 1) / kvq::kMaxSeqPerLaunch;
-    records = std::min(records, launches * (workgroups() / groups + 1) + 2 * B);
+    const int64_t groups = (int64_t)c->d.num_kv_heads * r.groups;
+    records = std::min(records, launches * ((r.waves ? 2 : 1) * workgroups(r) / groups + 1) + 3 * B);
   }
   return (size_t)std::max<int64_t>(1, records) * record_bytes(c, n_q);
 }
@@ -185,7 +202,8 @@ kvq_status attend(const kvq_cache* c, const void* q, int32_t n_q, int32_t window
     a.kc = kvq::region_units(lay.kc); a.km = kvq::region_units(lay.km); a.vc = kvq::region_units(lay.vc);
     a.vm = kvq::region_units(lay.vm); a.tk = kvq::region_units(lay.tk); a.tv = kvq::region_units(lay.tv); a.vb = kvq::region_units(lay.vb);
     a.hq = d.num_q_heads; a.hkv = d.num_kv_heads; a.gk = d.key_group; a.gv = d.value_group; a.W = c->W;
-    a.split_tokens = p.per[k];  // units per workgroup
+    a.units_per_wg = p.per[k];
+    a.extra_units = p.extra[k];
     a.qscale = (float)(1.4426950408889634 / std::sqrt((double)d.head_dim));
     a.nqry = p.r.nqry; a.qpr = p.r.qpr; a.nrg = p.r.nrg; a.gqh = d.num_q_heads / d.num_kv_heads;
     a.pm = c->pm;
@@ -195,12 +213,14 @@ kvq_status attend(const kvq_cache* c, const void* q, int32_t n_q, int32_t window
       if (c->L[i] == 0) continue;
       kvq::DecodeSeq& s = a.seq[a.nseq++];
       s.head0 = c->head0[i];
-      s.seq = i; s.L = s.L_old = c->L[i]; s.Lq = c->Lq[i];
+      s.seq = i; s.L = c->L[i]; s.Lq = c->Lq[i];
+      s.L_old = p.real[i];
       s.nq = p.units[i]; s.nsplit = p.ns[i]; s.ws_base = p.base[i];
       s.wg_begin = p.begin[i];
     }
     a.total_wg = p.total[k];  // units
-    const int e = kvq::launch_block_tiles(a, c->type_k, c->type_v, p.r.rows, stream);
+    const int e = p.r.waves ? kvq::launch_block_rows(a, c->type_k, c->type_v, p.r.waves, stream)
+                            : kvq::launch_block_tiles(a, c->type_k, c->type_v, p.r.rows, stream);
     if (e) return kvq::hip_fail(e, "block-scaled attention launch");
   }
   for (int b = 0; b < d.batch; b += kvq::kMaxSeqPerLaunch) {

@@ -229,6 +229,11 @@ struct DecodeArgs {
   // a workgroup of its own, else the last split adds it; a sequence of one split is
   // written to out.  window = 0 elsewhere.
   int32_t window, sinks;
+  // attention over block-scaled caches: units of the launch's list (total_wg of them)
+  // that a workgroup takes; seq[].wg_begin is a sequence's first one, seq[].nq the
+  // units of a row group (many rows: of a kv head), seq[].L_old those of them that
+  // stand for work (tiles); extra_units (many rows): those of a row group that do not
+  int32_t units_per_wg, extra_units;
 };
 
 // The packed key groups that a row group of windowed attention reads: the sinks'
@@ -257,6 +262,27 @@ KVQ_WINDOW_HD inline WindowGroups window_groups(int32_t seen_first, int32_t seen
   const int32_t last = (int32_t)(((uint32_t)end + up) >> gk_shift);
   g.count = g.sink + (last > g.first ? last - g.first : 0);
   return g;
+}
+
+// Many rows over a block-scaled cache: the 32-token blocks that a group of
+// `step` queries reads, packed ones (of its key groups) and then the fp16 tail's, from
+// block tail0 of the sequence on.
+struct RowBlocks {
+  WindowGroups groups;
+  int32_t packed, tail0, total;
+};
+KVQ_WINDOW_HD inline RowBlocks row_blocks(int32_t nqry, int32_t step, int32_t L, int32_t Lq, int32_t gk_shift,
+                                          int32_t window, int32_t sinks, int32_t group) {
+  const int32_t q0 = group * step < nqry - 1 ? group * step : nqry - 1, q1 = q0 + step - 1 < nqry - 1 ? q0 + step - 1 : nqry - 1;
+  const int32_t first = L - nqry + 1 + q0, last = L - nqry + 1 + q1, from = first > window ? first - window : 0;
+  RowBlocks r;
+  r.groups = window_groups(first, last, Lq, gk_shift, window, sinks);
+  r.packed = r.groups.count << (gk_shift - 5);
+  r.tail0 = Lq / 32;
+  if (sinks <= Lq && from / 32 > r.tail0) r.tail0 = from / 32;
+  const int32_t end = (int32_t)(((int64_t)last + 31) / 32);
+  r.total = r.packed + (end > r.tail0 ? end - r.tail0 : 0);
+  return r;
 }
 
 struct MergeSeq {
@@ -412,6 +438,7 @@ int launch_append_block(const AppendArgs& a, const RotaryArgs* rot, int type_k, 
 int launch_dequant_block(const struct DequantArgs& a, void* stream);
 int launch_export_block(const struct ExportArgs& a, void* stream);
 int launch_block_tiles(const DecodeArgs& a, int type_k, int type_v, int rows, void* stream);
+int launch_block_rows(const DecodeArgs& a, int type_k, int type_v, int waves, void* stream);
 int launch_table_set(const TableSet& t, void* stream);
 // Zero the given 32-bit words of the arena (byte offsets), up to kTableSetMax per launch.
 struct WordReset {
