@@ -40,7 +40,6 @@ constexpr int kSlots = 4;           // blocks in LDS
 
 struct Operands {
   u4_t op[kSlots][16][64];    // of a block: keys (token half, 32 channels), values (16 channels)
-  float2 scale[kSlots];
   uint32_t big[kSlots][8];    // fp16 tail: whether any value of 16 channels is 8 or more
 };
 
@@ -53,8 +52,20 @@ struct Part {
 template <int NW>
 struct Staged {
   u4_t x[8 / NW];
-  float2 scale;
 };
+
+// Nothing moves across: products and vector instructions stay in the order written, one
+// beside the other.  (The compiler's own order, all products and then the weights, leaves
+// the matrix cores idle half of the time.)
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// lo halves of two numbers whose hi halves are h: each instruction reads a half as it is.
+__device__ __forceinline__ uint32_t low_halves(uint32_t h, float a, float b) {
+  float x, y;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(x) : "v"(h), "v"(a));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(h), "v"(b));
+  return mfma_ops::h2u((h2_t){(_Float16)x, (_Float16)y});
+}
 
 template <bool K8, bool V8, int NW>
 __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk, Operands& sm) {
@@ -96,42 +107,49 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
   }
 
   // ------------------------------------------------ blocks to LDS
+  // (pages come by vector loads two blocks ahead of their codes', scales three ahead of use:
+  // results arrive in the order asked for, and no block waits for its own)
   const bool paged = a.pm.table != nullptr;
-  auto load = [&](int b, Staged<NW>& o) __attribute__((always_inline)) {
-    const int t = place(b);
-    int in;
-    const uint8_t* seg = a.arena + packed_seg(a.pm, S.head0, a.head_stride, S.seq, wk.h, t, in);
-    const uint8_t* kr = seg + region(a.kc) + (size_t)in * kHeadDim;
-    const uint8_t* vr = seg + region(a.vc) + (size_t)in * kHeadDim;
-    const int n = wv & 3;
-    const uint32_t k_at = ((n >> 1) * 16 + col) * kHeadDim + (n & 1) * 64 + 16 * blk, v_at = n * 1024 + lane * 16;
-    if constexpr (NW == 8) {
-      o.x[0] = *reinterpret_cast<const u4_t*>(wv < 4 ? kr + k_at : vr + v_at);
-    } else {
-      o.x[0] = *reinterpret_cast<const u4_t*>(kr + k_at);
-      o.x[1] = *reinterpret_cast<const u4_t*>(vr + v_at);
-    }
-    o.scale = *reinterpret_cast<const float2*>(seg + region(a.km) + (size_t)(in >> gsh) * 8);
+  const uint8_t* head = a.arena + (paged ? a.pm.pool0 + (uint64_t)wk.h * a.pm.page_head_bytes : S.head0 + (uint64_t)wk.h * a.head_stride);
+  const int32_t* table = a.pm.table + (size_t)S.seq * a.pm.max_pages;
+  const int page_shift = paged ? a.pm.page_shift : 31, in_page = paged ? a.pm.page_tokens - 1 : 0x7FFFFFFF;
+  const uint64_t page_bytes = paged ? a.pm.page_bytes : 0;
+  int zero = 0;
+  asm("" : "+v"(zero));  // (keeps the loads' addresses in vector registers)
+  const int n = wv & 3;
+  const uint32_t k_at = ((n >> 1) * 16 + col) * kHeadDim + (n & 1) * 64 + 16 * blk, v_at = n * 1024 + lane * 16;
+  const bool key_wave = NW == 4 || wv < 4;
+  const uint64_t code0 = key_wave ? region(a.kc) : region(a.vc), value0 = region(a.vc), scale0 = region(a.km);
+  const uint32_t code_at = key_wave ? k_at : v_at;
+  auto page_of = [&](int b) { return paged ? table[(place(b) >> page_shift) + zero] : 0; };
+  auto load = [&](int b, int page, Staged<NW>& o) __attribute__((always_inline)) {
+    const int in = place(b) & in_page;
+    const uint8_t* seg = head + (uint64_t)(uint32_t)page * page_bytes + (size_t)in * kHeadDim;
+    o.x[0] = *reinterpret_cast<const u4_t*>(seg + code0 + code_at);
+    if constexpr (NW == 4) o.x[1] = *reinterpret_cast<const u4_t*>(seg + value0 + v_at);
   };
+  auto load_scale = [&](int b, int page) __attribute__((always_inline)) {
+    const int in = place(b) & in_page;
+    return *reinterpret_cast<const float2*>(head + (uint64_t)(uint32_t)page * page_bytes + scale0 + (size_t)((in >> gsh) + zero) * 8);
+  };
+  const int op_at = key_wave ? (n >> 1) * 4 + 2 * (n & 1) : 8 + 2 * n;
   auto put = [&](int b, const Staged<NW>& o) __attribute__((always_inline)) {
-    const int slot = b & (kSlots - 1), n = wv & 3;
-    u4_t(*op)[64] = sm.op[slot];
-    auto put_keys = [&](u4_t x) {
-      op[(n >> 1) * 4 + 2 * (n & 1)][lane] = __builtin_bit_cast(u4_t, block_ops::operand<K8>(x[0], x[1]));
-      op[(n >> 1) * 4 + 2 * (n & 1) + 1][lane] = __builtin_bit_cast(u4_t, block_ops::operand<K8>(x[2], x[3]));
+    u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
+    auto put2 = [&](auto e4m3, int i, u4_t x) __attribute__((always_inline)) {
+      op[i][lane] = __builtin_bit_cast(u4_t, block_ops::operand<decltype(e4m3)::value>(x[0], x[1]));
+      op[i + 1][lane] = __builtin_bit_cast(u4_t, block_ops::operand<decltype(e4m3)::value>(x[2], x[3]));
     };
-    auto put_values = [&](u4_t x) {
-      op[8 + 2 * n][lane] = __builtin_bit_cast(u4_t, block_ops::operand<V8>(x[0], x[1]));
-      op[8 + 2 * n + 1][lane] = __builtin_bit_cast(u4_t, block_ops::operand<V8>(x[2], x[3]));
-    };
-    if constexpr (NW == 8) {
-      if (wv < 4) put_keys(o.x[0]);
-      else put_values(o.x[0]);
+    using K = std::integral_constant<bool, K8>;
+    using V = std::integral_constant<bool, V8>;
+    if constexpr (NW == 4) {
+      put2(K{}, op_at, o.x[0]);
+      put2(V{}, 8 + 2 * n, o.x[1]);
+    } else if constexpr (K8 == V8) {
+      put2(K{}, op_at, o.x[0]);
     } else {
-      put_keys(o.x[0]);
-      put_values(o.x[1]);
+      if (key_wave) put2(K{}, op_at, o.x[0]);
+      else put2(V{}, op_at, o.x[0]);
     }
-    if (threadIdx.x == 0) sm.scale[slot] = o.scale;
   };
   // A block of the fp16 tail: raw halves; tokens past the sequence are zeros.
   auto put_tail = [&](int b) {
@@ -162,33 +180,39 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
   // ------------------------------------------------ rows
   float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f};
   f4_t acc[2][8];
-  block_ops::ValueUnit unit;
+  // Accumulators are in units of a reference value scale: a block's own enters its
+  // weights' exponent (block_ops.h)
+  float ref = 1.f;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[u][t] = (f4_t){0.f, 0.f, 0.f, 0.f};
 
-  auto scores = [&](int b, f4_t (&d)[2][2]) __attribute__((always_inline)) {
+  auto read_keys = [&](int b, u4_t (&k)[8]) __attribute__((always_inline)) {
     const u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
 #pragma unroll
-    for (int mb = 0; mb < 2; ++mb) {
+    for (int i = 0; i < 8; ++i) k[i] = op[i][lane];
+  };
+  auto score = [&](int i, const u4_t (&k)[8], f4_t (&d)[2][2]) __attribute__((always_inline)) {  // operand i: token half, 32 channels
 #pragma unroll
-      for (int u = 0; u < 2; ++u) d[u][mb] = (f4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        const h8_t k8 = __builtin_bit_cast(h8_t, op[mb * 4 + kb][lane]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) d[u][mb] = mfma(k8, __builtin_bit_cast(h8_t, q[u][kb]), d[u][mb]);
-      }
+    for (int u = 0; u < 2; ++u) {
+      const f4_t c = i & 3 ? d[u][i >> 2] : (f4_t){0.f, 0.f, 0.f, 0.f};
+      d[u][i >> 2] = mfma(__builtin_bit_cast(h8_t, k[i]), __builtin_bit_cast(h8_t, q[u][i & 3]), c);
     }
+  };
+  auto scores = [&](int b, f4_t (&d)[2][2]) __attribute__((always_inline)) {
+    u4_t k[8];
+    read_keys(b, k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) score(i, k, d);
   };
   const h8_t none = {0, 0, 0, 0, 0, 0, 0, 0};
   h8_t ph[2] = {none, none}, pl[2] = {none, none};  // weights of the block before
+  auto value_op = [&](int b, int mb) __attribute__((always_inline)) { return sm.op[b & (kSlots - 1)][8 + mb][lane]; };
   auto values = [&](int b) __attribute__((always_inline)) {
-    const u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) {
-      const h8_t v8 = __builtin_bit_cast(h8_t, op[8 + mb][lane]);
+      const h8_t v8 = __builtin_bit_cast(h8_t, value_op(b, mb));
 #pragma unroll
       for (int u = 0; u < 2; ++u) acc[u][mb] = mfma(v8, ph[u], acc[u][mb]);
 #pragma unroll
@@ -228,9 +252,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     }
   };
 
-  // Scores d of block b to weights; `after` (products of other blocks that need
-  // neither) runs beside the maxima, `before` beside the exponentials.
-  auto softmax = [&](int b, f4_t (&d)[2][2], float s_k, float s_v, auto after, auto before) __attribute__((always_inline)) {
+  auto mask = [&](int b, f4_t (&d)[2][2]) __attribute__((always_inline)) {
     const int t0 = place(b);
     if (t0 + 32 > wave_first || (t0 < wave_limit - a.window && t0 + 32 > a.sinks)) {
 #pragma unroll
@@ -238,92 +260,150 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
         const int left = lim[u] - t0 - 4 * blk, from = max(lim[u] - a.window, 0) - t0 - 4 * blk, sunk = a.sinks - t0 - 4 * blk;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int n = 16 * (e >> 2) + (e & 3);
-          float s = n < left && (n >= from || n < sunk) ? d[u][e >> 2][e & 3] : -__builtin_inff();
+          const int i = 16 * (e >> 2) + (e & 3);
+          float s = i < left && (i >= from || i < sunk) ? d[u][e >> 2][e & 3] : -__builtin_inff();
           asm volatile("" : "+v"(s));  // (a branch: blocks within every window pass it by)
           d[u][e >> 2][e & 3] = s;
         }
       }
     }
-    after();
-    float f[2], top[2], alpha[2] = {1.f, 1.f};
+  };
+  float f[2], top[2], alpha[2], ratio, s_v;  // of the block at hand
+  // Factors and maxima of scores d, half u of the rows.  (A block of zeros has scores 0 at
+  // any scale, where a hidden token's is -inf, and adds nothing in any unit.)
+  auto find_top = [&](int u, const f4_t (&d)[2][2], float2 scale) __attribute__((always_inline)) {
+    f[u] = ksc[u] * (scale.x > 0.f ? scale.x : 1.f);
+    const f4_t y = d[u][0], z = d[u][1];
+    top[u] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
+    top[u] = fmaxf(top[u] * f[u], kNoScore);
+  };
+  // References: rows above the limit, and a value scale too far off, move theirs; whether any did.
+  auto refer = [&](float2 scale) __attribute__((always_inline)) -> bool {
+    s_v = scale.y > 0.f ? scale.y : ref;
+    ratio = s_v * __builtin_amdgcn_rcpf(ref);
+    const bool far = ratio > 4.f || ratio < 0.25f;
+    if (__builtin_amdgcn_ballot_w64(top[0] - m[0] > kTop || top[1] - m[1] > kTop || far) == 0) return false;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f[u] = ksc[u] * (s_k > 0.f ? s_k : 1.f);  // (a block of zeros has scores 0 at any scale; a hidden token's is -inf)
-      const f4_t y = d[u][0], z = d[u][1];
-      top[u] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
-      top[u] = fmaxf(top[u] * f[u], kNoScore);
+      float t = fmaxf(top[u], __shfl_xor(top[u], 16));  // the row's maximum over its four lanes
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = t - m[u] > kTop ? t + (kHeadroom - kTop) : m[u];
+      alpha[u] = __builtin_amdgcn_exp2f(m[u] - mn) * (far ? ref / s_v : 1.f);
+      l[u] *= __builtin_amdgcn_exp2f(m[u] - mn);
+      m[u] = mn;
     }
-    const float change = unit.next(s_v);
-    bool moved = false;
-    if (__builtin_amdgcn_ballot_w64(top[0] - m[0] > kTop || top[1] - m[1] > kTop)) {
-      // the rows' maxima over their four lanes; rows above the limit move their reference
-      moved = true;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float t = fmaxf(top[u], __shfl_xor(top[u], 16));
-        t = fmaxf(t, __shfl_xor(t, 32));
-        const float mn = t - m[u] > kTop ? t + (kHeadroom - kTop) : m[u];
-        alpha[u] = __builtin_amdgcn_exp2f(m[u] - mn);
-        m[u] = mn;
-        l[u] *= alpha[u];
-      }
+    if (far) {
+      ref = s_v;
+      ratio = 1.f;
     }
-    before();
-    u4_t hw[2], lw[2];
+    return true;
+  };
+  auto rescale = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float bias = unit.up - m[u];
-      float sum = 0.f;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float x0 = d[u][t >> 1][2 * (t & 1)], x1 = d[u][t >> 1][2 * (t & 1) + 1];
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(x0, f[u], bias)), p1 = __builtin_amdgcn_exp2f(fmaf(x1, f[u], bias));
-        sum += p0 + p1;
-        const block_ops::Halves h = block_ops::split(p0, p1);
-        hw[u][t] = h.hi;
-        lw[u][t] = h.lo;
-      }
-      l[u] = fmaf(sum, unit.down, l[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      ph[u] = __builtin_bit_cast(h8_t, hw[u]);
-      pl[u] = __builtin_bit_cast(h8_t, lw[u]);
-    }
-    if (moved || change != 1.f) {  // after the products that belong to the old references
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int t = 0; t < 8; ++t) acc[u][t] *= alpha[u] * change;
-    }
+      for (int t = 0; t < 8; ++t) acc[u][t] *= alpha[u];
   };
 
   // packed blocks.  (LDS of the part before is read: its last barrier is behind that.)
   const int b0 = wk.b0, pe = min(wk.b1, rb.packed);
   if (b0 < pe) {
+    const int last = pe - 1;  // (past the last block: that one again, unused)
+    auto scalar_page = [&](int b) { return __builtin_amdgcn_readfirstlane(page_of(min(b, last))); };
     Staged<NW> s0, s1;
-    load(b0, s0);
-    load(min(b0 + 1, pe - 1), s1);
+    float2 c0, c1, c2;
+    {
+      const int p0 = scalar_page(b0), p1 = scalar_page(b0 + 1), p2 = scalar_page(b0 + 2);
+      load(b0, p0, s0);
+      load(min(b0 + 1, last), p1, s1);
+      c0 = load_scale(b0, p0);
+      c1 = load_scale(min(b0 + 1, last), p1);
+      c2 = load_scale(min(b0 + 2, last), p2);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) ksc[u] = a.qscale * block_ops::lift_query(q[u]);
-    for (int i = threadIdx.x; i < 8 * 64; i += 64 * NW)  // the values before the first block: zeros, of weights 0
-      sm.op[(b0 - 1) & (kSlots - 1)][8 + (i >> 6)][i & 63] = (u4_t){0u, 0u, 0u, 0u};
-    put(b0, s0);
-    load(min(b0 + 2, pe - 1), s0);
-    put(b0 + 1, s1);
-    load(min(b0 + 3, pe - 1), s1);
+      for (int u = 0; u < 2; ++u) ksc[u] = a.qscale * block_ops::lift_query(q[u]);
+      for (int i = threadIdx.x; i < 8 * 64; i += 64 * NW)  // the values before the first block: zeros, of weights 0
+        sm.op[(b0 - 1) & (kSlots - 1)][8 + (i >> 6)][i & 63] = (u4_t){0u, 0u, 0u, 0u};
+      put(b0, s0);
+      load(min(b0 + 2, last), p2, s0);
+      put(b0 + 1, s1);
+    }
+    int p3 = scalar_page(b0 + 3), p4 = page_of(min(b0 + 4, last));
+    load(min(b0 + 3, last), p3, s1);
+    if (c0.y > 0.f) ref = c0.y;
     __syncthreads();
     f4_t d[2][2], next[2][2];
     scores(b0, d);
-    // LDS holds b - 1 (values), b, b + 1; b + 2 is written, b + 4 asked for (past the last
-    // block: that one again, unused)
+    // LDS holds b - 1 (values), b, b + 1; b + 2 is written, b + 4 asked for
     for (int b = b0; b < pe; ++b) {
+      u4_t k[8], v[4];
+      read_keys(b + 1, k);  // (past the last block: whatever LDS holds, unused)
+      mask(b, d);
+      // the next block's scores beside the staging and this one's maxima
+      in_order();
+      score(0, k, next);
       put(b + 2, s0);
+      in_order();
+      score(1, k, next);
+      const int page = __builtin_amdgcn_readfirstlane(p4);
+      p4 = page_of(min(b + 5, last));
+      const float2 scale = c0;
+      c0 = c1;
+      c1 = c2;
+      in_order();
+      score(2, k, next);
+      c2 = load_scale(min(b + 3, last), p3);
+      p3 = page;
+      in_order();
+      score(3, k, next);
       s0 = s1;
-      load(min(b + 4, pe - 1), s1);
-      const float2 sc = sm.scale[b & (kSlots - 1)];
-      softmax(b, d, sc.x, block_ops::uniform(sc.y), [&]() { scores(b + 1, next); }, [&]() { values(b - 1); });
+      load(min(b + 4, last), page, s1);
+      in_order();
+      score(4, k, next);
+      find_top(0, d, scale);
+      in_order();
+      score(5, k, next);
+      find_top(1, d, scale);
+      in_order();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = value_op(b - 1, i);
+      score(6, k, next);
+      score(7, k, next);
+      const bool moved = refer(scale);
+      // the values of the block before beside this one's weights: four products, a pair of weights
+      const float up = __builtin_amdgcn_logf(ratio), down = __builtin_amdgcn_exp2f(-up);
+      const float bias[2] = {up - m[0], up - m[1]};
+      float sum[2] = {0.f, 0.f};
+      u4_t hw[2], lw[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int u = i >> 2, t = i & 3;
+        const h8_t v8 = __builtin_bit_cast(h8_t, v[i & 3]);
+        in_order();
+        acc[0][i] = mfma(v8, ph[0], acc[0][i]);
+        const float x0 = fmaf(d[u][t >> 1][2 * (t & 1)], f[u], bias[u]), x1 = fmaf(d[u][t >> 1][2 * (t & 1) + 1], f[u], bias[u]);
+        in_order();
+        acc[1][i] = mfma(v8, ph[1], acc[1][i]);
+        const float p0 = __builtin_amdgcn_exp2f(x0);
+        in_order();
+        acc[0][i] = mfma(v8, pl[0], acc[0][i]);
+        const float p1 = __builtin_amdgcn_exp2f(x1);
+        in_order();
+        acc[1][i] = mfma(v8, pl[1], acc[1][i]);
+        if (i < 4) v[i] = value_op(b - 1, i + 4);
+        sum[u] += p0 + p1;
+        uint32_t h = mfma_ops::h2u((h2_t){(_Float16)p0, (_Float16)p1});
+        asm("" : "+v"(h));
+        hw[u][t] = h;
+        lw[u][t] = low_halves(h, p0, p1);
+      }
+      in_order();
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        l[u] = fmaf(sum[u], down, l[u]);
+        ph[u] = __builtin_bit_cast(h8_t, hw[u]);
+        pl[u] = __builtin_bit_cast(h8_t, lw[u]);
+      }
+      if (moved) rescale();  // after the products that belong to the old references
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -342,7 +422,29 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     __syncthreads();
     f4_t d[2][2];
     scores(b, d);
-    softmax(b, d, 1.f, 1.f, []() {}, []() {});
+    mask(b, d);
+    const float2 scale = make_float2(1.f, 1.f);
+    find_top(0, d, scale);
+    find_top(1, d, scale);
+    if (refer(scale)) rescale();
+    const float up = __builtin_amdgcn_logf(ratio), down = __builtin_amdgcn_exp2f(-up);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float sum = 0.f;
+      u4_t hw, lw;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(d[u][t >> 1][2 * (t & 1)], f[u], up - m[u]));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(d[u][t >> 1][2 * (t & 1) + 1], f[u], up - m[u]));
+        sum += p0 + p1;
+        const block_ops::Halves h = block_ops::split(p0, p1);
+        hw[t] = h.hi;
+        lw[t] = h.lo;
+      }
+      l[u] = fmaf(sum, down, l[u]);
+      ph[u] = __builtin_bit_cast(h8_t, hw);
+      pl[u] = __builtin_bit_cast(h8_t, lw);
+    }
     tail_values(b);
     __syncthreads();
   }
@@ -356,14 +458,14 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     l[u] += __shfl_xor(l[u], 32);
     if (!live[u]) continue;
     if (S.nsplit == 1) {
-      const float r = unit.ref / l[u];
+      const float r = ref / l[u];
       float* o = a.out + ((size_t)S.seq * a.nqry * a.hq + at[u]) * kHeadDim + 4 * blk;
 #pragma unroll
       for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_any*>(o + 16 * t) = acc[u][t] * r;
     } else {
       float* rec = a.ws + ((size_t)(S.ws_base + wk.split) * a.hq * a.nqry + at[u]) * kRecFloats;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_t*>(rec + 4 + 16 * t + 4 * blk) = acc[u][t] * unit.ref;
+      for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_t*>(rec + 4 + 16 * t + 4 * blk) = acc[u][t] * ref;
       if (blk == 0) {
         rec[0] = l[u] > 0.f ? m[u] : -__builtin_inff();
         rec[1] = l[u];
