@@ -36,11 +36,14 @@ using mfma_ops::mfma;
 constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ratio up to 4
 constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
 constexpr float kNoScore = -1e30f;  // below any score
-constexpr int kSlots = 4;           // blocks in LDS
 
+// Blocks in LDS: with eight waves (a workgroup per compute unit) a barrier every
+// second block, so that waves come apart and one's products run beside another's weights.
+template <int NW>
 struct Operands {
-  u4_t op[kSlots][16][64];    // of a block: keys (token half, 32 channels), values (16 channels)
-  uint32_t big[kSlots][8];    // fp16 tail: whether any value of 16 channels is 8 or more
+  static constexpr int kSlots = NW == 8 ? 8 : 4, kAhead = NW == 8 ? 3 : 2;  // blocks written ahead
+  u4_t op[kSlots][16][64];  // of a block: keys (token half, 32 channels), values (16 channels)
+  uint32_t big[8];          // fp16 tail: whether any value of 16 channels is 8 or more
 };
 
 // A workgroup's blocks of one (sequence, kv head, group of rows).
@@ -68,7 +71,8 @@ __device__ __forceinline__ uint32_t low_halves(uint32_t h, float a, float b) {
 }
 
 template <bool K8, bool V8, int NW>
-__device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk, Operands& sm) {
+__device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk, Operands<NW>& sm) {
+  constexpr int kSlots = Operands<NW>::kSlots, kAhead = Operands<NW>::kAhead;
   const DecodeSeq& S = a.seq[wk.si];
   const uint8_t* ring = a.arena + S.head0 + (uint64_t)wk.h * a.head_stride;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -107,7 +111,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
   }
 
   // ------------------------------------------------ blocks to LDS
-  // (pages come by vector loads two blocks ahead of their codes', scales three ahead of use:
+  // (pages come by vector loads a block ahead of their codes', scales two ahead of use:
   // results arrive in the order asked for, and no block waits for its own)
   const bool paged = a.pm.table != nullptr;
   const uint8_t* head = a.arena + (paged ? a.pm.pool0 + (uint64_t)wk.h * a.pm.page_head_bytes : S.head0 + (uint64_t)wk.h * a.head_stride);
@@ -173,7 +177,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       op[w][lane] = k;
       op[8 + w][lane] = v;
       const bool big = __builtin_amdgcn_ballot_w64(top >= 0x4800u) != 0;  // 8.0
-      if (lane == 0) sm.big[b & (kSlots - 1)][w] = big;
+      if (lane == 0) sm.big[w] = big;
     }
   };
 
@@ -226,7 +230,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) {
       const u4_t w = op[8 + mb][lane];
-      const bool big = sm.big[b & (kSlots - 1)][mb] != 0;
+      const bool big = sm.big[mb] != 0;
       u4_t normal = {0u, 0u, 0u, 0u}, lifted;
       if (big) {
 #pragma unroll
@@ -310,53 +314,56 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
   if (b0 < pe) {
     const int last = pe - 1;  // (past the last block: that one again, unused)
     auto scalar_page = [&](int b) { return __builtin_amdgcn_readfirstlane(page_of(min(b, last))); };
-    Staged<NW> s0, s1;
-    float2 c0, c1, c2;
+    Staged<NW> st;
+    float2 c0, c1;
+    int pages[2];  // of blocks b + 2 and, kAhead = 3, b + 3
     {
-      const int p0 = scalar_page(b0), p1 = scalar_page(b0 + 1), p2 = scalar_page(b0 + 2);
-      load(b0, p0, s0);
-      load(min(b0 + 1, last), p1, s1);
-      c0 = load_scale(b0, p0);
-      c1 = load_scale(min(b0 + 1, last), p1);
-      c2 = load_scale(min(b0 + 2, last), p2);
+      Staged<NW> first[kAhead];
+      int at[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) at[i] = scalar_page(b0 + i);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) load(min(b0 + i, last), at[i], first[i]);
+      c0 = load_scale(b0, at[0]);
+      c1 = load_scale(min(b0 + 1, last), at[1]);
+      pages[0] = kAhead == 3 ? at[kAhead - 1] : scalar_page(b0 + 2);
+      pages[1] = scalar_page(b0 + 3);
 #pragma unroll
       for (int u = 0; u < 2; ++u) ksc[u] = a.qscale * block_ops::lift_query(q[u]);
       for (int i = threadIdx.x; i < 8 * 64; i += 64 * NW)  // the values before the first block: zeros, of weights 0
         sm.op[(b0 - 1) & (kSlots - 1)][8 + (i >> 6)][i & 63] = (u4_t){0u, 0u, 0u, 0u};
-      put(b0, s0);
-      load(min(b0 + 2, last), p2, s0);
-      put(b0 + 1, s1);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) put(b0 + i, first[i]);
     }
-    int p3 = scalar_page(b0 + 3), p4 = page_of(min(b0 + 4, last));
-    load(min(b0 + 3, last), p3, s1);
+    load(min(b0 + kAhead, last), pages[kAhead - 2], st);
+    int page_next = page_of(min(b0 + kAhead + 1, last));
     if (c0.y > 0.f) ref = c0.y;
     __syncthreads();
-    f4_t d[2][2], next[2][2];
-    scores(b0, d);
-    // LDS holds b - 1 (values), b, b + 1; b + 2 is written, b + 4 asked for
-    for (int b = b0; b < pe; ++b) {
+    f4_t d0[2][2], d1[2][2];
+    scores(b0, d0);
+    // LDS holds b - 1 (values), b, b + 1 .. ; b + kAhead is written, the one after it asked for
+    auto block = [&](int b, f4_t (&d)[2][2], f4_t (&next)[2][2]) __attribute__((always_inline)) {
       u4_t k[8], v[4];
       read_keys(b + 1, k);  // (past the last block: whatever LDS holds, unused)
       mask(b, d);
       // the next block's scores beside the staging and this one's maxima
       in_order();
       score(0, k, next);
-      put(b + 2, s0);
+      put(b + kAhead, st);
       in_order();
       score(1, k, next);
-      const int page = __builtin_amdgcn_readfirstlane(p4);
-      p4 = page_of(min(b + 5, last));
+      const int page = __builtin_amdgcn_readfirstlane(page_next);
+      page_next = page_of(min(b + kAhead + 2, last));
       const float2 scale = c0;
       c0 = c1;
-      c1 = c2;
       in_order();
       score(2, k, next);
-      c2 = load_scale(min(b + 3, last), p3);
-      p3 = page;
+      c1 = load_scale(min(b + 2, last), pages[0]);
+      pages[0] = kAhead == 3 ? pages[1] : page;
+      pages[1] = page;
       in_order();
       score(3, k, next);
-      s0 = s1;
-      load(min(b + 4, last), page, s1);
+      load(min(b + kAhead + 1, last), page, st);
       in_order();
       score(4, k, next);
       find_top(0, d, scale);
@@ -380,21 +387,26 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
         const h8_t v8 = __builtin_bit_cast(h8_t, v[i & 3]);
         in_order();
         acc[0][i] = mfma(v8, ph[0], acc[0][i]);
-        const float x0 = fmaf(d[u][t >> 1][2 * (t & 1)], f[u], bias[u]), x1 = fmaf(d[u][t >> 1][2 * (t & 1) + 1], f[u], bias[u]);
+        float x0 = fmaf(d[u][t >> 1][2 * (t & 1)], f[u], bias[u]), x1 = fmaf(d[u][t >> 1][2 * (t & 1) + 1], f[u], bias[u]);
+        asm volatile("" : "+v"(x0), "+v"(x1));
         in_order();
         acc[1][i] = mfma(v8, ph[1], acc[1][i]);
-        const float p0 = __builtin_amdgcn_exp2f(x0);
+        float p0 = __builtin_amdgcn_exp2f(x0);
+        asm volatile("" : "+v"(p0));
         in_order();
         acc[0][i] = mfma(v8, pl[0], acc[0][i]);
-        const float p1 = __builtin_amdgcn_exp2f(x1);
+        float p1 = __builtin_amdgcn_exp2f(x1);
+        asm volatile("" : "+v"(p1));
         in_order();
         acc[1][i] = mfma(v8, pl[1], acc[1][i]);
         if (i < 4) v[i] = value_op(b - 1, i + 4);
         sum[u] += p0 + p1;
         uint32_t h = mfma_ops::h2u((h2_t){(_Float16)p0, (_Float16)p1});
         asm("" : "+v"(h));
+        uint32_t low = low_halves(h, p0, p1);
+        asm volatile("" : "+v"(low), "+v"(sum[u]));  // (here, not after the products)
         hw[u][t] = h;
-        lw[u][t] = low_halves(h, p0, p1);
+        lw[u][t] = low;
       }
       in_order();
 #pragma unroll
@@ -404,10 +416,11 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
         pl[u] = __builtin_bit_cast(h8_t, lw[u]);
       }
       if (moved) rescale();  // after the products that belong to the old references
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int mb = 0; mb < 2; ++mb) d[u][mb] = next[u][mb];
+    };
+    for (int b = b0; b < pe; b += 2) {
+      block(b, d0, d1);
+      if (NW == 4) __syncthreads();
+      if (b + 1 < pe) block(b + 1, d1, d0);
       __syncthreads();
     }
     values(pe - 1);
@@ -490,7 +503,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
 // workgroup takes a.units_per_wg of them.
 template <bool K8, bool V8, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void block_rows_kernel(DecodeArgs a) {
-  __shared__ __attribute__((aligned(16))) Operands sm;
+  __shared__ __attribute__((aligned(16))) Operands<NW> sm;
   const int per = a.units_per_wg, end = min((int)(blockIdx.x + 1) * per, a.total_wg), gsh = __builtin_ctz(a.gk);
   const int nrw = (a.nrg + NW - 1) / NW;
   for (int u = blockIdx.x * per; u < end;) {
