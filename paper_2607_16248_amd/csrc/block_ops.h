@@ -40,6 +40,22 @@ __device__ __forceinline__ h8_t operand(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(h8_t, w);
 }
 
+// Exponent of the power of two that puts a half of pattern `top` (a magnitude) at 2^14 or
+// above: 0 .. 38.
+__device__ __forceinline__ int lift_of(uint32_t top) {
+  const int e = (int)(__builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)top)) >> 23) - 127;
+  return top == 0u ? 0 : max(14 - e, 0);
+}
+// Halves times 2^up, at most 2^15 at a time.
+__device__ __forceinline__ void lift_step(u4_t& w, int step) {
+  const _Float16 f = __builtin_bit_cast(_Float16, (uint16_t)((step + 15) << 10));
+#pragma unroll
+  for (int n = 0; n < 4; ++n) w[n] = h2u(u2h(w[n]) * (h2_t){f, f});
+}
+__device__ __forceinline__ void lift_halves(u4_t& w, int up) {  // up: the wave's
+  for (; up > 0; up -= 15) lift_step(w, min(up, 15));
+}
+
 // A row's query, times the power of two that puts its largest element at 2^14 or
 // above (elements 2^-28 of that and smaller would be subnormal halves, whose
 // products lose bits).  Returns the power's reciprocal.  The row's four lanes (16
@@ -54,17 +70,12 @@ __device__ __forceinline__ float lift_query(u4_t (&q)[4]) {
   uint32_t top = max((uint32_t)m.x, (uint32_t)m.y);
   top = max(top, (uint32_t)__shfl_xor((int)top, 16));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-  // exponent of the largest element: -24 .. 15
-  const int e = (int)(__builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)top)) >> 23) - 127;
-  int up = top == 0u ? 0 : max(14 - e, 0);  // 0 .. 38, at most 15 at a time
+  int up = lift_of(top);
   const float back = ldexpf(1.f, -up);
   do {
     const int step = min(up, 15);
-    const _Float16 f = __builtin_bit_cast(_Float16, (uint16_t)((step + 15) << 10));
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-      for (int n = 0; n < 4; ++n) q[kb][n] = h2u(u2h(q[kb][n]) * (h2_t){f, f});
+    for (int kb = 0; kb < 4; ++kb) lift_step(q[kb], step);
     up -= step;
   } while (__builtin_amdgcn_ballot_w64(up > 0) != 0);
   return back;
@@ -84,34 +95,9 @@ __device__ __forceinline__ Halves split(float a, float b) {
   return h;
 }
 
-// Accumulators are sums of weights times codes in units of a reference value
-// scale: a block's own scale enters its weights' exponent (up = log2 of scale over
-// reference, down = 2^-up for the sum of the weights).  A scale more than 4 times
-// off the reference becomes the reference; rescale() is then its change, else 1.
-struct ValueUnit {
-  float ref = 1.f, up = 0.f, down = 1.f;
-  bool set = false;
-  // the factor that the accumulators take
-  __device__ __forceinline__ float next(float scale) {
-    up = 0.f;
-    down = 1.f;
-    if (!(scale > 0.f)) return 1.f;  // (a block of zeros adds nothing in any unit)
-    if (!set) {
-      set = true;
-      ref = scale;
-      return 1.f;
-    }
-    const float ratio = scale * __builtin_amdgcn_rcpf(ref);
-    if (ratio <= 4.f && ratio >= 0.25f) {
-      up = __builtin_amdgcn_logf(ratio);
-      down = __builtin_amdgcn_exp2f(-up);
-      return 1.f;
-    }
-    const float f = ref / scale;
-    ref = scale;
-    return f;
-  }
-};
+// log2 of a block's value scale; of a block of zeros less than of any other (the
+// smallest scale is 2^-24 / 448).
+__device__ __forceinline__ float log_scale(float s) { return s > 0.f ? __builtin_amdgcn_logf(s) : -34.f; }
 
 // The sequence that holds unit u (DecodeSeq::wg_begin: its first unit): the last one
 // that begins at u or before.

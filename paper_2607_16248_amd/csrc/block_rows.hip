@@ -33,8 +33,8 @@ using block_ops::h8_t;
 using block_ops::u4_t;
 using mfma_ops::mfma;
 
-constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ratio up to 4
-constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
+constexpr float kTop = 14.f;        // weights stay below 2^14 ...
+constexpr float kHeadroom = 6.f;    // ... a new reference puts the largest at 2^8
 constexpr float kNoScore = -1e30f;  // below any score
 
 // Blocks in LDS: with eight waves (a workgroup per compute unit) a barrier every
@@ -43,7 +43,7 @@ template <int NW>
 struct Operands {
   static constexpr int kSlots = NW == 8 ? 8 : 4, kAhead = NW == 8 ? 3 : 2;  // blocks written ahead
   u4_t op[kSlots][16][64];  // of a block: keys (token half, 32 channels), values (16 channels)
-  uint32_t big[8];          // fp16 tail: whether any value of 16 channels is 8 or more
+  uint32_t top[8];          // fp16 tail: the pattern of the largest of 16 channels' values
 };
 
 // A workgroup's blocks of one (sequence, kv head, group of rows).
@@ -176,17 +176,15 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       }
       op[w][lane] = k;
       op[8 + w][lane] = v;
-      const bool big = __builtin_amdgcn_ballot_w64(top >= 0x4800u) != 0;  // 8.0
-      if (lane == 0) sm.big[w] = big;
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s));
+      if (lane == 0) sm.top[w] = top;
     }
   };
 
   // ------------------------------------------------ rows
   float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f};
   f4_t acc[2][8];
-  // Accumulators are in units of a reference value scale: a block's own enters its
-  // weights' exponent (block_ops.h)
-  float ref = 1.f;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -223,39 +221,6 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       for (int u = 0; u < 2; ++u) acc[u][mb] = mfma(v8, pl[u], acc[u][mb]);
     }
   };
-  // The tail's values: lifted by 2^12 while all are below 8, else their normal halves
-  // as they are and the subnormal ones lifted (products of those lose bits).
-  auto tail_values = [&](int b) {
-    const u4_t(*op)[64] = sm.op[b & (kSlots - 1)];
-#pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
-      const u4_t w = op[8 + mb][lane];
-      const bool big = sm.big[mb] != 0;
-      u4_t normal = {0u, 0u, 0u, 0u}, lifted;
-      if (big) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          uint32_t x, y;
-          mfma_ops::split_subnormal(w[t], x, y);
-          normal[t] = x;
-          lifted[t] = y;
-        }
-      } else {
-        lifted = __builtin_bit_cast(u4_t, mfma_ops::lifted(w, false));
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f4_t x = {0.f, 0.f, 0.f, 0.f};
-        x = mfma(__builtin_bit_cast(h8_t, lifted), ph[u], x);
-        x = mfma(__builtin_bit_cast(h8_t, lifted), pl[u], x);
-        acc[u][mb] = mfma(__builtin_bit_cast(h8_t, normal), ph[u], acc[u][mb]);
-        acc[u][mb] = mfma(__builtin_bit_cast(h8_t, normal), pl[u], acc[u][mb]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[u][mb][r] = fmaf(x[r], 1.f / mfma_ops::kLift, acc[u][mb][r]);
-      }
-    }
-  };
-
   auto mask = [&](int b, f4_t (&d)[2][2]) __attribute__((always_inline)) {
     const int t0 = place(b);
     if (t0 + 32 > wave_first || (t0 < wave_limit - a.window && t0 + 32 > a.sinks)) {
@@ -272,33 +237,29 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       }
     }
   };
-  float f[2], top[2], alpha[2], ratio, s_v;  // of the block at hand
-  // Factors and maxima of scores d, half u of the rows.  (A block of zeros has scores 0 at
-  // any scale, where a hidden token's is -inf, and adds nothing in any unit.)
+  // A block's value scale enters its weights' exponent, p = 2^(score + log2 s_v - m): the
+  // reference m goes by what a weight contributes, and numbers of any size keep their
+  // bits next to others.  The sum of the weights takes it out again.  (A block of zeros
+  // contributes nothing: a scale below any other; its scores are 0 at any scale, where a
+  // hidden token's is -inf.)
+  float f[2], top[2], alpha[2], up;  // of the block at hand
   auto find_top = [&](int u, const f4_t (&d)[2][2], float2 scale) __attribute__((always_inline)) {
     f[u] = ksc[u] * (scale.x > 0.f ? scale.x : 1.f);
     const f4_t y = d[u][0], z = d[u][1];
     top[u] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
-    top[u] = fmaxf(top[u] * f[u], kNoScore);
+    top[u] = fmaxf(fmaf(top[u], f[u], up), kNoScore);
   };
-  // References: rows above the limit, and a value scale too far off, move theirs; whether any did.
-  auto refer = [&](float2 scale) __attribute__((always_inline)) -> bool {
-    s_v = scale.y > 0.f ? scale.y : ref;
-    ratio = s_v * __builtin_amdgcn_rcpf(ref);
-    const bool far = ratio > 4.f || ratio < 0.25f;
-    if (__builtin_amdgcn_ballot_w64(top[0] - m[0] > kTop || top[1] - m[1] > kTop || far) == 0) return false;
+  // Rows above the limit move their references; whether any did.
+  auto refer = [&]() __attribute__((always_inline)) -> bool {
+    if (__builtin_amdgcn_ballot_w64(top[0] - m[0] > kTop || top[1] - m[1] > kTop) == 0) return false;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float t = fmaxf(top[u], __shfl_xor(top[u], 16));  // the row's maximum over its four lanes
       t = fmaxf(t, __shfl_xor(t, 32));
       const float mn = t - m[u] > kTop ? t + (kHeadroom - kTop) : m[u];
-      alpha[u] = __builtin_amdgcn_exp2f(m[u] - mn) * (far ? ref / s_v : 1.f);
-      l[u] *= __builtin_amdgcn_exp2f(m[u] - mn);
+      alpha[u] = __builtin_amdgcn_exp2f(m[u] - mn);
+      l[u] *= alpha[u];
       m[u] = mn;
-    }
-    if (far) {
-      ref = s_v;
-      ratio = 1.f;
     }
     return true;
   };
@@ -337,7 +298,6 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     }
     load(min(b0 + kAhead, last), pages[kAhead - 2], st);
     int page_next = page_of(min(b0 + kAhead + 1, last));
-    if (c0.y > 0.f) ref = c0.y;
     __syncthreads();
     f4_t d0[2][2], d1[2][2];
     scores(b0, d0);
@@ -355,6 +315,7 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       const int page = __builtin_amdgcn_readfirstlane(page_next);
       page_next = page_of(min(b + kAhead + 2, last));
       const float2 scale = c0;
+      up = block_ops::log_scale(scale.y);
       c0 = c1;
       in_order();
       score(2, k, next);
@@ -375,9 +336,9 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
       for (int i = 0; i < 4; ++i) v[i] = value_op(b - 1, i);
       score(6, k, next);
       score(7, k, next);
-      const bool moved = refer(scale);
+      const bool moved = refer();
       // the values of the block before beside this one's weights: four products, a pair of weights
-      const float up = __builtin_amdgcn_logf(ratio), down = __builtin_amdgcn_exp2f(-up);
+      const float down = __builtin_amdgcn_exp2f(-up);
       const float bias[2] = {up - m[0], up - m[1]};
       float sum[2] = {0.f, 0.f};
       u4_t hw[2], lw[2];
@@ -436,11 +397,17 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     f4_t d[2][2];
     scores(b, d);
     mask(b, d);
-    const float2 scale = make_float2(1.f, 1.f);
+    // values enter times the power of two that puts the block's largest at 2^14 or above
+    // (subnormal halves lose bits in products)
+    uint32_t most = 0u;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) most = max(most, sm.top[w]);
+    const int lift = block_ops::lift_of(most);
+    const float2 scale = make_float2(1.f, ldexpf(1.f, -lift));
+    up = (float)-lift;
     find_top(0, d, scale);
     find_top(1, d, scale);
-    if (refer(scale)) rescale();
-    const float up = __builtin_amdgcn_logf(ratio), down = __builtin_amdgcn_exp2f(-up);
+    if (refer()) rescale();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float sum = 0.f;
@@ -454,11 +421,19 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
         hw[t] = h.hi;
         lw[t] = h.lo;
       }
-      l[u] = fmaf(sum, down, l[u]);
+      l[u] = fmaf(sum, ldexpf(1.f, lift), l[u]);
       ph[u] = __builtin_bit_cast(h8_t, hw);
       pl[u] = __builtin_bit_cast(h8_t, lw);
     }
-    tail_values(b);
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      u4_t w = value_op(b, mb);
+      block_ops::lift_halves(w, lift);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) acc[u][mb] = mfma(__builtin_bit_cast(h8_t, w), ph[u], acc[u][mb]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) acc[u][mb] = mfma(__builtin_bit_cast(h8_t, w), pl[u], acc[u][mb]);
+    }
     __syncthreads();
   }
 
@@ -471,14 +446,14 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     l[u] += __shfl_xor(l[u], 32);
     if (!live[u]) continue;
     if (S.nsplit == 1) {
-      const float r = ref / l[u];
+      const float r = 1.f / l[u];
       float* o = a.out + ((size_t)S.seq * a.nqry * a.hq + at[u]) * kHeadDim + 4 * blk;
 #pragma unroll
       for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_any*>(o + 16 * t) = acc[u][t] * r;
     } else {
       float* rec = a.ws + ((size_t)(S.ws_base + wk.split) * a.hq * a.nqry + at[u]) * kRecFloats;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_t*>(rec + 4 + 16 * t + 4 * blk) = acc[u][t] * ref;
+      for (int t = 0; t < 8; ++t) *reinterpret_cast<f4_t*>(rec + 4 + 16 * t + 4 * blk) = acc[u][t];
       if (blk == 0) {
         rec[0] = l[u] > 0.f ? m[u] : -__builtin_inff();
         rec[1] = l[u];

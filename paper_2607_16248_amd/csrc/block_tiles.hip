@@ -3,11 +3,13 @@
 // rows of a kv head.
 //
 //   S^T = K Q^T   (16 tokens x 16 rows; codes as exact halves, q as the fp16 it is)
-//   p = 2^(s_k c S + log2(s_v / ref) - m),   O^T += V^T P^T   (p in hi + lo halves)
+//   p = 2^(s_k c S + log2 s_v - m),   O^T += V^T P^T   (p in hi + lo halves)
 //
 // with s_k, s_v the block's scales: one number each for all 32 tokens that a wave
 // takes at a time, so they enter as factors of scores and weights, and codes stay
-// the integers (or e4m3 numbers) they are.  Products are transposed, so a lane's
+// the integers (or e4m3 numbers) they are.  The reference m of a row goes by what its
+// weights contribute, not by the scores alone: values of blocks far apart in size keep
+// their bits.  Products are transposed, so a lane's
 // weights are the next product's operand without a lane exchange.  A lane reads 16
 // consecutive bytes of a key row (any order of channels does, the query has the
 // same), and values lie in operand order (kvq_layout.h, block_value).
@@ -38,8 +40,8 @@ using block_ops::h8_t;
 using block_ops::u4_t;
 using mfma_ops::mfma;
 
-constexpr float kTop = 13.f;        // weights stay below 2^13, times a scale ratio up to 4
-constexpr float kHeadroom = 6.f;    // a new reference puts the largest 2^7 below that
+constexpr float kTop = 14.f;        // weights stay below 2^14 ...
+constexpr float kHeadroom = 6.f;    // ... a new reference puts the largest at 2^8
 constexpr float kNoScore = -1e30f;  // below any score
 
 // What a wave reads of a 32-token block.
@@ -158,12 +160,11 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
   float ksc[NT];
 #pragma unroll
   for (int u = 0; u < NT; ++u) ksc[u] = a.qscale * block_ops::lift_query(q[u]);
-  float m[NT], most[NT], l[NT];
+  float m[NT], l[NT];
   f4_t acc[NT][8];
-  block_ops::ValueUnit unit;
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
-    m[u] = most[u] = kNoScore;
+    m[u] = kNoScore;
     l[u] = 0.f;
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[u][t] = (f4_t){0.f, 0.f, 0.f, 0.f};
@@ -174,13 +175,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
   auto attend = [&](int i) __attribute__((always_inline)) {
     const int next = min(i + 1, last);  // (after the last block: that one again, unused)
     const float s_k = block_ops::uniform(scale.x), s_v = block_ops::uniform(scale.y);
-    const float change = unit.next(s_v);
-    if (change != 1.f) {
-#pragma unroll
-      for (int u = 0; u < NT; ++u)
-#pragma unroll
-        for (int t = 0; t < 8; ++t) acc[u][t] *= change;
-    }
+    const float up = block_ops::log_scale(s_v), down = __builtin_amdgcn_exp2f(-up);
     f4_t d[NT][2];
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb) {
@@ -222,8 +217,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
       f[u] = ksc[u] * (s_k > 0.f ? s_k : 1.f);  // (a block of zeros has scores 0 at any scale; a hidden token's is -inf)
       const f4_t y = d[u][0], z = d[u][1];
       top[u] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
-      top[u] = fmaxf(top[u] * f[u], kNoScore);
-      most[u] = fmaxf(most[u], top[u]);
+      top[u] = fmaxf(fmaf(top[u], f[u], up), kNoScore);
       over |= top[u] - m[u] > kTop;
     }
     if (__builtin_amdgcn_ballot_w64(over)) {
@@ -242,7 +236,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
     }
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      const float bias = unit.up - m[u];
+      const float bias = up - m[u];
       float sum = 0.f;
       u4_t hw, lw;
 #pragma unroll
@@ -254,7 +248,7 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
         hw[t] = h.hi;
         lw[t] = h.lo;
       }
-      l[u] = fmaf(sum, unit.down, l[u]);
+      l[u] = fmaf(sum, down, l[u]);
       ph[u] = __builtin_bit_cast(h8_t, hw);
       pl[u] = __builtin_bit_cast(h8_t, lw);
     }
@@ -278,14 +272,10 @@ __device__ __forceinline__ void attend_part(const DecodeArgs& a, const Part& wk,
   for (int u = 0; u < NT; ++u) {
     l[u] += __shfl_xor(l[u], 16);
     l[u] += __shfl_xor(l[u], 32);
-    most[u] = fmaxf(most[u], __shfl_xor(most[u], 16));
-    most[u] = fmaxf(most[u], __shfl_xor(most[u], 32));
-    const float to_max = l[u] > 0.f ? __builtin_amdgcn_exp2f(m[u] - most[u]) : 0.f;  // records are relative to the maximum
-    st.m[u] = l[u] > 0.f ? most[u] : -__builtin_inff();
-    st.l[u] = l[u] * to_max;
-    const float f = unit.ref * to_max;
+    st.m[u] = l[u] > 0.f ? m[u] : -__builtin_inff();
+    st.l[u] = l[u];
 #pragma unroll
-    for (int t = 0; t < 8; ++t) st.acc[u][t] = acc[u][t] * f;
+    for (int t = 0; t < 8; ++t) st.acc[u][t] = acc[u][t];
   }
   if (S.L > S.Lq && wk.u1 == S.L_old) {  // the fp16 tail
     TailState<NT> tail;

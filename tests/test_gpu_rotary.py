@@ -1,0 +1,180 @@
+"""Rotated appends on the GPU: queries and the cache's bytes equal those of rows that were
+rotated in 64 bits, rounded once to fp16 and appended as they are; every class,
+contiguous, paged and block-scaled; no tolerance.
+"""
+import numpy as np
+import pytest
+
+from block_oracle import rotate
+from paper_2607_16248_amd import BlockCache, KVCache, KvqError, kvq
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def tables(rows, rot, seed=0, far=0):
+    """Angles of positions far, far + 1, ... (seed > 0: any angles)."""
+    if seed:
+        a = np.random.default_rng(seed).uniform(-np.pi, np.pi, (rows, rot // 2))
+    else:
+        a = (far + np.arange(rows))[:, None] * 10000.0 ** (-np.arange(0, rot, 2) / rot)
+    return np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
+
+
+def make(kind, b, gq, hkv, cap, block, R, page):
+    if kind in ("i8", "e4m3"):
+        return BlockCache(b, gq * hkv, hkv, cap, kind, block_tokens=block, fp16_window=R, page_tokens=page)
+    return KVCache(b, gq * hkv, hkv, cap, [kind[0]] * b, [kind[1]] * b, key_group=block, value_group=32, fp16_window=R,
+                   page_tokens=page)
+
+
+def half_of(x):
+    """fp16 numbers of a (fp16 or bf16) tensor, as numpy."""
+    return x.float().cpu().numpy().astype(np.float16)
+
+
+def images(c, b, hkv):
+    return [c.export(s, h) for s in range(b) for h in range(hkv)]
+
+
+@pytest.mark.parametrize("kind,block,R,page", [
+    ((1, 1), 32, 0, 0), ((2, 2), 32, 40, 128), ((4, 4), 64, 0, 0), ((8, 8), 128, 130, 0), ((2, 8), 32, 7, 0),
+    ("i8", 32, 0, 0), ("e4m3", 64, 40, 256), ("e4m3", 128, 0, 0), ("i8", 64, 200, 0)])
+@pytest.mark.parametrize("dtype,rot,pairs", [("float16", 128, False), ("bfloat16", 128, True), ("bfloat16", 64, False),
+                                             ("float16", 96, False), ("float16", 16, True)])
+def test_bytes_of_rotated_rows(kind, block, R, page, dtype, rot, pairs):
+    b, gq, hkv, cap = 3, 5 if rot == 96 else 2, 2, 420
+    hq, dt = gq * hkv, getattr(torch, dtype)
+    a, ref = (make(kind, b, gq, hkv, cap, block, R, page) for _ in range(2))
+    cos, sin = tables(cap, rot)
+    cd, sd = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    g = torch.Generator(device="cuda").manual_seed(7)
+    at = [0] * b
+    for step, n_new in enumerate([[150, 1, 0], [1, 1, 1], [33, 140, 90], [0, 5, 64], [1, 0, 1]]):
+        n = max(n_new) + (step == 2)  # (rows behind the longest, too)
+        # one buffer of queries, keys and values side by side
+        rows = torch.randn((b, n, hq + 2 * hkv, 128), generator=g, device="cuda").to(dt)
+        q, k, v = rows[:, :, :hq], rows[:, :, hq:hq + hkv], rows[:, :, hq + hkv:]
+        if step % 2:
+            k = k.contiguous()
+        q_out = torch.full((b, n, hq, 128), 7.0, device="cuda", dtype=torch.float16)
+        got = a.append_rotary(q, k, v, cd, sd, n_new, pairs=pairs, q_out=q_out)
+        assert got is q_out
+        kr, qr, vh = (np.full((b, n, h, 128), 7.0, np.float16) for h in (hkv, hq, hkv))
+        for s in range(b):
+            m, p = n_new[s], slice(at[s], at[s] + n_new[s])
+            kr[s, :m], qr[s, :m] = (rotate(half_of(x[s, :m]) if dt == torch.float16 else x[s, :m].float().cpu().numpy(),
+                                           cos[p], sin[p], pairs) for x in (k, q))
+            vh[s, :m] = half_of(v[s, :m])
+        assert np.array_equal(q_out.cpu().numpy(), qr)
+        ref.append(torch.from_numpy(kr).cuda(), torch.from_numpy(vh).cuda(), n_new)
+        at = [p + m for p, m in zip(at, n_new)]
+        assert [a.seq_len(s) for s in range(b)] == at
+        assert all(np.array_equal(x, y) for x, y in zip(images(a, b, hkv), images(ref, b, hkv))), step
+    a.check()
+    dec = torch.randn((b, hq, 128), generator=g, device="cuda", dtype=torch.float16)
+    assert torch.equal(a.decode(dec), ref.decode(dec))
+
+
+@pytest.mark.parametrize("kind", [(4, 4), "e4m3"])
+def test_given_positions(kind):
+    b, hkv, gq, rows, n = 2, 2, 4, 50, 70
+    cos, sin = tables(rows, 128, seed=3)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    at = torch.randint(0, rows, (b, n), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.randn((b, n, hkv, 128), generator=g, device="cuda", dtype=torch.float16)
+    q = torch.randn((b, n, hkv * gq, 128), generator=g, device="cuda", dtype=torch.float16)
+    a, ref = (make(kind, b, gq, hkv, 100, 32, 0, 0) for _ in range(2))
+    cd, sd = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    out = a.append_rotary(q, x, x, cd, sd, positions=at)
+    p = at.cpu().numpy()
+    turned = np.stack([rotate(x[s].cpu().numpy(), cos[p[s]], sin[p[s]], False) for s in range(b)])
+    ref.append(torch.from_numpy(turned).cuda(), x)
+    assert all(np.array_equal(y, z) for y, z in zip(images(a, b, hkv), images(ref, b, hkv)))
+    want = np.stack([rotate(q[s].cpu().numpy(), cos[p[s]], sin[p[s]], False) for s in range(b)])
+    assert np.array_equal(out.cpu().numpy(), want)
+    a.check()
+    # positions outside the tables are row 0's, and reported
+    c = make(kind, b, gq, hkv, 100, 32, 0, 0)
+    bad = at.clone()
+    bad[1, 3], bad[0, 69] = rows, -1
+    c.append_rotary(None, x, x, cd, sd, positions=bad)
+    with pytest.raises(KvqError) as e:
+        c.check()
+    assert e.value.status == kvq.ERR_RANGE
+    p = np.where((p := bad.cpu().numpy()) % rows == p, p, 0)
+    turned = np.stack([rotate(x[s].cpu().numpy(), cos[p[s]], sin[p[s]], False) for s in range(b)])
+    ref2 = make(kind, b, gq, hkv, 100, 32, 0, 0)
+    ref2.append(torch.from_numpy(turned).cuda(), x)
+    assert all(np.array_equal(y, z) for y, z in zip(images(c, b, hkv), images(ref2, b, hkv)))
+
+
+def test_angles_far_out_and_roundings():
+    """Positions beyond a million; products that cancel, subnormal results, ties between two halves."""
+    rng = np.random.default_rng(2)
+    n, rot = 64, 128
+    cos, sin = tables(n, rot, far=3_000_000)
+    cos[:8], sin[:8] = np.float32(0.5), np.float32(0.5)  # a / 2 - b / 2: ties of halves are exact here
+    cos[8:16], sin[8:16] = np.float32(2.0 ** -12), np.float32(1 + 2.0 ** -20)
+    x = rng.integers(0, 0x7C00, (1, n, 2, 128)).astype(np.uint16).view(np.float16)
+    x = (x * rng.choice([-1, 1], x.shape)).astype(np.float16)
+    x[0, 20:] = (rng.standard_normal((n - 20, 2, 128)) * 2.0 ** -13).astype(np.float16)
+    x[0, 40:, :, 64:] = x[0, 40:, :, :64]  # a cos - a sin
+    x = np.clip(x, -30000, 30000)
+    c = BlockCache(1, 4, 2, n, "i8", fp16_window=n)  # (all tokens stay fp16)
+    xd = torch.from_numpy(x).cuda()
+    q = xd.repeat(1, 1, 2, 1).contiguous()
+    out = c.append_rotary(q, xd, xd, torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda())
+    assert np.array_equal(out.cpu().numpy()[0], rotate(q.cpu().numpy()[0], cos, sin, False))
+    Kd, _ = c.dequant(0, 0, n)
+    assert np.array_equal(Kd.cpu().numpy(), rotate(x[0], cos, sin, False).astype(np.float32))
+
+
+def test_rows_that_are_not_aligned():
+    """Rows that begin at odd elements, strides that are no multiple of 8."""
+    b, n, hq, hkv, rot = 2, 40, 4, 2, 128
+    cos, sin = tables(n + 1, rot)
+    width = (hq + 2 * hkv) * 128 + 3
+    buf = torch.randn((b * n * width + 1,), device="cuda", dtype=torch.float16)
+    rows = buf[1:].view(b, n, width)
+    q, k, v = (rows[:, :, s:s + h * 128].unflatten(2, (h, 128)) for s, h in ((0, hq), (hq * 128, hkv), ((hq + hkv) * 128, hkv)))
+    t = torch.zeros((cos.size + 1, 2), device="cuda").T.contiguous()  # tables at a 4-byte border only
+    t[0, 1:], t[1, 1:] = torch.from_numpy(cos).cuda().view(-1), torch.from_numpy(sin).cuda().view(-1)
+    cd, sd = t[0, 1:].view(cos.shape), t[1, 1:].view(sin.shape)
+    for kind in ((2, 2), "e4m3"):
+        a, ref = (make(kind, b, 2, hkv, n, 32, 0, 0) for _ in range(2))
+        out = a.append_rotary(q, k, v, cd, sd)
+        turned = np.stack([rotate(k[s].cpu().numpy(), cos[:n], sin[:n], False) for s in range(b)])
+        ref.append(torch.from_numpy(turned).cuda(), v.contiguous())
+        assert all(np.array_equal(x, y) for x, y in zip(images(a, b, hkv), images(ref, b, hkv)))
+        assert np.array_equal(out.cpu().numpy()[1], rotate(q[1].cpu().numpy(), cos[:n], sin[:n], False))
+
+
+def test_values_that_overflow_fp16():
+    """bf16 beyond fp16's range is reported once it is packed."""
+    x = torch.full((1, 32, 2, 128), 1.0, device="cuda", dtype=torch.bfloat16)
+    y = x.clone()
+    y[0, 5, 1, 9] = 1e6
+    cos, sin = (torch.from_numpy(t).cuda() for t in tables(32, 128))
+    for K, V in ((y, x), (x, y)):
+        for kind in ((4, 4), "i8"):
+            c = make(kind, 1, 1, 2, 64, 32, 0, 0)
+            c.append_rotary(None, K, V, cos, sin)
+            with pytest.raises(KvqError) as e:
+                c.check()
+            assert e.value.status == kvq.ERR_RANGE
+
+
+def test_another_stream():
+    b, n, hkv = 2, 100, 2
+    cos, sin = (torch.from_numpy(t).cuda() for t in tables(n, 128))
+    x = torch.randn((b, n, hkv, 128), device="cuda", dtype=torch.float16)
+    q = torch.randn((b, n, 8, 128), device="cuda", dtype=torch.float16)
+    a, c = (make("e4m3", b, 4, hkv, n, 32, 0, 0) for _ in range(2))
+    want = a.append_rotary(q, x, x, cos, sin)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = c.append_rotary(q, x, x, cos, sin, stream=side)
+    side.synchronize()
+    assert torch.equal(want, got)
+    assert all(np.array_equal(y, z) for y, z in zip(images(a, b, hkv), images(c, b, hkv)))
