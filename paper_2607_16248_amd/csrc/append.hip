@@ -443,7 +443,7 @@ __device__ __forceinline__ uint32_t quantize_values(const AppendArgs& a, int bv,
 }
 
 // ROT: rows of a rotated append (rot), whose fresh keys turn as they are loaded.
-template <int GK, bool AL, bool ROT>
+template <int GK, bool AL, int ROT>
 __device__ __forceinline__ void quantize_group(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h, int gi,
                                                int bk, int bv, uint32_t* minmax, uint32_t* par) {
   uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;  // the fp16 ring's region
@@ -465,13 +465,13 @@ __device__ __forceinline__ void quantize_group(const AppendArgs& a, const Rotary
       const int p = p0 + 32 * b + value_token(wv, t);
       vx[t] = load2<AL>(rv.at(p) + 2 * lane);
       if constexpr (ROT) {
-        if (p >= S.L_old) vx[t] = rotary::to_half2(vx[t], rot->bf16 != 0);
+        if (p >= S.L_old) vx[t] = rotary::to_half2<ROT>(vx[t]);
       }
     }
   };
   load_v(0);
   if constexpr (ROT) {
-    const rotary::Turn turn(*rot, lane);
+    const rotary::Turn<ROT> turn(*rot, lane);
 #pragma unroll
     for (int i = 0; i < GK / 16; ++i) {
       const int p = p0 + 16 * i + 4 * wv + row;
@@ -580,12 +580,16 @@ __device__ __forceinline__ void quantize_group(const AppendArgs& a, const Rotary
   }
 }
 
-template <int GK, bool AL, bool ROT>
+template <int GK, bool AL, int ROT>
 __device__ __forceinline__ void append_group(const AppendArgs& a, const RotaryArgs* rot, int bk, int bv) {
   __shared__ __attribute__((aligned(16))) uint32_t minmax[4 * 128], par[192];
   const int wg = blockIdx.x;
   int si = 0;
-  for (int i = 1; i < a.nseq; ++i) si = (a.seq[i].wg_begin <= wg) ? i : si;
+  if constexpr (ROT) {
+    si = sequence_of(a, wg);
+  } else {
+    for (int i = 1; i < a.nseq; ++i) si = (a.seq[i].wg_begin <= wg) ? i : si;
+  }
   const AppendSeq& S = a.seq[si];
   // kv heads fastest: neighbouring workgroups read neighbouring 256-byte rows
   const int local = wg - S.wg_begin, part = local / a.hkv, h = local - part * a.hkv;
@@ -595,17 +599,18 @@ __device__ __forceinline__ void append_group(const AppendArgs& a, const RotaryAr
   } else if (!ROT || part < nquant + S.n_copy) {
     copy_ring<AL, ROT>(a, rot, S, h, part - nquant);
   } else if constexpr (ROT) {
-    rotary::turn_queries(a, *rot, S, h, part - nquant - S.n_copy);
+    const PartHead q = part_head(local - (nquant + S.n_copy) * a.hkv, S.n_query, a.hkv);
+    rotary::turn_queries<ROT>(a, *rot, S, q.h, q.part);
   }
 }
 
 template <int GK, bool AL>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int bk, int bv) {
-  append_group<GK, AL, false>(a, nullptr, bk, bv);
+  append_group<GK, AL, rotary::kNone>(a, nullptr, bk, bv);
 }
-template <int GK, bool AL>
+template <int GK, bool AL, int ROT>
 __global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(AppendArgs a, RotaryArgs rot, int bk, int bv) {
-  append_group<GK, AL, true>(a, &rot, bk, bv);
+  append_group<GK, AL, ROT>(a, &rot, bk, bv);
 }
 
 __global__ __launch_bounds__(256) void table_set_kernel(TableSet t) {
@@ -647,28 +652,34 @@ int launch_append(const AppendArgs& a, int bk, int bv, void* stream) {
   return (int)hipGetLastError();
 }
 
+namespace {
+
+template <int GK>
+int launch_turned(const AppendArgs& a, const RotaryArgs& r, int bk, int bv, hipStream_t s) {
+  const dim3 grid(a.total_wg), block(kAppendThreads);
+  const bool al = r.aligned != 0;
+  if (r.bf16) {
+    if (al) hipLaunchKernelGGL((append_rotary_kernel<GK, true, rotary::kBrain>), grid, block, 0, s, a, r, bk, bv);
+    else hipLaunchKernelGGL((append_rotary_kernel<GK, false, rotary::kBrain>), grid, block, 0, s, a, r, bk, bv);
+  } else {
+    if (al) hipLaunchKernelGGL((append_rotary_kernel<GK, true, rotary::kHalf>), grid, block, 0, s, a, r, bk, bv);
+    else hipLaunchKernelGGL((append_rotary_kernel<GK, false, rotary::kHalf>), grid, block, 0, s, a, r, bk, bv);
+  }
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
 int launch_append_rotary(const AppendArgs& a, const RotaryArgs* rot, int bk, int bv, void* stream) {
   if (rot == nullptr) return launch_append(a, bk, bv, stream);
   if (a.total_wg <= 0) return 0;
-  const bool al = rot->aligned != 0;
-  const dim3 grid(a.total_wg), block(kAppendThreads);
   hipStream_t s = (hipStream_t)stream;
   switch (a.gk) {
-    case 32:
-      if (al) hipLaunchKernelGGL((append_rotary_kernel<32, true>), grid, block, 0, s, a, *rot, bk, bv);
-      else hipLaunchKernelGGL((append_rotary_kernel<32, false>), grid, block, 0, s, a, *rot, bk, bv);
-      break;
-    case 64:
-      if (al) hipLaunchKernelGGL((append_rotary_kernel<64, true>), grid, block, 0, s, a, *rot, bk, bv);
-      else hipLaunchKernelGGL((append_rotary_kernel<64, false>), grid, block, 0, s, a, *rot, bk, bv);
-      break;
-    case 128:
-      if (al) hipLaunchKernelGGL((append_rotary_kernel<128, true>), grid, block, 0, s, a, *rot, bk, bv);
-      else hipLaunchKernelGGL((append_rotary_kernel<128, false>), grid, block, 0, s, a, *rot, bk, bv);
-      break;
+    case 32: return launch_turned<32>(a, *rot, bk, bv, s);
+    case 64: return launch_turned<64>(a, *rot, bk, bv, s);
+    case 128: return launch_turned<128>(a, *rot, bk, bv, s);
     default: return (int)hipErrorInvalidValue;
   }
-  return (int)hipGetLastError();
 }
 
 int launch_table_set(const TableSet& t, void* stream) {

@@ -43,9 +43,31 @@ struct Rows {
   }
 };
 
+// The sequence of a workgroup: the last one that begins at it or before.  One load for
+// all of them: asked for one after another, 64 of them took 15 us.
+__device__ __forceinline__ int sequence_of(const AppendArgs& a, int wg) {
+  static_assert(kMaxSeqPerLaunch <= 64, "one lane per sequence");
+  if (a.nseq == 1) return 0;
+  const int lane = threadIdx.x & 63;
+  const auto* args = (const AppendArgs*)__builtin_amdgcn_kernarg_segment_ptr();  // (indexed by lane, `a` would be copied)
+  const int begin = args->seq[min(lane, kMaxSeqPerLaunch - 1)].wg_begin;
+  return __popcll(__builtin_amdgcn_ballot_w64(lane < a.nseq && begin <= wg)) - 1;
+}
+
+// Workgroup `local` of parts x hkv as (part, kv head).  The heads of a part sit 8 apart,
+// on one XCD, whose L2 then holds its tokens' angles for all of them.
+struct PartHead {
+  int part, h;
+};
+__device__ __forceinline__ PartHead part_head(int local, int parts, int hkv) {
+  const int chunk = local / (8 * hkv), r = local - chunk * 8 * hkv;
+  if (8 * chunk + 8 <= parts) return {8 * chunk + (r & 7), r >> 3};
+  return {8 * chunk + r / hkv, r % hkv};
+}
+
 // Copy part `part` (kCopyTokens tokens) of the new tokens that stay fp16 into
 // the ring of head h.
-template <bool AL, bool ROT>
+template <bool AL, int ROT>
 __device__ __forceinline__ void copy_ring(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h, int part) {
   uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;
   const int first = max(S.Lq_new, S.L_old) + part * kCopyTokens, end = min(S.L_new, first + kCopyTokens);
@@ -61,12 +83,12 @@ __device__ __forceinline__ void copy_ring(const AppendArgs& a, const RotaryArgs*
       x[0][i] = load8<AL>(a.K + token * ks + at);
       x[1][i] = load8<AL>(a.V + token * vs + at);
       if constexpr (ROT) {
-        const rotary::Turn turn(*rot, threadIdx.x & 63);
+        const rotary::Turn<ROT> turn(*rot, threadIdx.x & 63);
         rotary::Angles g;
         turn.load(*rot, rotary::table_row(*rot, a.arena, (int64_t)token, p), g);
         x[0][i] = turn.apply(x[0][i], g);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) x[1][i][n] = rotary::to_half2(x[1][i][n], rot->bf16 != 0);
+        for (int n = 0; n < 4; ++n) x[1][i][n] = rotary::to_half2<ROT>(x[1][i][n]);
       }
     }
   }

@@ -60,27 +60,40 @@ __device__ __forceinline__ float e4m3_value(uint32_t m) {
 
 // Codes of eight elements (four pairs of halves), a byte each.
 __device__ __forceinline__ uint2 whole_codes(const uint32_t (&x)[4], Scale g) {
-  uint32_t w[2] = {0u, 0u};
-  const float h = 0.5f * g.s;
+  if (g.s == 0.f) return make_uint2(0x80808080u, 0x80808080u);
+  constexpr float kWhole = 0x1.8p23f + 128.f;  // the sum's low byte: f + 128, f whole, ties to even
+  uint32_t c[8];
+  float most = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float v = g.s == 0.f ? 0.f : half_at(x[e >> 1], e & 1);
-    float f = __builtin_rintf(v * g.rs);
-    const float d = fmaf(-f, g.s, v), n = __builtin_fabsf(d);
-    const bool odd = ((int)f & 1) != 0;
-    if (n > h || (n == h && odd && g.s != 0.f)) f += __builtin_copysignf(1.f, d);
-    w[e >> 2] |= (uint32_t)((int)f + 128) << (8 * (e & 3));
+    const float y = half_at(x[e >> 1], e & 1) * g.rs, at = y + kWhole;
+    most = fmaxf(most, __builtin_fabsf(y - (at - kWhole)));
+    c[e] = __builtin_bit_cast(uint32_t, at);
   }
+  if (__builtin_amdgcn_ballot_w64(most > 0.5f - 0x1p-13f)) {
+    const float h = 0.5f * g.s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = fmaf(kWhole - __builtin_bit_cast(float, c[e]), g.s, half_at(x[e >> 1], e & 1)), n = __builtin_fabsf(d);
+      if (n > h || (n == h && (c[e] & 1u))) c[e] += d > 0.f ? 1u : ~0u;
+    }
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    w[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[4 * k + 3], c[4 * k + 2], 0x0C0C0400u),
+                                 __builtin_amdgcn_perm(c[4 * k + 1], c[4 * k], 0x0C0C0400u), 0x05040100u);
   return make_uint2(w[0], w[1]);
 }
 __device__ __forceinline__ uint2 e4m3_codes(const uint32_t (&x)[4], Scale g) {
-  float y[8];
-  bool near = false;
+  if (g.s == 0.f) return make_uint2(0u, 0u);
+  float y[8], least = __builtin_inff();
+  uint32_t middle = ~0u;  // the low 20 bits of an estimate are its place between two numbers
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    y[e] = g.s == 0.f ? 0.f : half_at(x[e >> 1], e & 1) * g.rs;
-    const uint32_t u = __builtin_bit_cast(uint32_t, y[e]) & 0x7FFFFFFFu;
-    near |= ((u + 0x80008u) & 0xFFFFFu) <= 0x10u || (u < 0x3C800000u && u != 0u);  // 2^-6
+    y[e] = half_at(x[e >> 1], e & 1) * g.rs;
+    middle = min(middle, (__builtin_bit_cast(uint32_t, y[e]) << 12) + (0x80008u << 12));
+    least = fminf(least, __builtin_fabsf(y[e]));
   }
   int w[2];
 #pragma unroll
@@ -88,23 +101,23 @@ __device__ __forceinline__ uint2 e4m3_codes(const uint32_t (&x)[4], Scale g) {
     w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
     w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], w[k], true);
   }
-  if (__builtin_amdgcn_ballot_w64(near)) {
+  if (__builtin_amdgcn_ballot_w64(middle <= 0x10u << 12 || least < 0x1p-6f)) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int sh = 8 * (e & 3);
       const uint32_t code = ((uint32_t)w[e >> 2] >> sh) & 0xFFu, m = code & 0x7Fu;
-      const float v = __builtin_fabsf(g.s == 0.f ? 0.f : half_at(x[e >> 1], e & 1));
+      const float v = __builtin_fabsf(half_at(x[e >> 1], e & 1));
       const float at = e4m3_value(m), d = fmaf(-at, g.s, v);
       const uint32_t other = d > 0.f ? m + 1u : m - (m > 0u ? 1u : 0u);
       const float r = fmaf(-0.5f * (at + e4m3_value(other)), g.s, v);  // beyond the middle?
       const bool move = d > 0.f ? r > 0.f || (r == 0.f && (m & 1u)) : d < 0.f && (r < 0.f || (r == 0.f && (m & 1u)));
-      if (move && g.s != 0.f) w[e >> 2] = (int)(((uint32_t)w[e >> 2] & ~(0xFFu << sh)) | (((code & 0x80u) | other) << sh));
+      if (move) w[e >> 2] = (int)(((uint32_t)w[e >> 2] & ~(0xFFu << sh)) | (((code & 0x80u) | other) << sh));
     }
   }
   return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
 }
 
-template <int GK, bool AL, bool ROT>
+template <int GK, bool AL, int ROT>
 __device__ __forceinline__ void quantize_block(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h,
                                                int gi, bool k8, bool v8, uint32_t* tops) {
   const uint8_t* ring = a.arena + S.head0 + (uint64_t)h * a.head_stride;
@@ -124,7 +137,7 @@ __device__ __forceinline__ void quantize_block(const AppendArgs& a, const Rotary
 #pragma unroll
     for (int t = 0; t < 8; ++t) vx[b][t] = load2<AL>(rv.at(p0 + 32 * b + value_token(wv, t)) + 2 * lane);
   if constexpr (ROT) {
-    const rotary::Turn turn(*rot, lane);
+    const rotary::Turn<ROT> turn(*rot, lane);
 #pragma unroll
     for (int i = 0; i < GK / 16; ++i) {
       const int p = p0 + 16 * i + 4 * wv + row;
@@ -133,12 +146,12 @@ __device__ __forceinline__ void quantize_block(const AppendArgs& a, const Rotary
       turn.load(*rot, rotary::table_row(*rot, a.arena, (int64_t)(token0 + (p - S.L_old)), p), g);
       kx[i] = turn.apply(kx[i], g);
     }
-    if (rot->bf16) {
+    if constexpr (ROT == rotary::kBrain) {
 #pragma unroll
       for (int b = 0; b < GK / 32; ++b)
 #pragma unroll
         for (int t = 0; t < 8; ++t)
-          if (p0 + 32 * b + value_token(wv, t) >= S.L_old) vx[b][t] = rotary::to_half2(vx[b][t], true);
+          if (p0 + 32 * b + value_token(wv, t) >= S.L_old) vx[b][t] = rotary::to_half2<ROT>(vx[b][t]);
     }
   }
   uint32_t mk = 0u, mv = 0u;
@@ -188,38 +201,39 @@ __device__ __forceinline__ void quantize_block(const AppendArgs& a, const Rotary
   }
 }
 
-template <int GK, bool AL, bool ROT>
+template <int GK, bool AL, int ROT>
 __device__ __forceinline__ void append_part(const AppendArgs& a, const RotaryArgs* rot, bool k8, bool v8) {
   __shared__ uint32_t tops[4];
   const int wg = blockIdx.x;
-  int si = 0;
-  for (int i = 1; i < a.nseq; ++i) si = (a.seq[i].wg_begin <= wg) ? i : si;
-  const AppendSeq& S = a.seq[si];
-  const int local = wg - S.wg_begin, part = local / a.hkv, h = local - part * a.hkv;
+  const AppendSeq& S = a.seq[sequence_of(a, wg)];
   const int nquant = a.quantize ? S.n_quant : 0;
-  if (part < nquant) {
-    quantize_block<GK, AL, ROT>(a, rot, S, h, part, k8, v8, tops);
-  } else if (!ROT || part < nquant + S.n_copy) {
-    copy_ring<AL, ROT>(a, rot, S, h, part - nquant);
+  int local = wg - S.wg_begin;
+  if (local < nquant * a.hkv) {
+    const PartHead q = part_head(local, nquant, a.hkv);
+    quantize_block<GK, AL, ROT>(a, rot, S, q.h, q.part, k8, v8, tops);
+  } else if (local -= nquant * a.hkv; !ROT || local < S.n_copy * a.hkv) {
+    copy_ring<AL, ROT>(a, rot, S, local % a.hkv, local / a.hkv);
   } else if constexpr (ROT) {
-    rotary::turn_queries(a, *rot, S, h, part - nquant - S.n_copy);
+    const PartHead q = part_head(local - S.n_copy * a.hkv, S.n_query, a.hkv);
+    rotary::turn_queries<ROT>(a, *rot, S, q.h, q.part);
   }
 }
 
 template <int GK, bool AL>
 __global__ __launch_bounds__(kAppendThreads) void append_block_kernel(AppendArgs a, bool k8, bool v8) {
-  append_part<GK, AL, false>(a, nullptr, k8, v8);
+  append_part<GK, AL, rotary::kNone>(a, nullptr, k8, v8);
 }
-template <int GK, bool AL>
+template <int GK, bool AL, int ROT>
 __global__ __launch_bounds__(kAppendThreads) void append_block_rotary_kernel(AppendArgs a, RotaryArgs rot, bool k8, bool v8) {
-  append_part<GK, AL, true>(a, &rot, k8, v8);
+  append_part<GK, AL, ROT>(a, &rot, k8, v8);
 }
 
 template <int GK, bool AL>
 int launch_blocks(const AppendArgs& a, const RotaryArgs* rot, bool k8, bool v8, hipStream_t s) {
   const dim3 grid(a.total_wg), block(kAppendThreads);
-  if (rot) hipLaunchKernelGGL((append_block_rotary_kernel<GK, AL>), grid, block, 0, s, a, *rot, k8, v8);
-  else hipLaunchKernelGGL((append_block_kernel<GK, AL>), grid, block, 0, s, a, k8, v8);
+  if (rot == nullptr) hipLaunchKernelGGL((append_block_kernel<GK, AL>), grid, block, 0, s, a, k8, v8);
+  else if (rot->bf16) hipLaunchKernelGGL((append_block_rotary_kernel<GK, AL, rotary::kBrain>), grid, block, 0, s, a, *rot, k8, v8);
+  else hipLaunchKernelGGL((append_block_rotary_kernel<GK, AL, rotary::kHalf>), grid, block, 0, s, a, *rot, k8, v8);
   return (int)hipGetLastError();
 }
 

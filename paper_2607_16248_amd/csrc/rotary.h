@@ -1,10 +1,15 @@
 // Rotation of queries and keys by their positions, as the append kernels apply it
 // to the rows that they read (include/kvq.h, kvq_append_rotary):
 //   a' = a cos - b sin,  b' = a sin + b cos
-// for channels (a, b) of a pair.  Products of an fp16 (or bf16) number and an
-// fp32 one are exact in fp64, so the sum is rounded there to 53 bits and once more
-// to fp16: the quantizer that follows sees the numbers that the mathematics gives,
-// and the bytes do not depend on how a compiler fuses.
+// for channels (a, b) of a pair, as if in 64 bits (products of an fp16 or bf16 number and
+// an fp32 one are exact there) and rounded once to fp16: the quantizer that follows
+// sees the numbers that the mathematics gives, and the bytes do not depend on how a
+// compiler fuses.  Nearly all of them come from fp32 all the same: with q = fl(b sin)
+// and its exact rest e (one fma), v = fl(fl(a cos - q) - e) is within 1.5 ulp of the
+// exact sum, so its rounding to fp16 is right unless v lies within 2 ulp of the border
+// of two halves (one number in 1600).  Those take the 64-bit way.  All in fp64, whose
+// conversions run at a quarter of the rate: 16384 tokens of 32 query and 8 kv heads
+// 164 us, 100 so; the bytes alone take 60.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -20,11 +25,15 @@ typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef f4_t f4_any __attribute__((aligned(4)));
 
-__device__ __forceinline__ float from16(uint32_t bits, bool bf16) {
-  return bf16 ? __builtin_bit_cast(float, bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+// What a row holds (RotaryArgs::bf16), as the kernels' template argument.
+enum Rows16 { kNone = 0, kHalf = 1, kBrain = 2 };
+
+// Element e (0 or 1) of a pair.
+template <int T>
+__device__ __forceinline__ float at16(uint32_t v, int e) {
+  if constexpr (T == kBrain) return __builtin_bit_cast(float, e ? v & 0xFFFF0000u : v << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(e ? v >> 16 : v));
 }
-__device__ __forceinline__ float lo16(uint32_t v, bool bf16) { return from16(v & 0xFFFFu, bf16); }
-__device__ __forceinline__ float hi16(uint32_t v, bool bf16) { return from16(v >> 16, bf16); }
 
 // Two fp32 numbers as fp16, rounded to nearest (v_cvt_pk of the default mode).
 __device__ __forceinline__ uint32_t pack16(float a, float b) {
@@ -32,41 +41,67 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
 }
 // Inputs as fp16 numbers (exact for fp16; bf16 rounds below 2^-14 and overflows
 // to infinity, which the packing reports).
-__device__ __forceinline__ uint32_t to_half2(uint32_t v, bool bf16) {
-  return bf16 ? pack16(lo16(v, true), hi16(v, true)) : v;
+template <int T>
+__device__ __forceinline__ uint32_t to_half2(uint32_t v) {
+  if constexpr (T == kBrain) return pack16(at16<T>(v, 0), at16<T>(v, 1));
+  return v;
 }
 
-// d as an fp32 number that rounds to fp16 as d itself does.  Only an fp32 number
-// on the border between two halves can go wrong: it takes its last bit from the
-// side that d is on.
-__device__ __forceinline__ float near_border(double d, float f) {
+// Whether the number that v stands for may round to another half than v does: v within
+// 2 ulp of a border of halves, among the subnormal ones, whose borders lie elsewhere, or
+// not finite, which only the 64-bit way tells apart.
+__device__ __forceinline__ bool near_border(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+  return ((u + 0x1002u) & 0x1FFFu) <= 4u || (u < 0x38800000u && u != 0u) || u >= 0x7F800000u;
+}
+// d as an fp32 number that rounds to fp16 as d itself does: where the conversion is not
+// exact, its last bit says on which side of every border d is.
+__device__ __forceinline__ float to_odd(double d) {
+  const float f = (float)d;
   const double back = (double)f;
   if (back == d) return f;
   const uint32_t u = __builtin_bit_cast(uint32_t, f);
-  const bool further = __builtin_fabs(d) > __builtin_fabs(back);
-  return __builtin_bit_cast(float, further ? u | 1u : (u - 1u) | 1u);
+  return __builtin_bit_cast(float, __builtin_fabs(d) > __builtin_fabs(back) ? u | 1u : (u - 1u) | 1u);
 }
-__device__ __forceinline__ bool on_border(float f) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, f) & 0x7FFFFFFFu;
-  return (u & 0x1FFFu) == 0x1000u || (u < 0x38800000u && u != 0u);  // (subnormal halves: every number is looked at)
+// f[e] = x[e] c[e] + y[e] s[e], exact but for the one rounding that packs it.  near_border
+// is tested over the eight at once (a border's distance is what the 19 low bits hold, and
+// maximum passes a NaN on), and element by element only in waves where one failed: about
+// every fourth.
+__device__ __forceinline__ void turned(float (&f)[8], const float (&x)[8], const float (&c)[8], const float (&y)[8],
+                                       const float (&s)[8]) {
+  uint32_t border = ~0u;
+  float least = __builtin_inff(), most = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float q = y[e] * s[e], rest = fmaf(y[e], s[e], -q);
+    f[e] = fmaf(x[e], c[e], q) + rest;
+    border = min(border, (__builtin_bit_cast(uint32_t, f[e]) << 19) + (0x1002u << 19));
+    least = fminf(least, __builtin_fabsf(f[e]));
+    most = __builtin_elementwise_maximum(most, __builtin_fabsf(f[e]));
+  }
+  if (__builtin_amdgcn_ballot_w64(border <= 4u << 19 || least < 0x1p-14f || !(most < __builtin_inff()))) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (near_border(f[e])) f[e] = to_odd(__builtin_fma((double)x[e], (double)c[e], (double)y[e] * (double)s[e]));
+  }
 }
 
-// Eight angles of a lane: pairs j0 .. j0 + 7 (neighbours: j0 .. j0 + 3).
+// A lane's angles, by channel: a channel turns to x c + y s, y the other one of its pair.
 struct Angles {
-  double c[8], s[8];
+  float c[8], s[8];
 };
 
 // Channels 8 cc .. 8 cc + 7 of a row (16 lanes in a row of lanes hold one), whose
 // angles are in g.  All 16 lanes are active.
+template <int T>
 struct Turn {
   int rot, half, cc;  // half: in lanes
-  bool pairs, bf16, turns, second;
+  bool pairs, turns, second;
   int partner;        // lane of the other halves
-  int j0;
+  int j0;             // its first angle, of 8 (neighbours: of 4)
   __device__ __forceinline__ Turn(const RotaryArgs& r, int lane) {
     rot = r.rot;
     pairs = r.pairs != 0;
-    bf16 = r.bf16 != 0;
     cc = lane & 15;
     half = rot >> 4;
     turns = 8 * cc < rot;
@@ -85,51 +120,36 @@ struct Turn {
       c1 = *reinterpret_cast<const f4_any*>(c + 4);
       s1 = *reinterpret_cast<const f4_any*>(s + 4);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int n = e & 3;
-      g.c[e] = e < 4 ? c0[n] : c1[n];
-      g.s[e] = e < 4 ? s0[n] : s1[n];
-    }
-  }
-  // the row's 8 channels x as rotated halves
-  __device__ __forceinline__ u4_t apply(u4_t x, const Angles& g) const {
-    u4_t y;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) y[n] = (uint32_t)__shfl((int)x[n], partner);
-    u4_t o;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) o[n] = to_half2(x[n], bf16);
-    if (!turns) return o;
-    double d[8];
     if (pairs) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const double a = lo16(x[n], bf16), b = hi16(x[n], bf16);
-        d[2 * n] = __builtin_fma(a, g.c[n], -(b * g.s[n]));
-        d[2 * n + 1] = __builtin_fma(a, g.s[n], b * g.c[n]);
+      for (int e = 0; e < 8; ++e) {
+        g.c[e] = c0[e >> 1];
+        g.s[e] = e & 1 ? s0[e >> 1] : -s0[e >> 1];
       }
     } else {
+      const float sign = second ? 1.f : -1.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double own = e & 1 ? hi16(x[e >> 1], bf16) : lo16(x[e >> 1], bf16);
-        const double other = e & 1 ? hi16(y[e >> 1], bf16) : lo16(y[e >> 1], bf16);
-        const double t = other * g.s[e];
-        d[e] = __builtin_fma(own, g.c[e], second ? t : -t);
+        g.c[e] = e < 4 ? c0[e & 3] : c1[e & 3];
+        g.s[e] = sign * (e < 4 ? s0[e & 3] : s1[e & 3]);
       }
     }
-    float f[8];
-    bool any = false;
+  }
+  // the row's 8 channels v as rotated halves
+  __device__ __forceinline__ u4_t apply(u4_t v, const Angles& g) const {
+    u4_t w, o;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) w[n] = pairs ? __builtin_amdgcn_alignbit(v[n], v[n], 16) : (uint32_t)__shfl((int)v[n], partner);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o[n] = to_half2<T>(v[n]);
+    if (!turns) return o;
+    float x[8], y[8], f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      f[e] = (float)d[e];
-      any |= on_border(f[e]);
+      x[e] = at16<T>(v[e >> 1], e & 1);
+      y[e] = at16<T>(w[e >> 1], e & 1);
     }
-    if (__builtin_amdgcn_ballot_w64(any)) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (on_border(f[e])) f[e] = near_border(d[e], f[e]);
-    }
+    turned(f, x, g.c, y, g.s);
 #pragma unroll
     for (int n = 0; n < 4; ++n) o[n] = pack16(f[2 * n], f[2 * n + 1]);
     return o;
@@ -155,13 +175,14 @@ __device__ __forceinline__ u4_t load_row8(const uint16_t* p, bool aligned) {
 }
 
 // The queries of tokens part * kQueryTokens .. of a sequence, heads of kv head h.
+template <int T>
 __device__ __forceinline__ void turn_queries(const AppendArgs& a, const RotaryArgs& r, const AppendSeq& S, int h, int part) {
   static_assert(kQueryTokens * 16 == kAppendThreads, "a lane per 8 channels of a token");
   typedef u4_t u4_any __attribute__((aligned(4)));
   const int i = part * kQueryTokens + (threadIdx.x >> 4);
   if (i >= S.L_new - S.L_old) return;
   const int64_t token = (int64_t)S.seq * a.n_max + i;
-  const Turn turn(r, threadIdx.x & 63);
+  const Turn<T> turn(r, threadIdx.x & 63);
   Angles g;
   turn.load(r, table_row(r, a.arena, token, S.L_old + i), g);
   const uint16_t* in = r.q + token * r.q_stride + (int64_t)h * r.gqh * kHeadDim + 8 * turn.cc;
