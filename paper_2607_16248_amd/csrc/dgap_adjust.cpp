@@ -50,7 +50,12 @@ extern "C" kvq_status dgap_adjust(const dgap_adjustment* p, void* out, int64_t o
   a.mask_row = p->mask_row;
   a.mask_stride = p->mask_stride;
   a.batch = p->batch; a.vocab = p->vocab; a.history = p->history; a.biases = p->biases; a.mask_rows = p->mask_rows;
-  a.nchunk = (p->vocab + 7 + kvq::kAdjustChunk - 1) / kvq::kAdjustChunk;
+  a.wide = p->history > kvq::kAdjustCount;
+  // every chunk of a row reads the row's whole history: longer chunks where that is much,
+  // as long as they fill the chip
+  const int many = (p->vocab + 7 + kvq::kAdjustLong - 1) / kvq::kAdjustLong;
+  a.chunk = !a.wide && p->history >= 2048 && (int64_t)p->batch * many >= 512 ? kvq::kAdjustLong : kvq::kAdjustChunk;
+  a.nchunk = (p->vocab + 7 + a.chunk - 1) / a.chunk;
   // every row lies as far from a 16-byte border in as out
   const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(p->logits));
   a.runs = apart % (8 * size) == 0 && ((out_row_stride - p->row_stride) % 8 == 0 || p->batch == 1);

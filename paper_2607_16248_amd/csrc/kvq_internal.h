@@ -348,7 +348,9 @@ struct SampleArgs {
 
 // ---------------------------------------------------------------- adjusted logits
 
-constexpr int kAdjustChunk = 4096;  // logits per workgroup
+constexpr int kAdjustChunk = 4096, kAdjustLong = 16384;  // logits per workgroup
+constexpr int kAdjustPerThread = 16;
+constexpr int kAdjustCount = 0x7FFF;                     // the most that a packed table counts
 
 struct AdjustArgs {
   const void* logits;
@@ -366,7 +368,8 @@ struct AdjustArgs {
   const int32_t* mask_row;
   int64_t mask_stride;             // words
   int32_t batch, vocab, history, biases, mask_rows;
-  int32_t nchunk;                  // chunks of a row
+  int32_t chunk, nchunk;           // logits per chunk, chunks of a row
+  int32_t wide;                    // 1: histories beyond kAdjustCount
   int32_t runs;                    // 1: runs of 8 logits lie alike in memory, in and out (16-byte accesses)
 };
 
