@@ -10,12 +10,16 @@
 // four waves takes a (sequence, kv head, block): it reads every element once into
 // registers, the lanes as the packed caches' kernel (append.hip) has them, finds
 // both maxima with one barrier, and packs.
-// Codes are exact without a division.  Whole numbers: the rounded estimate f of
-// x / s leaves d = x - f s, exact in one fma (f s has 31 bits, and |d| < s), and
-// |d| against s / 2 says whether f or its neighbour is nearest.  e4m3: the hardware's
+// Codes are exact without a division.  Whole numbers: the rounded estimate f of x / s
+// is right unless the estimate lies within 2^-13 of the middle of two (its error is
+// below 2^-15); there d = x - f s, exact in one fma (f s has 31 bits, and |d| < s),
+// against s / 2 says whether f or its neighbour is nearest.  e4m3: the hardware's
 // conversion of the estimate is right unless that lies within 8 steps of fp32 from
 // the middle of two numbers, or among the subnormal ones; there the sign of
-// x - m s, m the middle, decides (exact: one fma).
+// x - m s, m the middle, decides (exact: one fma).  A wave looks for such elements
+// over eight at once.
+// 8 kv heads, blocks of 128 whole numbers: 16384 tokens 32 us (3.1 TB/s), rotated 49, with
+// 32 query heads 100 (3.7 TB/s); what is left of those is the arithmetic.
 #include <hip/hip_runtime.h>
 
 #include "append_common.h"

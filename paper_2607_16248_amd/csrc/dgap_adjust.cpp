@@ -51,10 +51,11 @@ extern "C" kvq_status dgap_adjust(const dgap_adjustment* p, void* out, int64_t o
   a.mask_stride = p->mask_stride;
   a.batch = p->batch; a.vocab = p->vocab; a.history = p->history; a.biases = p->biases; a.mask_rows = p->mask_rows;
   a.wide = p->history > kvq::kAdjustCount;
-  // every chunk of a row reads the row's whole history: longer chunks where that is much,
-  // as long as they fill the chip
+  // Every chunk of a row reads the row's whole history: long chunks where that is much, as
+  // long as there are enough of them for every CU (512 rows of 128256 fp16, short and long
+  // chunks: histories of 1024 tokens 62 us and 62, 4096 72 and 70, 8192 89 and 77).
   const int many = (p->vocab + 7 + kvq::kAdjustLong - 1) / kvq::kAdjustLong;
-  a.chunk = !a.wide && p->history >= 2048 && (int64_t)p->batch * many >= 512 ? kvq::kAdjustLong : kvq::kAdjustChunk;
+  a.chunk = !a.wide && p->history >= 4096 && (int64_t)p->batch * many >= 512 ? kvq::kAdjustLong : kvq::kAdjustChunk;
   a.nchunk = (p->vocab + 7 + a.chunk - 1) / a.chunk;
   // every row lies as far from a 16-byte border in as out
   const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(p->logits));
