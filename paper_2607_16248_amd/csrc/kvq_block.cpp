@@ -24,8 +24,11 @@ struct Rows {
   int groups = 1;  // that take parts of their own: row groups, or workgroups' sets of them
 };
 
-// Many rows from so many (query, head) rows of a kv head on.
-constexpr int kManyRows = 64;
+// Many rows from so many (query, head) rows of a kv head on.  32 query and 8 kv heads,
+// e4m3, 16 sequences of 8000 to 16384 tokens: 64 rows 169 us in tiles and 199 in the other
+// kernel, 128 rows 281 and 189; one sequence of 16384: 64 rows 40 and 43, 96 rows 42 and
+// 46, 128 rows 49 and 51, 256 rows 50 and 50, 512 rows 78 and 73.
+constexpr int kManyRows = 96;
 
 Rows rows_for(const kvq_cache* c, int nqry) {
   const int gqh = c->d.num_q_heads / c->d.num_kv_heads;
@@ -35,6 +38,7 @@ Rows rows_for(const kvq_cache* c, int nqry) {
   r.qpr = std::min(nqry, r.rows / gqh);
   r.nrg = r.groups = (nqry + r.qpr - 1) / r.qpr;
   if (nqry * gqh >= kManyRows) {
+    // (five groups: 53 us with eight waves, 58 with four; three: 51 and 47)
     r.waves = r.nrg > 4 ? 8 : 4;
     r.groups = (r.nrg + r.waves - 1) / r.waves;
   }
@@ -73,8 +77,10 @@ int32_t tile_extra(int32_t tail, int32_t G, int64_t share) {
   const int64_t tokens = std::min<int64_t>((tail > 0 ? tail + 64 - G : 0) + kPartTokens, share * G / 4);
   return std::max(0, (int32_t)((tokens + G - 1) / G));
 }
-// Many rows: the same, in blocks.
-constexpr int kRowExtra = 8;
+// Many rows: the same, in blocks.  512 rows of 5 sequences of 300 to 16384 tokens, 384 of
+// 16 of 2000 to 16384: 302 us without them, 173 and 482 with 8, 143 and 491 with 16, 144
+// and 515 with 32.
+constexpr int kRowExtra = 16;
 
 // What a call's launches are given: the list of work units of a launch's sequences, of
 // which every workgroup takes `per`.
