@@ -77,6 +77,50 @@ def test_against_64_bits(kind, n, vocab, history, biases, states):
         assert torch.equal(buf[rest], before[rest])
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("biases", [0, 40])
+@pytest.mark.parametrize("vocab,shift", [(16384, 0), (16389, 3), (33333, 1)])
+def test_many_rows_with_long_histories(kind, biases, vocab, shift):
+    n = 520 if vocab <= 16384 else 300
+    kw = settings(n, vocab, 4100, biases, 3, vocab + biases)
+    g = torch.Generator(device="cuda").manual_seed(vocab + 1)
+    width = vocab + 8 - vocab % 8
+    buf = (4 * torch.randn((n * width + 8,), generator=g, device="cuda")).to(TYPES[kind])
+    z = buf[shift:shift + n * width].view(n, width)[:, :vocab]
+    out = torch.empty((n, vocab), device="cuda", dtype=TYPES[kind])
+    dgap_adjust(z, out, **kw)
+    check(z, out, **kw)
+    dgap_adjust(z, **kw)  # in place: runs of 16 bytes
+    assert torch.equal(z.nan_to_num(nan=123.0), out.nan_to_num(nan=123.0))
+
+
+@pytest.mark.parametrize("history", [32767, 32768, 70000])
+@pytest.mark.parametrize("prompt", [0, 1, 32768])
+def test_one_token_again_and_again(history, prompt):
+    n, vocab = 3, 5000
+    z = torch.randn((n, vocab), device="cuda")
+    one = torch.ones((n,), device="cuda")
+    kw = {"tokens": torch.full((n, history), 4097, device="cuda", dtype=torch.int32),
+          "length": torch.tensor([history, history - 1, 1], device="cuda", dtype=torch.int32),
+          "prompt": torch.full((n,), prompt, device="cuda", dtype=torch.int32), "repetition": 1.5 * one, "presence": 0.25 * one,
+          "frequency": 2.0 ** -10 * one, "bias_token": torch.tensor([[4097, 3, 3, 4097]] * n, device="cuda", dtype=torch.int32),
+          "bias": torch.tensor([[9.0, 1.0, 2.0, -0.5]] * n, device="cuda")}
+    out = torch.empty_like(z)
+    dgap_adjust(z, out, **kw)
+    check(z, out, **kw)
+    assert torch.equal(out[:, 4], z[:, 4]) and torch.equal(out[:, 3], z[:, 3] + 2)
+
+
+@pytest.mark.parametrize("history", [10, 40000])
+def test_the_most_biases(history):
+    n, vocab = 2, 6000
+    kw = settings(n, vocab, history, 65535, 0, history)
+    z = torch.randn((n, vocab), device="cuda").half()
+    out = torch.empty_like(z)
+    dgap_adjust(z, out, **kw)
+    check(z, out, **kw)
+
+
 def test_nothing_to_adjust_keeps_every_bit():
     x = torch.arange(65536, device="cuda").int().to(torch.int16).view(torch.float16).view(4, -1)  # every fp16 number
     out = torch.zeros_like(x)

@@ -178,3 +178,25 @@ def test_another_stream():
     side.synchronize()
     assert torch.equal(want, got)
     assert all(np.array_equal(y, z) for y, z in zip(images(a, b, hkv), images(c, b, hkv)))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_queries_that_are_not_finite(dtype, pairs):
+    """Infinities turn to infinities (to NaN where the formula has inf - inf or 0 inf), others in their row stay."""
+    n = 6
+    cos, sin = tables(n, 128)
+    cos[2], sin[2] = 1.25 * cos[2], 1.25 * sin[2]  # (of bf16's largest numbers products overflow fp32)
+    cd, sd = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    q = torch.randn((1, n, 4, 128), device="cuda").to(getattr(torch, dtype))
+    big = torch.finfo(q.dtype).max
+    q[0, :, 0, 3], q[0, :, 1, 70], q[0, :, 2, 11], q[0, :, 3, 90] = float("inf"), -float("inf"), float("nan"), big
+    q[0, 1, 3, 91] = -big
+    k = torch.randn((1, n, 2, 128), device="cuda").to(q.dtype)
+    c = make("i8", 1, 2, 2, n, 32, n, 0)
+    out = c.append_rotary(q, k, k, cd, sd, pairs=pairs).cpu().numpy()[0]
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = rotate(q.double().cpu().numpy()[0], cos, sin, pairs)
+    assert np.isinf(want).any() and np.isnan(want).any()
+    assert np.array_equal(out, want, equal_nan=True)
+    c.check()
