@@ -95,9 +95,13 @@ __device__ __forceinline__ Halves split(float a, float b) {
   return h;
 }
 
-// log2 of a block's value scale; of a block of zeros less than of any other (the
-// smallest scale is 2^-24 / 448).
-__device__ __forceinline__ float log_scale(float s) { return s > 0.f ? __builtin_amdgcn_logf(s) : -34.f; }
+// log2 of a block's value scale.  A block of zeros contributes nothing, but its weights
+// count: in a row's reference it stands as one of scale 2^-80 (the smallest real one is
+// 2^-24 / 448), so that weights of a block of scale s keep their bits while the zeros'
+// scores lie less than 80 + log2 s above theirs.  The sum of weights takes the power out
+// again: up to 2^14 2^80 per token, in range for 2^31 tokens.
+constexpr int kZeros = 80;
+__device__ __forceinline__ float log_scale(float s) { return s > 0.f ? __builtin_amdgcn_logf(s) : -(float)kZeros; }
 
 // The sequence that holds unit u (DecodeSeq::wg_begin: its first unit): the last one
 // that begins at u or before.

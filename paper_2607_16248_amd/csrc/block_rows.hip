@@ -244,9 +244,8 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
   };
   // A block's value scale enters its weights' exponent, p = 2^(score + log2 s_v - m): the
   // reference m goes by what a weight contributes, and numbers of any size keep their
-  // bits next to others.  The sum of the weights takes it out again.  (A block of zeros
-  // contributes nothing: a scale below any other; its scores are 0 at any scale, where a
-  // hidden token's is -inf.)
+  // bits next to others.  The sum of the weights takes it out again.  (Keys of zeros: their
+  // scores are 0 at any scale, where a hidden token's is -inf.)
   float f[2], top[2], alpha[2], up;  // of the block at hand
   auto find_top = [&](int u, const f4_t (&d)[2][2], float2 scale) __attribute__((always_inline)) {
     f[u] = ksc[u] * (scale.x > 0.f ? scale.x : 1.f);
@@ -403,11 +402,11 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     scores(b, d);
     mask(b, d);
     // values enter times the power of two that puts the block's largest at 2^14 or above
-    // (subnormal halves lose bits in products)
+    // (subnormal halves lose bits in products); a block of zeros stands as a packed one
     uint32_t most = 0u;
 #pragma unroll
     for (int w = 0; w < 8; ++w) most = max(most, sm.top[w]);
-    const int lift = block_ops::lift_of(most);
+    const int lift = most == 0u ? block_ops::kZeros : block_ops::lift_of(most);
     const float2 scale = make_float2(1.f, ldexpf(1.f, -lift));
     up = (float)-lift;
     find_top(0, d, scale);
