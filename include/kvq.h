@@ -177,8 +177,11 @@ typedef struct {
  * rotated queries in the form that the attention calls take (rows past n_new[i]
  * are left as they were); NULL where q is.  q_out may not overlap an input.
  * n_max, n_new as in kvq_append.  Rows and tables need their elements' alignment.
- * A given position outside the tables is taken as 0 and reported by kvq_check
- * (KVQ_ERR_RANGE), as is what kvq_append reports.
+ * kvq_check reports (KVQ_ERR_RANGE) a given position outside the tables, taken as 0;
+ * a turned key or a converted value that is not finite in fp16, from this append on,
+ * also where it stays fp16 (attention over it is undefined); and what kvq_append
+ * reports.  Rotated queries are the caller's: they are not looked at, and the attention
+ * calls need finite ones.
  * Errors, before anything is launched or changed: KVQ_ERR_ARG (null or misaligned
  * pointers, strides, type, rotary_dim or table_rows out of range, places past the
  * tables where positions is NULL), and kvq_append's. */

@@ -3,10 +3,11 @@
 Every source is compiled by hipcc with packed fp32 ops disabled; the
 quantize-on-append sources are also built with floating-point contraction
 off: the exact remainder that decides a 4- or 8-bit code takes its roundings
-one by one, fused only where it says so.  The decode sources are built assuming no NaN operands (queries are finite, cached
-values are finite by construction, and the only infinity, the -inf start of
-a running maximum, never meets another): the maxima of the online softmax
-then need no quieting of their inputs.
+one by one, fused only where it says so.  The decode sources are built assuming no NaN operands (queries and appended
+tokens have to be finite, for packed values and rotated tokens the range flag
+says where they were not, and the only infinity, the -inf start of a running
+maximum, never meets another): the maxima of the online softmax then need no
+quieting of their inputs.
 """
 import concurrent.futures as cf
 import os

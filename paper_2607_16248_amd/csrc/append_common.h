@@ -66,7 +66,8 @@ __device__ __forceinline__ PartHead part_head(int local, int parts, int hkv) {
 }
 
 // Copy part `part` (kCopyTokens tokens) of the new tokens that stay fp16 into
-// the ring of head h.
+// the ring of head h.  Turned keys and converted values may have left fp16's range:
+// attention reads them before their group is packed, so they are reported here.
 template <bool AL, int ROT>
 __device__ __forceinline__ void copy_ring(const AppendArgs& a, const RotaryArgs* rot, const AppendSeq& S, int h, int part) {
   uint8_t* blk = a.arena + S.head0 + (uint64_t)h * a.head_stride;
@@ -89,6 +90,7 @@ __device__ __forceinline__ void copy_ring(const AppendArgs& a, const RotaryArgs*
         x[0][i] = turn.apply(x[0][i], g);
 #pragma unroll
         for (int n = 0; n < 4; ++n) x[1][i][n] = rotary::to_half2<ROT>(x[1][i][n]);
+        rotary::report_range(a.arena, x[0][i], x[1][i]);
       }
     }
   }

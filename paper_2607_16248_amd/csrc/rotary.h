@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)a) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16);
 }
 // Inputs as fp16 numbers (exact for fp16; bf16 rounds below 2^-14 and overflows
-// to infinity, which the packing reports).
+// to infinity, which is reported when it enters the cache).
 template <int T>
 __device__ __forceinline__ uint32_t to_half2(uint32_t v) {
   if constexpr (T == kBrain) return pack16(at16<T>(v, 0), at16<T>(v, 1));
@@ -163,6 +163,18 @@ __device__ __forceinline__ int64_t table_row(const RotaryArgs& r, uint8_t* arena
   if (at >= 0 && at < r.rows) return at;
   *reinterpret_cast<volatile uint32_t*>(arena) = 4u;  // KVQ_ERR_RANGE
   return 0;
+}
+
+// Reports halves that are not finite (KVQ_ERR_RANGE).
+__device__ __forceinline__ void report_range(uint8_t* arena, u4_t k, u4_t v) {
+  typedef uint16_t us2_t __attribute__((ext_vector_type(2)));
+  us2_t m = {0, 0};
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(us2_t, k[n] & 0x7FFF7FFFu));
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(us2_t, v[n] & 0x7FFF7FFFu));
+  }
+  if (max(m.x, m.y) >= 0x7C00) *reinterpret_cast<volatile uint32_t*>(arena) = 4u;
 }
 
 // Eight elements of a row, 16 bytes at a time where rows allow it.
