@@ -48,11 +48,11 @@ __device__ __forceinline__ uint32_t to_half2(uint32_t v) {
 }
 
 // Whether the number that v stands for may round to another half than v does: v within
-// 2 ulp of a border of halves, among the subnormal ones, whose borders lie elsewhere, or
-// not finite, which only the 64-bit way tells apart.
+// 2 ulp of a border of halves, among the subnormal ones, whose borders lie elsewhere, zero,
+// whose sign the exact rest has covered, or not finite, which only the 64-bit way tells apart.
 __device__ __forceinline__ bool near_border(float v) {
   const uint32_t u = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
-  return ((u + 0x1002u) & 0x1FFFu) <= 4u || (u < 0x38800000u && u != 0u) || u >= 0x7F800000u;
+  return ((u + 0x1002u) & 0x1FFFu) <= 4u || u < 0x38800000u || u >= 0x7F800000u;
 }
 // d as an fp32 number that rounds to fp16 as d itself does: where the conversion is not
 // exact, its last bit says on which side of every border d is.
