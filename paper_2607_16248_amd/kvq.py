@@ -236,6 +236,8 @@ def kvq_truncate(cache: int, lens: Sequence[int]) -> None:
     """Every sequence keeps its first lens[i] tokens (one length per sequence)."""
     if not all(0 <= n < _I32 for n in lens):
         raise ValueError("lengths are numbers of 32 bits, 0 and above")
+    if cache and (kvq_seq_len(cache, len(lens)) >= 0 or kvq_seq_len(cache, len(lens) - 1) < 0):  # (the call reads one for each)
+        raise ValueError("a length for every sequence of the cache is needed")
     _check(lib().kvq_truncate(cache, (ctypes.c_int32 * max(1, len(lens)))(*lens)))
 
 
