@@ -283,7 +283,9 @@ kvq_status kvq_decode_attention_noalloc(const kvq_cache* cache, const void* q, f
  * calls.  K, V: as for kvq_append, 4-byte aligned.  ws_bytes must cover the
  * lengths after the append (kvq_workspace_bytes covers any length).  Every
  * argument, capacity and workspace check happens before anything is
- * launched, and a failed check leaves the cache unchanged. */
+ * launched, and a failed check leaves the cache unchanged (of the two calls
+ * the second may find no host memory, KVQ_ERR_CAPACITY: the tokens are
+ * appended then, as kvq_seq_len says). */
 kvq_status kvq_append_decode(kvq_cache* cache, const void* K, const void* V, int32_t n_max,
                              const int32_t* n_new, const void* q, float* out, void* ws, size_t ws_bytes,
                              void* stream);

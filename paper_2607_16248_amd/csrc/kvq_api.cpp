@@ -1265,42 +1265,40 @@ kvq_status kvq_append_decode(kvq_cache* c, const void* K, const void* V, int32_t
   // plan with the lengths after the append; nothing is launched or changed
   // unless the workspace fits
   const std::vector<int32_t> L_old = c->L, Lq_old = c->Lq;
+  const auto restore = [&] {
+    c->L = L_old;
+    c->Lq = Lq_old;
+  };
   for (int i = 0; i < d.batch; ++i) {
     c->L[i] = L_old[i] + n_new[i];
     c->Lq[i] = packed_len(c, i, c->L[i]);
   }
-  SplitPlan p;
-  size_t need = 0;
   try {
-    p = c->block ? SplitPlan{} : plan_splits(c);
-    need = c->block ? c->block->need(c, 1, -1, 0) : (size_t)p.records * d.num_q_heads * kvq::kRecFloats * sizeof(float);
-  } catch (const std::bad_alloc&) {
-    c->L = L_old;
-    c->Lq = Lq_old;
+    const SplitPlan p = c->block ? SplitPlan{} : plan_splits(c);
+    const size_t need = c->block ? c->block->need(c, 1, -1, 0) : (size_t)p.records * d.num_q_heads * kvq::kRecFloats * sizeof(float);
+    const char* bad = nullptr;
+    kvq_status bad_st = KVQ_ERR_ARG;
+    if (need > 0 && !ws) bad = "workspace is NULL";
+    else if (ws_bytes < need) bad = "workspace too small for the lengths after the append", bad_st = KVQ_ERR_CAPACITY;
+    else if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) bad = "workspace must be 16-byte aligned";
+    flush |= c->block != nullptr;  // (they have no fused step)
+    if (bad || flush) restore();
+    if (bad) return fail(bad_st, "%s (needs %zu bytes, has %zu)", bad, need, ws_bytes);
+    if (flush) {  // a key group fills: the append kernel packs it, then a plain decode
+      kvq_status st = kvq_append(c, K, V, n_max, n_new, stream);
+      if (st != KVQ_OK) return st;
+      return kvq_decode_attention(c, q, out, ws, ws_bytes, stream);
+    }
+    const FusedAppend app{K, V, n_max, &L_old};
+    kvq_status st = run_partials(c, p, q, ws, ws_bytes, stream, any ? &app : nullptr);
+    if (st != KVQ_OK) return st;
+    st = run_merge(c, p, ws, out, stream);
+    if (st != KVQ_OK) return st;
+    return ok();
+  } catch (const std::bad_alloc&) {  // (before the first launch, which is what stores the tokens)
+    restore();
     throw;
   }
-  const char* bad = nullptr;
-  kvq_status bad_st = KVQ_ERR_ARG;
-  if (need > 0 && !ws) bad = "workspace is NULL";
-  else if (ws_bytes < need) bad = "workspace too small for the lengths after the append", bad_st = KVQ_ERR_CAPACITY;
-  else if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) bad = "workspace must be 16-byte aligned";
-  flush |= c->block != nullptr;  // (they have no fused step)
-  if (bad || flush) {
-    c->L = L_old;
-    c->Lq = Lq_old;
-  }
-  if (bad) return fail(bad_st, "%s (needs %zu bytes, has %zu)", bad, need, ws_bytes);
-  if (flush) {  // a key group fills: the append kernel packs it, then a plain decode
-    kvq_status st = kvq_append(c, K, V, n_max, n_new, stream);
-    if (st != KVQ_OK) return st;
-    return kvq_decode_attention(c, q, out, ws, ws_bytes, stream);
-  }
-  const FusedAppend app{K, V, n_max, &L_old};
-  kvq_status st = run_partials(c, p, q, ws, ws_bytes, stream, any ? &app : nullptr);
-  if (st != KVQ_OK) return st;
-  st = run_merge(c, p, ws, out, stream);
-  if (st != KVQ_OK) return st;
-  return ok();
 } catch (const std::bad_alloc&) {
   return no_memory();
 }
