@@ -64,6 +64,7 @@ int32_t row_units(const kvq_cache* c, int i, const Rows& r, int32_t window, int3
 
 // Workgroups of a launch, where there is work for so many: as many as are resident.
 int64_t workgroups(const Rows& r) { return (r.waves == 8 ? 1 : 2) * kvq::target_workgroups(1); }
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 22) - 1;  // of up to 512 threads: a launch's threads stay below 2^32
 constexpr int kMinBlocks = 4;  // 32-token blocks per workgroup at least (tiles: one per wave)
 
 // Tiles: units that stand for a row group's beginning and end (queries, joined waves,
@@ -125,8 +126,9 @@ Plan plan_for(const kvq_cache* c, int nqry, int32_t window, int32_t sinks) {
     }
     const int64_t least = r.waves ? kMinBlocks : (kMinBlocks * 32 + G - 1) / G;
     int64_t per = std::max<int64_t>({(total + workgroups(r) - 1) / workgroups(r), least, 1});
-    if (c->split_tokens > 0) per = c->split_tokens / (r.waves ? 32 : G);
-    p.fits &= total + per < INT32_MAX && (total + per - 1) / per < (int64_t)1 << 22;
+    // (forced splits: as many as one launch takes at most, longer ones where there would be more)
+    if (c->split_tokens > 0) per = std::max<int64_t>(c->split_tokens / (r.waves ? 32 : G), (total + kMostWorkgroups - 1) / kMostWorkgroups);
+    p.fits &= total + per < INT32_MAX;
     p.per.push_back((int32_t)per);
     p.extra.push_back(extra);
     p.total.push_back((int32_t)std::min<int64_t>(total, INT32_MAX));
