@@ -234,10 +234,14 @@ def kvq_seq_release(cache: int, seq: int) -> None:
 
 def kvq_truncate(cache: int, lens: Sequence[int]) -> None:
     """Every sequence keeps its first lens[i] tokens (one length per sequence)."""
-    if not all(0 <= n < _I32 for n in lens):
-        raise ValueError("lengths are numbers of 32 bits, 0 and above")
     if cache and (kvq_seq_len(cache, len(lens)) >= 0 or kvq_seq_len(cache, len(lens) - 1) < 0):  # (the call reads one for each)
         raise ValueError("a length for every sequence of the cache is needed")
+    _truncate(cache, lens)
+
+
+def _truncate(cache: int, lens: Sequence[int]) -> None:
+    if not all(0 <= n < _I32 for n in lens):
+        raise ValueError("lengths are numbers of 32 bits, 0 and above")
     _check(lib().kvq_truncate(cache, (ctypes.c_int32 * max(1, len(lens)))(*lens)))
 
 
@@ -604,7 +608,7 @@ class KVCache:
         """Keep the first lens[i] tokens of every sequence (those after them are dropped)."""
         if len(lens) != self.batch:
             raise ValueError(f"{self.batch} lengths are needed")
-        kvq_truncate(self.handle, lens)
+        _truncate(self.handle, lens)
 
     def seq_len(self, seq):
         return kvq_seq_len(self.handle, seq)
