@@ -401,12 +401,15 @@ __device__ __forceinline__ void attend_rows(const DecodeArgs& a, const Part& wk,
     f4_t d[2][2];
     scores(b, d);
     mask(b, d);
-    // values enter times the power of two that puts the block's largest at 2^14 or above
-    // (subnormal halves lose bits in products); a block of zeros stands as a packed one
+    // values enter times the power of two that puts the block's largest at 2^7 or above: out
+    // of reach of subnormal halves, which lose bits in products, and no further, since what
+    // values are larger than codes their weights are smaller, and lose bits beside packed
+    // blocks (at 2^14: 6e-4 of a row's output beside a scale 2^15 times its own).  A block
+    // of zeros stands as a packed one.
     uint32_t most = 0u;
 #pragma unroll
     for (int w = 0; w < 8; ++w) most = max(most, sm.top[w]);
-    const int lift = most == 0u ? block_ops::kZeros : block_ops::lift_of(most);
+    const int lift = most == 0u ? block_ops::kZeros : max(block_ops::lift_of(most) - 7, 0);
     const float2 scale = make_float2(1.f, ldexpf(1.f, -lift));
     up = (float)-lift;
     find_top(0, d, scale);
