@@ -224,13 +224,20 @@ typedef struct {
  * The handle goes to every call that takes a kvq_cache, with these differences:
  * kvq_append_decode runs as kvq_append and kvq_decode_attention,
  * kvq_decode_partials and kvq_decode_merge answer KVQ_ERR_UNSUPPORTED,
- * kvq_dequant gives code * s rounded once to fp32, attention is within 1e-5
- * (2-norm) of the exact one over these values, kvq_export's image is
+ * kvq_dequant gives code * s rounded once to fp32, kvq_export's image is
  *   key codes [Lq][128] | key scales [Lq/block_tokens] fp32 | value codes
  *   [Lq][128] | value scales [Lq/block_tokens] fp32 | key tail [L-Lq][128] fp16 |
  *   value tail [L-Lq][128] fp16
  * (KVQ_I8 codes as two's complement bytes), and the workspaces of decode, chunk and
  * window calls do not grow with the batch beyond what their splits write.
+ * Attention over these values is exact but for, in every element of an output,
+ *   (2^-19 A + 2^-17) sum_t w_t |V^_t| + 2^-31 n max_t w_t m_t
+ * over the row's n visible tokens: w_t their softmax weights, A their largest
+ * sum_c |q_c K^_c| log2(e) / sqrt(d), m_t the largest magnitude in token t's block,
+ * visible or not (fp16 tail: of 32 tokens).  The second part matters where tokens of
+ * weight are far smaller than others of their block, and further tokens too; where
+ * blocks are of like size 2-norm errors are about 1e-6.  Sums over millions of tokens
+ * add their roundings, 2^-24 for each 32 tokens that one wave takes.
  * Errors as kvq_cache_init's; kvq_block_cache_bytes gives 0 for an invalid
  * descriptor. */
 size_t kvq_block_cache_bytes(const kvq_block_desc* desc);
@@ -367,8 +374,9 @@ size_t kvq_window_workspace_bytes(const kvq_cache* cache, int32_t n_q, int32_t w
  * [batch][n_q][Hq][d]; ws: device scratch of ws_bytes >=
  * kvq_window_workspace_bytes(cache, n_q, window, sinks), 16-byte aligned,
  * contents undefined on entry and exit; calls that may overlap take one each.
- * Results are within 1e-5 (2-norm) of the exact ones, and bitwise
- * reproducible for a fixed split setting.
+ * Results are within 1e-5 (2-norm) of the exact ones (block-scaled caches: what
+ * kvq_block_cache_init states), and bitwise reproducible for a fixed split
+ * setting.
  * Errors: KVQ_ERR_ARG (n_q, window or sinks out of range, a sequence shorter
  * than n_q > 1, null pointers, misaligned workspace), KVQ_ERR_CAPACITY
  * (workspace too small, no host memory), KVQ_ERR_HIP. */
