@@ -234,10 +234,10 @@ typedef struct {
  *   (2^-19 A + 2^-17) sum_t w_t |V^_t| + 2^-31 n max_t w_t m_t
  * over the row's n visible tokens: w_t their softmax weights, A their largest
  * sum_c |q_c K^_c| log2(e) / sqrt(d), m_t the largest magnitude in token t's block,
- * visible or not (fp16 tail: of 32 tokens).  The second part matters where tokens of
- * weight are far smaller than others of their block, and further tokens too; where
- * blocks are of like size 2-norm errors are about 1e-6.  Sums over millions of tokens
- * add their roundings, 2^-24 for each 32 tokens that one wave takes.
+ * visible or not (fp16 tail: of 32 tokens).  The second part counts where a row's
+ * weight lies on tokens far smaller than the largest of their block; where blocks are
+ * of like size 2-norm errors are about 1e-6.  Sums over millions of tokens add their
+ * roundings, 2^-24 for each 32 tokens that one wave takes.
  * Errors as kvq_cache_init's; kvq_block_cache_bytes gives 0 for an invalid
  * descriptor. */
 size_t kvq_block_cache_bytes(const kvq_block_desc* desc);

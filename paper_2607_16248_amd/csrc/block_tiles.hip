@@ -25,8 +25,10 @@
 // Single tokens are bound by memory: 32 sequences of 9000 to 16384 tokens, 8 kv heads,
 // 847 MB of e4m3, 143 us (5.9 TB/s; a reading probe reaches 6.4).  With 32 rows (five
 // queries of four heads over 4 sequences of 20000 to 32768 tokens, 222 MB) it is the
-// latency of a wave's block, whose products and weights follow one another: 75 us
-// (3.0 TB/s).  Two blocks of a wave in turn cost more in registers than they gave.
+// latency of a wave's block, whose products and weights follow one another, and the
+// registers: two tiles take all 256 and spill 62 (252 bytes of scratch a lane; one tile
+// takes 207 to 209 and spills none): 75 us (3.0 TB/s).  Over 4 sequences of 32768 one query
+// takes 50 us, four (one tile) 59, five (two) 70.  Two blocks of a wave in turn need more.
 #include <hip/hip_runtime.h>
 
 #include "block_ops.h"

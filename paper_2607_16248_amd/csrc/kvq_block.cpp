@@ -27,7 +27,8 @@ struct Rows {
 // Many rows from so many (query, head) rows of a kv head on.  32 query and 8 kv heads,
 // e4m3, 16 sequences of 8000 to 16384 tokens: 64 rows 169 us in tiles and 199 in the other
 // kernel, 128 rows 281 and 189; one sequence of 16384: 64 rows 40 and 43, 96 rows 42 and
-// 46, 128 rows 49 and 51, 256 rows 50 and 50, 512 rows 78 and 73.
+// 46, 128 rows 49 and 51, 256 rows 50 and 50, 512 rows 78 and 73.  One number for both:
+// between 96 and 256 rows one sequence loses up to 4 us to what a batch gains (92).
 constexpr int kManyRows = 96;
 
 Rows rows_for(const kvq_cache* c, int nqry) {
